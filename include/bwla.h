@@ -422,6 +422,145 @@ BWLA_API bwla_status_t bwla_probe_clock(void* d_out, void* stream);
 BWLA_API bwla_status_t bwla_probe_load_latency(const void* d_buf, size_t bytes, size_t stride_bytes, int iters,
                                                void* d_out, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Between the merged q|k|v projection of a decoder block and its o projection: rotary positions, a
+ * key-value cache in pages, the attention that reads it, and eviction from it.  The conventions above
+ * hold; rows and pages need 16-byte alignment.  Integer arrays on the device are not validated on the
+ * host: a page number outside [0, pages) is a page that holds nothing (nothing is read or written
+ * there), a length is cut to [0, max_len], positions of the rotary tables are cut to their rows.
+ * ------------------------------------------------------------------------------------------- */
+
+/* Limits (violations give BWLA_ERR_UNSUPPORTED). */
+#define BWLA_MAX_HEAD_DIM 256       /* also a multiple of 8 */
+#define BWLA_MAX_CACHE_LEN (1 << 24) /* tokens of one sequence */
+#define BWLA_MAX_HEADS 1024         /* query heads; a multiple of the key-value heads */
+
+/*
+ * Keys and values in pages: element (page p, head h, slot s, column c) lies p * page_stride +
+ * h * head_stride + s * slot_stride + c elements behind d_k or d_v.  Strides in elements, multiples of
+ * 16 bytes; the products are taken in 64 bits.  page_size is a power of two.
+ */
+typedef struct bwla_kv_cache {
+    void *d_k, *d_v;
+    int64_t page_stride, head_stride, slot_stride;
+    int64_t pages;
+    int32_t page_size, kv_heads, head_dim;
+    int32_t dtype;                  /* bwla_xdtype_t of keys, values, queries and outputs */
+} bwla_kv_cache_t;
+
+/*
+ * The sequences of a call.  Cached token j of sequence b lies in slot j % page_size of page
+ * d_table[b * table_stride + j / page_size].  d_len[b] counts its cached tokens, the new ones included:
+ * they are its last.  Its new tokens are the rows d_first[b] to d_first[b + 1] - 1 of the call's
+ * queries; d_first = NULL: one each, row b.  `tokens` is the number of rows, max_new and max_len are at
+ * least the most new and the most cached tokens of a sequence (what goes beyond them is left out).
+ */
+typedef struct bwla_kv_batch {
+    const int32_t* d_table;
+    const int32_t* d_len;
+    const int32_t* d_first;
+    int64_t tokens;
+    int32_t sequences, table_stride, max_new, max_len;
+} bwla_kv_batch_t;
+
+/*
+ * How a query and a key make a score.  With i, p the query's index in the cache and its position, j, r
+ * the key's (the index is the position where d_position is NULL):
+ *   seen   = the key's page exists, doc[i] = doc[j] >= 0, and (j < prefix or j <= i and p - r < window)
+ *   score  = capped(scale q.k) - slope_h |p - r|,  capped(x) = cap tanh(x / cap)
+ * cap = 0: no cap; window = 0: none; any pointer may be NULL.  d_slopes has an entry for each query
+ * head, d_prefix one for each sequence; d_doc and d_position are sequences x index_stride.
+ * Stored keys and values of tokens that a query of the call sees are finite; what lies in slots behind
+ * a sequence's length, in pages that no table names, or in tokens that no query of a sequence sees may
+ * be anything.
+ */
+typedef struct bwla_score {
+    const float* d_slopes;
+    const int32_t* d_prefix;
+    const int32_t* d_doc;
+    const int32_t* d_position;
+    float scale, cap;
+    int32_t window, index_stride;
+} bwla_score_t;
+
+/*
+ * Rotary positions.  Column pair i < pairs of a head (columns i and pairs + i, or 2 i and 2 i + 1 with
+ * `interleaved`) is turned by the angle whose cosine and sine are d_cos, d_sin[row * pairs + i], row
+ * being the token's position on the pair's axis: the first sections[0] pairs are on axis 0, the next
+ * sections[1] on axis 1, and so on (one to four axes; the sections add up to `pairs`).  Columns from
+ * 2 * pairs on stay.
+ */
+typedef struct bwla_rope {
+    const float *d_cos, *d_sin;
+    int32_t rows, pairs, axes, interleaved;
+    int32_t sections[4];
+} bwla_rope_t;
+
+/*
+ * Rotate the queries and keys of a merged projection's rows and write them where the attention reads
+ * them.  d_position: axes x tokens.  d_qkv: tokens rows of (q_heads + 2 kv_heads) * head_dim values, query heads first, then keys,
+ * then values, row_stride elements apart.  Queries go to d_q (tokens x q_heads x head_dim, dense); keys and
+ * values to the new tokens' slots of the cache, all in the cache's type (nearest even).  d_weights (may
+ * be NULL; see bwla_attention_forward): the slots' sums are set to zero.  d_cache_position (may be NULL;
+ * sequences x position_stride): gets the new tokens' positions on axis 0, at their index in the cache.
+ * No page is written by two sequences of one call.
+ */
+BWLA_API bwla_status_t bwla_rope_append(const bwla_kv_cache_t* cache, const bwla_kv_batch_t* batch, const bwla_rope_t* rope,
+                               const int32_t* d_position, const void* d_qkv, int x_dtype, int64_t row_stride, int32_t q_heads, void* d_q,
+                               float* d_weights, int32_t* d_cache_position, int32_t position_stride, void* stream);
+
+/*
+ * Softmax attention of each sequence's new tokens over its cache (their own keys included: append
+ * first).  d_q: tokens rows of q_heads * head_dim, q_stride elements apart; query head h reads key-value
+ * head h / (q_heads / kv_heads).  d_out: tokens x q_heads x head_dim, dense; a row that sees nothing is 0.
+ * d_lse (may be NULL): tokens x q_heads, the logarithm of the sum of exp(score) over what is seen, -inf
+ * where that is nothing.
+ * d_weights (may be NULL; needs d_lse): pages x kv_heads x page_size floats, dense; each seen token's softmax weights,
+ * summed over the sequence's new tokens and the query heads of a group, are added at its slot.  A page
+ * is named by one sequence only then.
+ * Any number of new tokens: few rows over a long cache are split over its length and joined.
+ * d_ws: scratch of bwla_attention_workspace_size bytes (`weights`: whether d_weights is given); any
+ * contents.  Calls that share one must not overlap.  The same call on the same data gives the same bits.
+ */
+BWLA_API bwla_status_t bwla_attention_workspace_size(const bwla_kv_cache_t* cache, const bwla_kv_batch_t* batch,
+                                            int32_t q_heads, int weights, size_t* bytes);
+BWLA_API bwla_status_t bwla_attention_forward(const bwla_kv_cache_t* cache, const bwla_kv_batch_t* batch,
+                                     const bwla_score_t* score, const void* d_q, int64_t q_stride, int32_t q_heads,
+                                     void* d_out, float* d_lse, float* d_weights, void* d_ws, size_t ws_bytes,
+                                     void* stream);
+
+/*
+ * The sums of weights on their own: adds exp(score - lse) of the call's queries at each seen token's
+ * slot of d_weights, as above, from a lse that an attention call of the same queries left.  d_lse may
+ * belong to more rows than this call has (the last queries of a prompt only: the batch then counts
+ * these as its new tokens, and d_q and d_lse point at them).
+ */
+BWLA_API bwla_status_t bwla_attention_weights_workspace_size(const bwla_kv_cache_t* cache, const bwla_kv_batch_t* batch,
+                                                    int32_t q_heads, size_t* bytes);
+BWLA_API bwla_status_t bwla_attention_weights(const bwla_kv_cache_t* cache, const bwla_kv_batch_t* batch,
+                                     const bwla_score_t* score, const void* d_q, int64_t q_stride, int32_t q_heads,
+                                     const float* d_lse, float* d_weights, void* d_ws, size_t ws_bytes, void* stream);
+
+/*
+ * Cut each sequence to its `keep` heaviest tokens, in order, in pages of their own.  A token's weight is
+ * the sum of its d_weights over the key-value heads, taken in 64 bits and rounded once to fp32; NaN counts as
+ * -inf.  The first `sinks` and the last `recent` tokens come before all others (sinks + recent <= keep),
+ * then the heaviest, ties to the lowest index; tokens whose page does not exist are not kept.
+ * Kept token n of sequence b goes to slot n % page_size of page d_table_out[b * table_out_stride +
+ * n / page_size]: its key, its value and its sums.  These pages are named by nothing else in the call
+ * (pages that sequences share stay whole).  d_len_out[b]: tokens kept.  d_kept (sequences x keep; may be NULL):
+ * their indices, -1 behind them.  d_position, d_position_out (may be NULL both; sequences x position_stride
+ * and sequences x keep): the kept tokens' entries, -1 behind them.
+ * d_first, max_new and tokens of the batch are not used.
+ */
+BWLA_API bwla_status_t bwla_cache_evict_workspace_size(const bwla_kv_cache_t* cache, const bwla_kv_batch_t* batch,
+                                              size_t* bytes);
+BWLA_API bwla_status_t bwla_cache_evict(const bwla_kv_cache_t* cache, const bwla_kv_batch_t* batch,
+                               const int32_t* d_table_out, int32_t table_out_stride, float* d_weights, int32_t keep,
+                               int32_t sinks, int32_t recent, int32_t* d_len_out, int32_t* d_kept,
+                               const int32_t* d_position, int32_t position_stride, int32_t* d_position_out, void* d_ws,
+                               size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -23,7 +23,10 @@ EXPORTS = ["bwla_status_string", "bwla_version", "bwla_kron_factor", "bwla_packe
            "bwla_probe_mfma_int8", "bwla_decode_forward_launches", "bwla_decode_forward_bits", "bwla_pack_codes_a4",
            "bwla_linear_forward_a4", "bwla_probe_empty_launch", "bwla_probe_load_latency", "bwla_probe_clock",
            "bwla_linear_forward_bits", "bwla_linear_forward_swiglu_bits", "bwla_code_room_size", "bwla_decode_forward_room",
-           "bwla_linear_forward_room", "bwla_linear_forward_swiglu_room", "bwla_linear_forward_kernel"]
+           "bwla_linear_forward_room", "bwla_linear_forward_swiglu_room", "bwla_linear_forward_kernel",
+           # marshalled in attention_binding.py
+           "bwla_rope_append", "bwla_attention_workspace_size", "bwla_attention_forward", "bwla_attention_weights_workspace_size",
+           "bwla_attention_weights", "bwla_cache_evict_workspace_size", "bwla_cache_evict"]
 
 
 class BwlaLayer(Structure):

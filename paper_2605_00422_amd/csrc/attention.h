@@ -1,0 +1,164 @@
+// What the kernels between the q|k|v and the o projection share: the arguments, where a cached token lies,
+// what a query sees, and how a product becomes a score.
+//
+// Scores are kept in base 2 throughout: y = score * log2(e), weights are exp2(y - m).  With the product
+// a = q.k that is y = a * c1 without a cap (c1 = scale log2 e, positive), C tanh(a * c2) with one
+// (C = cap log2 e, c2 = scale / cap), minus slope log2(e) |p - r| with a bias.
+#pragma once
+#include <type_traits>
+
+#include "bwla_internal.h"
+
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+
+constexpr float ATT_LOG2E = 1.4426950408889634f;
+constexpr float ATT_LN2 = 0.6931471805599453f;
+
+struct AttArgs {
+    const char *k, *v;
+    const char* q;
+    char* out;
+    float* lse;
+    float* weights;
+    const int32_t *table, *len, *first;
+    const float* slopes;
+    const int32_t *prefix, *doc, *pos;
+    int64_t page_bytes, head_bytes, slot_bytes, q_bytes;   // strides of pages, heads, slots; of the rows of q
+    int64_t tokens;
+    int32_t pages, page_shift, hkv, hq, group, d;
+    int32_t seqs, table_stride, max_new, max_len, index_stride;
+    int32_t window;                                        // INT32_MAX: none
+    float c1, c2, capped;                                  // capped: C, 0: no cap
+};
+
+// launchers (attention_tile_*.hip, attention_split.hip, attention_weights.hip, attention_rope.hip, cache_evict.hip)
+hipError_t bwla_launch_attention_tile(const AttArgs& a, int dtype, hipStream_t st);
+hipError_t bwla_launch_attention_tile_f32(const AttArgs& a, hipStream_t st);
+
+// few rows over a long cache: how the cache's length is split
+struct AttSplit {
+    int chunk, splits;       // cached tokens of one workgroup; workgroups along the longest sequence
+    int rows;                // rows of a sequence and key-value head: new tokens x group
+    int row_tiles;           // tiles of 16 rows
+    int pitch;               // cached tokens of a row of the scores that the sums of weights read
+    size_t part_bytes, stat_bytes, score_bytes;
+};
+AttSplit bwla_att_split(const AttArgs& a, bool weights);
+bool bwla_att_is_split(const AttArgs& a);
+hipError_t bwla_launch_attention_split(const AttArgs& a, const AttSplit& s, int dtype, void* ws, hipStream_t st);
+
+struct AttWeightsPlan {
+    int parts;               // the rows of a sequence and key-value head are dealt out over this many workgroups
+    size_t bytes;            // scratch for their sums (0: one part)
+};
+AttWeightsPlan bwla_att_weights_plan(const AttArgs& a, int dtype);
+hipError_t bwla_launch_attention_weights(const AttArgs& a, int dtype, void* ws, hipStream_t st);
+
+struct RopeArgs {
+    const char* qkv;
+    char *k, *v, *q;
+    const float *cos, *sin;
+    const int32_t *pos, *table, *len, *first;
+    float* weights;
+    int32_t* cache_pos;
+    int64_t page_stride, head_stride, slot_stride, row_stride, tokens;    // elements
+    int32_t pages, page_shift, hkv, hq, d, seqs, table_stride, max_new, max_len, pos_stride;
+    int32_t rows, pairs, axes, interleaved;
+    int32_t ends[4];                                       // first pair behind each axis's section
+};
+hipError_t bwla_launch_rope(const RopeArgs& a, int x_dtype, int dtype, hipStream_t st);
+
+struct EvictArgs {
+    char *k, *v;
+    float* weights;
+    const int32_t *table, *len, *table_out, *pos;
+    int32_t *len_out, *kept, *pos_out;
+    uint32_t* keys;                                        // scratch: seqs x max_len, weights as ordered integers
+    int32_t* list;                                         // scratch: seqs x max_len, kept tokens
+    int64_t page_bytes, head_bytes, slot_bytes;
+    int32_t pages, page_shift, hkv, row_bytes, seqs, table_stride, table_out_stride, max_len;
+    int32_t keep, sinks, recent, pos_stride;
+};
+hipError_t bwla_launch_evict(const EvictArgs& a, hipStream_t st);
+
+#ifdef __HIPCC__
+// A sequence as the kernels see it: what lies outside the caller's bounds is cut off here, once
+struct AttSeq {
+    int n, fresh, row0;      // cached tokens, new ones among them, first row of q
+    int prefix;
+    const int32_t *table, *doc, *pos;
+};
+__device__ __forceinline__ AttSeq att_seq(const AttArgs& a, int b) {
+    AttSeq s;
+    s.n = min(max(a.len[b], 0), a.max_len);
+    int64_t row0 = b, fresh = 1;
+    if (a.first) {
+        row0 = a.first[b];
+        fresh = (int64_t)a.first[b + 1] - row0;
+    }
+    if (row0 < 0 || row0 > a.tokens) { row0 = 0; fresh = 0; }
+    if (fresh > a.tokens - row0) fresh = a.tokens - row0;
+    s.fresh = (int)min(max(fresh, (int64_t)0), (int64_t)a.max_new);
+    s.row0 = (int)row0;
+    s.prefix = a.prefix ? min(a.prefix[b], s.n) : 0;
+    s.table = a.table + (int64_t)b * a.table_stride;
+    s.doc = a.doc ? a.doc + (int64_t)b * a.index_stride : nullptr;
+    s.pos = a.pos ? a.pos + (int64_t)b * a.index_stride : nullptr;
+    return s;
+}
+
+// A row of the products: new token t of the sequence, as the mask and the bias see it
+struct AttRow {
+    int i, p, doc;           // index in the cache (-1: the row sees nothing), position, document
+};
+__device__ __forceinline__ AttRow att_row(const AttSeq& s, int t, bool live) {
+    AttRow r;
+    r.i = live ? s.n - s.fresh + t : -1;
+    if (r.i < 0) { r.i = -1; r.p = 0; r.doc = -2; return r; }
+    r.p = s.pos ? max(s.pos[r.i], 0) : r.i;
+    r.doc = s.doc ? s.doc[r.i] : 0;
+    if (r.doc < 0) r.doc = -2;
+    return r;
+}
+// A cached token: its position, and its document, -1 where it does not exist (doc of a token in none: -1 too)
+struct AttKey {
+    int p, doc;
+};
+__device__ __forceinline__ AttKey att_key(const AttArgs& a, const AttSeq& s, int j, bool there) {
+    AttKey k;
+    const bool ok = there && j < s.n;
+    k.p = s.pos && ok ? max(s.pos[j], 0) : j;
+    k.doc = ok ? (s.doc ? max(s.doc[j], -1) : 0) : -1;
+    return k;
+}
+__device__ __forceinline__ bool att_sees(const AttRow& r, int prefix, int window, int j, int kp, int kdoc) {
+    return r.doc == kdoc && r.i >= 0 && (j < prefix || (j <= r.i && r.p - kp < window));
+}
+
+// tanh to one or two units of the last place: below 0.6 an odd polynomial (degree 11, fitted to tanh(x) / x in
+// x^2, relative error 2.5e-9 before rounding), above by the exponential
+__device__ __forceinline__ float att_tanh(float x) {
+    const float u = x * x;
+    float p = -0.00585642786f;
+    p = fmaf(p, u, 0.0207574754f);
+    p = fmaf(p, u, -0.0537699218f);
+    p = fmaf(p, u, 0.133317047f);
+    p = fmaf(p, u, -0.33333284f);
+    p = fmaf(p * u, x, x);
+    const float e = __builtin_amdgcn_exp2f(fabsf(x) * (2.f * ATT_LOG2E));
+    const float big = copysignf(1.f - 2.f * __builtin_amdgcn_rcpf(1.f + e), x);
+    return fabsf(x) < 0.6f ? p : big;
+}
+__device__ __forceinline__ float att_score(const AttArgs& a, float prod) {
+    return a.capped != 0.f ? a.capped * att_tanh(prod * a.c2) : prod * a.c1;
+}
+
+__device__ __forceinline__ uint32_t att_pack_bf16(float lo, float hi) {
+    typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+    v2bf r;
+    r[0] = (__bf16)lo;
+    r[1] = (__bf16)hi;
+    return __builtin_bit_cast(uint32_t, r);
+}
+#endif

@@ -1,0 +1,403 @@
+// Attention of few rows over a long cache (decoding): the cache's length is split over workgroups, and a
+// second launch joins their parts.
+//
+// The products' rows are the new tokens times the query heads of one key-value head, 16 to a tile, so that a
+// group of heads reads its keys and values once.  A wavefront takes 32 cached tokens a step and keeps them in
+// registers from load to use, with no LDS: S^T = K Q^T on 16x16 MFMA has the keys as rows, read as they lie
+// (64 bytes of 16 keys an instruction), and leaves lane (row r = lane & 15, g = lane >> 4) the scores of keys 4g
+// to 4g + 3, which is the order in which the second product O^T = V^T P^T contracts.  Its operand V^T is
+// gathered from rows of V by byte permutes: lane m reads columns 8m to 8m + 7 of its four keys, whole rows of
+// 256 bytes side by side, and tile c of the result holds columns 8m + c.
+// Softmax: running maximum and sum in fp32 per wavefront, joined over the four wavefronts in LDS and over the
+// splits in att_join_kernel, in a fixed order.  Weights enter the second product in the cache's type.
+#include "attention.h"
+
+namespace {
+
+constexpr int SP_WAVES = 4;
+constexpr int SP_STEP = 32;                    // cached tokens of a step of one wavefront
+constexpr int SP_MAX_CHUNK = 2048;
+
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ float xor16(float v, bool max_of) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    const float a = __uint_as_float(r[0]), b = __uint_as_float(r[1]);
+    return max_of ? fmaxf(a, b) : a + b;
+}
+__device__ __forceinline__ float xor32(float v, bool max_of) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    const float a = __uint_as_float(r[0]), b = __uint_as_float(r[1]);
+    return max_of ? fmaxf(a, b) : a + b;
+}
+
+// BF: bf16 (else fp32); DP: columns, 64, 128 or 256; EXACT: d == DP (else columns from d on count as zero)
+template <bool BF, int DP, bool EXACT>
+__global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, AttSplit sp, float* __restrict__ part,
+                                                                 float2* __restrict__ stat, float* __restrict__ scores) {
+    constexpr int ES = BF ? 2 : 4;
+    constexpr int KS = DP * ES / 64;           // 64-byte steps along a row of K
+    constexpr int CW = DP >= 128 ? 8 : DP / 16;  // columns of a lane side by side
+    constexpr int U = DP / 16 / CW;
+    constexpr int NT = U * CW;                 // column tiles of the result
+    constexpr int VB = CW * ES;                // bytes of those columns
+    constexpr int VD = VB / 4;                 // ... in dwords
+    __shared__ int tab[SP_MAX_CHUNK + 8];
+    __shared__ float s_m[SP_WAVES][16], s_l[SP_WAVES][16], s_mm[16], s_ll[16];
+    __shared__ __align__(16) float s_o[SP_WAVES][16][DP + 4];
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, g = lane >> 4;
+    const int split = blockIdx.x, h = blockIdx.y / sp.row_tiles, rt = blockIdx.y - h * sp.row_tiles, b = blockIdx.z;
+    const AttSeq s = att_seq(a, b);
+    const int rows = s.fresh * a.group, row = rt * 16 + li;
+    if (rt * 16 >= rows) return;
+    const int64_t unit = ((int64_t)b * a.hkv + h) * sp.row_tiles + rt;
+    const int c0 = split * sp.chunk, c1 = min(c0 + sp.chunk, s.n);
+    // where no position and no row count says otherwise, keys in front of the first row's window are not read
+    const int i_first = s.n - s.fresh + rt * 16 / a.group;
+    const int skip_to = (s.pos || a.window == INT32_MAX) ? 0 : i_first - a.window + 1;
+    const bool none = c0 >= c1 || (c1 <= skip_to && c0 >= s.prefix);
+    if (none && sp.splits > 1) {
+        if (threadIdx.x < 16) stat[(unit * sp.splits + split) * 16 + threadIdx.x] = make_float2(-INFINITY, 0.f);
+        if (scores) {                          // (what the sums of weights read of it)
+            for (int r = 0; r < 16 && rt * 16 + r < rows; ++r)
+                for (int j = c0 + threadIdx.x; j < c1; j += 64 * SP_WAVES)
+                    scores[((int64_t)(b * a.hkv + h) * sp.rows + rt * 16 + r) * sp.pitch + j] = -INFINITY;
+        }
+        return;
+    }
+    const int e0 = c0 >> a.page_shift;
+    const int entries = c1 > c0 ? ((c1 - 1) >> a.page_shift) - e0 + 1 : 0;
+    for (int e = threadIdx.x; e < entries; e += 64 * SP_WAVES) {
+        const int p = s.table[e0 + e];
+        tab[e] = (unsigned)p < (unsigned)a.pages ? p : -1;
+    }
+    // this lane's row
+    const int tok = row / a.group, head = h * a.group + row - tok * a.group;
+    const AttRow me = att_row(s, tok, row < rows);
+    const float slope = a.slopes && row < rows ? a.slopes[head] * ATT_LOG2E : 0.f;
+    v4u qf[KS];
+    {
+        const char* qp = a.q + (int64_t)(s.row0 + (row < rows ? tok : 0)) * a.q_bytes +
+                         (int64_t)(row < rows ? head : 0) * a.d * ES + 16 * g;
+#pragma unroll
+        for (int t = 0; t < KS; ++t) {
+            const bool in = row < rows && (EXACT || 64 * t + 16 * g < a.d * ES);
+            qf[t] = in ? *(const v4u*)(qp + 64 * t) : v4u{0, 0, 0, 0};
+        }
+    }
+    __syncthreads();
+
+    v4f o[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) o[t] = v4f{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
+    const char* kh = a.k + (int64_t)h * a.head_bytes;
+    const char* vh = a.v + (int64_t)h * a.head_bytes;
+    const int slot_mask = (1 << a.page_shift) - 1;
+
+    for (int j0 = c0 + wave * SP_STEP; j0 < c1; j0 += SP_WAVES * SP_STEP) {
+        // pages hold 8 tokens at least, so a lane's four keys of V lie in one; tokens from c1 on read the last one's row
+        v4u kf[2][KS];
+        uint32_t vf[2][4][U][VD];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int j = min(j0 + 16 * t + li, c1 - 1);
+            const int p = max(tab[(j >> a.page_shift) - e0], 0);
+            const char* src = kh + (int64_t)p * a.page_bytes + (int64_t)(j & slot_mask) * a.slot_bytes + 16 * g;
+#pragma unroll
+            for (int u = 0; u < KS; ++u) {
+                if (EXACT || 64 * u + 16 * g < a.d * ES) kf[t][u] = *(const v4u*)(src + 64 * u);
+                else kf[t][u] = v4u{0, 0, 0, 0};
+            }
+        }
+        int page_v[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int jv = j0 + 16 * t + 4 * g;
+            page_v[t] = tab[(min(jv, c1 - 1) >> a.page_shift) - e0];
+            const char* src = vh + (int64_t)max(page_v[t], 0) * a.page_bytes;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const char* rowp = src + (int64_t)(min(jv + r, c1 - 1) & slot_mask) * a.slot_bytes + li * VB;
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const bool in = EXACT || u * 16 * VB + li * VB < a.d * ES;
+                    if constexpr (VD >= 4) {
+#pragma unroll
+                        for (int w = 0; w < VD / 4; ++w) {
+                            const v4u x = in ? *(const v4u*)(rowp + u * 16 * VB + 16 * w) : v4u{0, 0, 0, 0};
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) vf[t][r][u][4 * w + e] = x[e];
+                        }
+                    } else {
+                        const v2u x = in ? *(const v2u*)(rowp + u * 16 * VB) : v2u{0, 0};
+                        vf[t][r][u][0] = x[0];
+                        vf[t][r][u][1] = x[1];
+                    }
+                }
+            }
+        }
+        float y[2][4];
+        bool used[2][4];                       // whether any row sees the key: what an unseen one holds stays out
+        float top = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            v4f acc{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int u = 0; u < KS; ++u) {
+                if constexpr (BF) {
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, kf[t][u]),
+                                                                  __builtin_bit_cast(v8bf, qf[u]), acc, 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[t][u][e]), __uint_as_float(qf[u][e]),
+                                                                   acc, 0, 0, 0);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int j = j0 + 16 * t + 4 * g + r;
+                const AttKey key = att_key(a, s, j, page_v[t] >= 0 && j < c1);
+                const bool seen = att_sees(me, s.prefix, a.window, j, key.p, key.doc);
+                float v = att_score(a, acc[r]);
+                if (a.slopes) v -= slope * fabsf((float)(me.p - key.p));
+                y[t][r] = seen ? v : -INFINITY;
+                used[t][r] = ((__ballot(seen) >> (16 * g)) & 0xffffull) != 0;
+                top = fmaxf(top, y[t][r]);
+            }
+            if (scores && row < rows) {
+                const int j = j0 + 16 * t + 4 * g;
+                if (j < c1) {
+                    float* dst = scores + ((int64_t)(b * a.hkv + h) * sp.rows + row) * sp.pitch + j;
+                    *(float4*)dst = make_float4(y[t][0], y[t][1], y[t][2], y[t][3]);
+                }
+            }
+        }
+        top = xor32(xor16(top, true), true);
+        if (__any(top > m)) {
+            const float now = fmaxf(m, top);
+            const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
+            l *= f;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) o[t] *= f;
+            m = now;
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+        float w[2][4];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                w[t][r] = __builtin_amdgcn_exp2f(y[t][r] - base);
+                l += w[t][r];
+            }
+        if constexpr (BF) {
+            const v4u pf = {att_pack_bf16(w[0][0], w[0][1]), att_pack_bf16(w[0][2], w[0][3]),
+                            att_pack_bf16(w[1][0], w[1][1]), att_pack_bf16(w[1][2], w[1][3])};
+            uint32_t keep[4];                  // halves of the operand that hold a key in use
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+                    keep[2 * t + r] = (used[t][2 * r] ? 0xffffu : 0u) | (used[t][2 * r + 1] ? 0xffff0000u : 0u);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int c = 0; c < CW; ++c) {
+                    const uint32_t sel = c & 1 ? 0x07060302u : 0x05040100u;
+                    v4u x;
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r)
+                            x[2 * t + r] = __builtin_amdgcn_perm(vf[t][2 * r + 1][u][c / 2], vf[t][2 * r][u][c / 2], sel) &
+                                           keep[2 * t + r];
+                    o[u * CW + c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        __builtin_bit_cast(v8bf, x), __builtin_bit_cast(v8bf, pf), o[u * CW + c], 0, 0, 0);
+                }
+        } else {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+#pragma unroll
+                        for (int c = 0; c < CW; ++c) {
+                            const float x = used[t][r] ? __uint_as_float(vf[t][r][u][c]) : 0.f;
+                            o[u * CW + c] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, w[t][r], o[u * CW + c], 0, 0, 0);
+                        }
+        }
+    }
+    // ---- the four wavefronts' parts, in their order
+    l = xor32(xor16(l, false), false);
+    if (g == 0) {
+        s_m[wave][li] = m;
+        s_l[wave][li] = l;
+    }
+    __syncthreads();
+    float mm = -INFINITY, ll = 0.f;
+#pragma unroll
+    for (int w = 0; w < SP_WAVES; ++w) mm = fmaxf(mm, s_m[w][li]);
+#pragma unroll
+    for (int w = 0; w < SP_WAVES; ++w)
+        if (s_m[w][li] != -INFINITY) ll += s_l[w][li] * __builtin_amdgcn_exp2f(s_m[w][li] - mm);
+    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mm);
+    // lane (row li, g) holds columns 128 u + 4 CW g + CW r + c
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int c = 0; c < CW; c += 4)
+                *(float4*)&s_o[wave][li][u * 16 * CW + 4 * CW * g + CW * r + c] =
+                    make_float4(o[u * CW + c][r] * f, o[u * CW + c + 1][r] * f, o[u * CW + c + 2][r] * f, o[u * CW + c + 3][r] * f);
+    if (wave == 0 && g == 0) {
+        if (sp.splits > 1) stat[(unit * sp.splits + split) * 16 + li] = make_float2(mm, ll);
+        s_mm[li] = mm;
+        s_ll[li] = ll;
+    }
+    __syncthreads();
+    constexpr int PER = 16 * DP / 4 / (64 * SP_WAVES);
+#pragma unroll
+    for (int it = 0; it < PER; ++it) {
+        const int idx = it * 64 * SP_WAVES + threadIdx.x, r = idx / (DP / 4), c = idx % (DP / 4) * 4;
+        float4 v = *(const float4*)&s_o[0][r][c];
+#pragma unroll
+        for (int w = 1; w < SP_WAVES; ++w) {
+            const float4 x = *(const float4*)&s_o[w][r][c];
+            v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+        }
+        if (sp.splits > 1) {
+            *(float4*)(part + ((unit * sp.splits + split) * 16 + r) * DP + c) = v;
+        } else if (rt * 16 + r < rows && c < a.d) {
+            const float total = s_ll[r], inv = total > 0.f ? 1.f / total : 0.f;
+            const int t = (rt * 16 + r) / a.group, hd = h * a.group + rt * 16 + r - t * a.group;
+            const int64_t at = ((int64_t)(s.row0 + t) * a.hq + hd) * a.d + c;
+            if constexpr (BF) *(uint2*)(a.out + at * 2) = make_uint2(att_pack_bf16(v.x * inv, v.y * inv), att_pack_bf16(v.z * inv, v.w * inv));
+            else *(float4*)(a.out + at * 4) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+            if (c == 0 && a.lse) a.lse[(int64_t)(s.row0 + t) * a.hq + hd] = total > 0.f ? (s_mm[r] + __log2f(total)) * ATT_LN2 : -INFINITY;
+        }
+    }
+}
+
+// One row's parts added up: 8 (4 at 256 columns) groups of threads take every eighth split, four columns a thread.
+template <bool BF, int DP>
+__global__ __launch_bounds__(256) void att_join_kernel(AttArgs a, AttSplit sp, const float* __restrict__ part,
+                                                       const float2* __restrict__ stat) {
+    constexpr int LANES = DP / 4, GROUPS = 256 / LANES;
+    __shared__ float red[8];
+    __shared__ __align__(16) float s_o[GROUPS][DP];
+    const int h = blockIdx.y, b = blockIdx.z, row = blockIdx.x;
+    const AttSeq s = att_seq(a, b);
+    if (row >= s.fresh * a.group) return;
+    const int rt = row >> 4, r = row & 15;
+    const int64_t unit = ((int64_t)b * a.hkv + h) * sp.row_tiles + rt;
+    const int used = (s.n + sp.chunk - 1) / sp.chunk;
+    const float2* st = stat + unit * sp.splits * 16 + r;
+    float m = -INFINITY;
+    for (int i = threadIdx.x; i < used; i += 256) m = fmaxf(m, st[i * 16].x);
+    m = bwla_wave_max(m);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    const int grp = threadIdx.x / LANES, c = threadIdx.x % LANES * 4;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    float l = 0.f;
+    for (int i = grp; i < used; i += GROUPS) {
+        const float2 x = st[i * 16];
+        if (x.x == -INFINITY) continue;
+        const float f = __builtin_amdgcn_exp2f(x.x - m);
+        l += x.y * f;
+        const float4 p = *(const float4*)(part + ((unit * sp.splits + i) * 16 + r) * DP + c);
+        v.x += p.x * f; v.y += p.y * f; v.z += p.z * f; v.w += p.w * f;
+    }
+    __shared__ float s_l[GROUPS];
+    if (c == 0) s_l[grp] = l;
+    *(float4*)&s_o[grp][c] = v;
+    __syncthreads();
+    if (grp != 0 || c >= a.d) return;
+    l = 0.f;
+    v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+        l += s_l[i];
+        const float4 p = *(const float4*)&s_o[i][c];
+        v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
+    }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const int t = row / a.group, hd = h * a.group + row - t * a.group;
+    const int64_t at = ((int64_t)(s.row0 + t) * a.hq + hd) * a.d + c;
+    if constexpr (BF) *(uint2*)(a.out + at * 2) = make_uint2(att_pack_bf16(v.x * inv, v.y * inv), att_pack_bf16(v.z * inv, v.w * inv));
+    else *(float4*)(a.out + at * 4) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+    if (c == 0 && a.lse) a.lse[(int64_t)(s.row0 + t) * a.hq + hd] = l > 0.f ? (m + __log2f(l)) * ATT_LN2 : -INFINITY;
+}
+
+// The rows' weights of each cached token, from the scores that the first launch left, added to the token's sum.
+__global__ __launch_bounds__(256) void att_sum_kernel(AttArgs a, AttSplit sp, const float* __restrict__ scores) {
+    const int j = blockIdx.x * 256 + threadIdx.x, h = blockIdx.y, b = blockIdx.z;
+    const AttSeq s = att_seq(a, b);
+    if (j >= s.n) return;
+    const int p = s.table[j >> a.page_shift];
+    if ((unsigned)p >= (unsigned)a.pages) return;
+    const float* src = scores + (int64_t)(b * a.hkv + h) * sp.rows * sp.pitch + j;
+    const int rows = s.fresh * a.group;
+    float sum = 0.f;
+    for (int r = 0; r < rows; ++r) {
+        const int t = r / a.group;
+        const float lse = a.lse[(int64_t)(s.row0 + t) * a.hq + h * a.group + r - t * a.group];
+        const float y = src[(int64_t)r * sp.pitch];
+        sum += y == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(y - lse * ATT_LOG2E);
+    }
+    float* w = a.weights + (((int64_t)p * a.hkv + h) << a.page_shift) + (j & ((1 << a.page_shift) - 1));
+    *w += sum;
+}
+
+template <bool BF, int DP>
+hipError_t launch(const AttArgs& a, const AttSplit& s, void* ws, hipStream_t st) {
+    float* part = (float*)ws;
+    float2* stat = (float2*)((char*)ws + s.part_bytes);
+    float* scores = a.weights ? (float*)((char*)ws + s.part_bytes + s.stat_bytes) : nullptr;
+    const dim3 grid(s.splits, a.hkv * s.row_tiles, a.seqs);
+    if (a.d == DP) att_split_kernel<BF, DP, true><<<grid, 64 * SP_WAVES, 0, st>>>(a, s, part, stat, scores);
+    else att_split_kernel<BF, DP, false><<<grid, 64 * SP_WAVES, 0, st>>>(a, s, part, stat, scores);
+    if (s.splits > 1) att_join_kernel<BF, DP><<<dim3(s.rows, a.hkv, a.seqs), 256, 0, st>>>(a, s, part, stat);
+    if (scores && a.max_len > 0) att_sum_kernel<<<dim3((a.max_len + 255) / 256, a.hkv, a.seqs), 256, 0, st>>>(a, s, scores);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+bool bwla_att_is_split(const AttArgs& a) { return (int64_t)a.max_new * a.group <= 64; }
+
+AttSplit bwla_att_split(const AttArgs& a, bool weights) {
+    AttSplit s;
+    s.rows = a.max_new * a.group;
+    s.row_tiles = (s.rows + 15) / 16;
+    const int64_t units = (int64_t)a.seqs * a.hkv * s.row_tiles;
+    const int64_t step = SP_WAVES * SP_STEP;
+    int64_t chunk = (units * a.max_len + 1023) / 1024;
+    chunk = (chunk + step - 1) / step * step;
+    s.chunk = (int)(chunk < 2 * step ? 2 * step : chunk > SP_MAX_CHUNK ? SP_MAX_CHUNK : chunk);
+    s.splits = a.max_len > 0 ? (a.max_len + s.chunk - 1) / s.chunk : 1;
+    s.pitch = (a.max_len + 31) & ~31;
+    const int dp = a.d <= 64 ? 64 : a.d <= 128 ? 128 : 256;
+    s.part_bytes = s.splits > 1 ? (size_t)units * s.splits * 16 * dp * 4 : 0;
+    s.stat_bytes = s.splits > 1 ? (size_t)bwla_align256((uint64_t)units * s.splits * 16 * 8) : 0;
+    s.score_bytes = weights ? (size_t)a.seqs * a.hkv * s.rows * s.pitch * 4 : 0;
+    return s;
+}
+
+hipError_t bwla_launch_attention_split(const AttArgs& a, const AttSplit& s, int dtype, void* ws, hipStream_t st) {
+    if (dtype == BWLA_X_BF16) {
+        if (a.d <= 64) return launch<true, 64>(a, s, ws, st);
+        if (a.d <= 128) return launch<true, 128>(a, s, ws, st);
+        return launch<true, 256>(a, s, ws, st);
+    }
+    if (a.d <= 64) return launch<false, 64>(a, s, ws, st);
+    if (a.d <= 128) return launch<false, 128>(a, s, ws, st);
+    return launch<false, 256>(a, s, ws, st);
+}
