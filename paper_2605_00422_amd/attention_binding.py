@@ -239,6 +239,8 @@ def cache_evict(cache: KVCache, batch: Batch, table_out, weights, keep: int, sin
             raise TypeError(f"{what} must be (sequences, keep), dense")
     if _ints(position, "position", 2) is not None and position.shape[0] != n:
         raise ValueError("position: one row for each sequence")
+    if keep == 0:                                      # (an empty tensor has no address)
+        position = position_out = None
     row = lambda t: 0 if t is None else t.stride(0) if n > 1 else t.shape[1]  # noqa: E731
     _ck(load().bwla_cache_evict(cache._ref, batch._ref, _p(table_out), row(table_out), _p(cache._of(weights, "weights")), keep, sinks, recent,
                                 _p(length_out), _p(kept), _p(position), row(position), _p(position_out), _p(ws), _bytes(ws), _s()),

@@ -132,9 +132,14 @@ __device__ __forceinline__ AttKey att_key(const AttArgs& a, const AttSeq& s, int
     k.doc = ok ? (s.doc ? max(s.doc[j], -1) : 0) : -1;
     return k;
 }
+// (rows that see nothing have document -2, keys that nothing sees -1; no short cuts: branches would cost more)
 __device__ __forceinline__ bool att_sees(const AttRow& r, int prefix, int window, int j, int kp, int kdoc) {
-    return r.doc == kdoc && r.i >= 0 && (j < prefix || (j <= r.i && r.p - kp < window));
+    return (r.doc == kdoc) & ((j < prefix) | ((j <= r.i) & (r.p - kp < window)));
 }
+// MFMA takes no notice of the execution mask: whatever a branch around one depends on is made a scalar, so that
+// the branch is a jump
+__device__ __forceinline__ bool att_uniform(bool x) { return __builtin_amdgcn_readfirstlane((int)x) != 0; }
+__device__ __forceinline__ int att_wave() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
 
 // tanh to one or two units of the last place: below 0.6 an odd polynomial (degree 11, fitted to tanh(x) / x in
 // x^2, relative error 2.5e-9 before rounding), above by the exponential
@@ -160,5 +165,11 @@ __device__ __forceinline__ uint32_t att_pack_bf16(float lo, float hi) {
     r[0] = (__bf16)lo;
     r[1] = (__bf16)hi;
     return __builtin_bit_cast(uint32_t, r);
+}
+// c plus both bf16 halves of x.  Outputs are divided by the sum of the weights as they enter the second product,
+// rounded to bf16, so that a row of one key is that key's value, and of equal values that value; lse is of the fp32 sum.
+__device__ __forceinline__ float att_add_bf16(uint32_t x, float c) {
+    typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf, x), __builtin_bit_cast(v2bf, 0x3f803f80u), c, false);
 }
 #endif

@@ -35,7 +35,7 @@ __device__ __forceinline__ float xor32(float v, bool max_of) {
 // BF: bf16 (else fp32); DP: columns, 64, 128 or 256; EXACT: d == DP (else columns from d on count as zero)
 template <bool BF, int DP, bool EXACT>
 __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, AttSplit sp, float* __restrict__ part,
-                                                                 float2* __restrict__ stat, float* __restrict__ scores) {
+                                                                 float4* __restrict__ stat, float* __restrict__ scores) {
     constexpr int ES = BF ? 2 : 4;
     constexpr int KS = DP * ES / 64;           // 64-byte steps along a row of K
     constexpr int CW = DP >= 128 ? 8 : DP / 16;  // columns of a lane side by side
@@ -44,10 +44,10 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
     constexpr int VB = CW * ES;                // bytes of those columns
     constexpr int VD = VB / 4;                 // ... in dwords
     __shared__ int tab[SP_MAX_CHUNK + 8];
-    __shared__ float s_m[SP_WAVES][16], s_l[SP_WAVES][16], s_mm[16], s_ll[16];
+    __shared__ float s_m[SP_WAVES][16], s_l[SP_WAVES][16], s_lr[SP_WAVES][16], s_mm[16], s_ll[16], s_llr[16];
     __shared__ __align__(16) float s_o[SP_WAVES][16][DP + 4];
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = att_wave(), li = lane & 15, g = lane >> 4;
     const int split = blockIdx.x, h = blockIdx.y / sp.row_tiles, rt = blockIdx.y - h * sp.row_tiles, b = blockIdx.z;
     const AttSeq s = att_seq(a, b);
     const int rows = s.fresh * a.group, row = rt * 16 + li;
@@ -59,7 +59,7 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
     const int skip_to = (s.pos || a.window == INT32_MAX) ? 0 : i_first - a.window + 1;
     const bool none = c0 >= c1 || (c1 <= skip_to && c0 >= s.prefix);
     if (none && sp.splits > 1) {
-        if (threadIdx.x < 16) stat[(unit * sp.splits + split) * 16 + threadIdx.x] = make_float2(-INFINITY, 0.f);
+        if (threadIdx.x < 16) stat[(unit * sp.splits + split) * 16 + threadIdx.x] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
         if (scores) {                          // (what the sums of weights read of it)
             for (int r = 0; r < 16 && rt * 16 + r < rows; ++r)
                 for (int j = c0 + threadIdx.x; j < c1; j += 64 * SP_WAVES)
@@ -92,7 +92,7 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
     v4f o[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) o[t] = v4f{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f;
+    float m = -INFINITY, l = 0.f, lr = 0.f;    // l: sum of the weights, lr: as the second product takes them
     const char* kh = a.k + (int64_t)h * a.head_bytes;
     const char* vh = a.v + (int64_t)h * a.head_bytes;
     const int slot_mask = (1 << a.page_shift) - 1;
@@ -181,6 +181,7 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
             const float now = fmaxf(m, top);
             const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
             l *= f;
+            lr *= f;
 #pragma unroll
             for (int t = 0; t < NT; ++t) o[t] *= f;
             m = now;
@@ -197,6 +198,8 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
         if constexpr (BF) {
             const v4u pf = {att_pack_bf16(w[0][0], w[0][1]), att_pack_bf16(w[0][2], w[0][3]),
                             att_pack_bf16(w[1][0], w[1][1]), att_pack_bf16(w[1][2], w[1][3])};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) lr = att_add_bf16(pf[e], lr);
             uint32_t keep[4];                  // halves of the operand that hold a key in use
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -234,17 +237,23 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
     }
     // ---- the four wavefronts' parts, in their order
     l = xor32(xor16(l, false), false);
+    lr = BF ? xor32(xor16(lr, false), false) : l;
     if (g == 0) {
         s_m[wave][li] = m;
         s_l[wave][li] = l;
+        s_lr[wave][li] = lr;
     }
     __syncthreads();
-    float mm = -INFINITY, ll = 0.f;
+    float mm = -INFINITY, ll = 0.f, llr = 0.f;
 #pragma unroll
     for (int w = 0; w < SP_WAVES; ++w) mm = fmaxf(mm, s_m[w][li]);
 #pragma unroll
     for (int w = 0; w < SP_WAVES; ++w)
-        if (s_m[w][li] != -INFINITY) ll += s_l[w][li] * __builtin_amdgcn_exp2f(s_m[w][li] - mm);
+        if (s_m[w][li] != -INFINITY) {
+            const float e = __builtin_amdgcn_exp2f(s_m[w][li] - mm);
+            ll += s_l[w][li] * e;
+            llr += s_lr[w][li] * e;
+        }
     const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mm);
     // lane (row li, g) holds columns 128 u + 4 CW g + CW r + c
 #pragma unroll
@@ -256,9 +265,10 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
                 *(float4*)&s_o[wave][li][u * 16 * CW + 4 * CW * g + CW * r + c] =
                     make_float4(o[u * CW + c][r] * f, o[u * CW + c + 1][r] * f, o[u * CW + c + 2][r] * f, o[u * CW + c + 3][r] * f);
     if (wave == 0 && g == 0) {
-        if (sp.splits > 1) stat[(unit * sp.splits + split) * 16 + li] = make_float2(mm, ll);
+        if (sp.splits > 1) stat[(unit * sp.splits + split) * 16 + li] = make_float4(mm, ll, llr, 0.f);
         s_mm[li] = mm;
         s_ll[li] = ll;
+        s_llr[li] = llr;
     }
     __syncthreads();
     constexpr int PER = 16 * DP / 4 / (64 * SP_WAVES);
@@ -274,7 +284,7 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
         if (sp.splits > 1) {
             *(float4*)(part + ((unit * sp.splits + split) * 16 + r) * DP + c) = v;
         } else if (rt * 16 + r < rows && c < a.d) {
-            const float total = s_ll[r], inv = total > 0.f ? 1.f / total : 0.f;
+            const float total = s_ll[r], inv = total > 0.f ? 1.f / s_llr[r] : 0.f;
             const int t = (rt * 16 + r) / a.group, hd = h * a.group + rt * 16 + r - t * a.group;
             const int64_t at = ((int64_t)(s.row0 + t) * a.hq + hd) * a.d + c;
             if constexpr (BF) *(uint2*)(a.out + at * 2) = make_uint2(att_pack_bf16(v.x * inv, v.y * inv), att_pack_bf16(v.z * inv, v.w * inv));
@@ -287,9 +297,10 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
 // One row's parts added up: 8 (4 at 256 columns) groups of threads take every eighth split, four columns a thread.
 template <bool BF, int DP>
 __global__ __launch_bounds__(256) void att_join_kernel(AttArgs a, AttSplit sp, const float* __restrict__ part,
-                                                       const float2* __restrict__ stat) {
+                                                       const float4* __restrict__ stat) {
     constexpr int LANES = DP / 4, GROUPS = 256 / LANES;
     __shared__ float red[8];
+    __shared__ float s_l[GROUPS], s_lr[GROUPS];
     __shared__ __align__(16) float s_o[GROUPS][DP];
     const int h = blockIdx.y, b = blockIdx.z, row = blockIdx.x;
     const AttSeq s = att_seq(a, b);
@@ -297,7 +308,7 @@ __global__ __launch_bounds__(256) void att_join_kernel(AttArgs a, AttSplit sp, c
     const int rt = row >> 4, r = row & 15;
     const int64_t unit = ((int64_t)b * a.hkv + h) * sp.row_tiles + rt;
     const int used = (s.n + sp.chunk - 1) / sp.chunk;
-    const float2* st = stat + unit * sp.splits * 16 + r;
+    const float4* st = stat + unit * sp.splits * 16 + r;
     float m = -INFINITY;
     for (int i = threadIdx.x; i < used; i += 256) m = fmaxf(m, st[i * 16].x);
     m = bwla_wave_max(m);
@@ -306,29 +317,33 @@ __global__ __launch_bounds__(256) void att_join_kernel(AttArgs a, AttSplit sp, c
     m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
     const int grp = threadIdx.x / LANES, c = threadIdx.x % LANES * 4;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    float l = 0.f;
+    float l = 0.f, lr = 0.f;
     for (int i = grp; i < used; i += GROUPS) {
-        const float2 x = st[i * 16];
+        const float4 x = st[i * 16];
         if (x.x == -INFINITY) continue;
         const float f = __builtin_amdgcn_exp2f(x.x - m);
         l += x.y * f;
+        lr += x.z * f;
         const float4 p = *(const float4*)(part + ((unit * sp.splits + i) * 16 + r) * DP + c);
         v.x += p.x * f; v.y += p.y * f; v.z += p.z * f; v.w += p.w * f;
     }
-    __shared__ float s_l[GROUPS];
-    if (c == 0) s_l[grp] = l;
+    if (c == 0) {
+        s_l[grp] = l;
+        s_lr[grp] = lr;
+    }
     *(float4*)&s_o[grp][c] = v;
     __syncthreads();
     if (grp != 0 || c >= a.d) return;
-    l = 0.f;
+    l = lr = 0.f;
     v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) {
         l += s_l[i];
+        lr += s_lr[i];
         const float4 p = *(const float4*)&s_o[i][c];
         v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
     }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float inv = l > 0.f ? 1.f / lr : 0.f;
     const int t = row / a.group, hd = h * a.group + row - t * a.group;
     const int64_t at = ((int64_t)(s.row0 + t) * a.hq + hd) * a.d + c;
     if constexpr (BF) *(uint2*)(a.out + at * 2) = make_uint2(att_pack_bf16(v.x * inv, v.y * inv), att_pack_bf16(v.z * inv, v.w * inv));
@@ -359,7 +374,7 @@ __global__ __launch_bounds__(256) void att_sum_kernel(AttArgs a, AttSplit sp, co
 template <bool BF, int DP>
 hipError_t launch(const AttArgs& a, const AttSplit& s, void* ws, hipStream_t st) {
     float* part = (float*)ws;
-    float2* stat = (float2*)((char*)ws + s.part_bytes);
+    float4* stat = (float4*)((char*)ws + s.part_bytes);
     float* scores = a.weights ? (float*)((char*)ws + s.part_bytes + s.stat_bytes) : nullptr;
     const dim3 grid(s.splits, a.hkv * s.row_tiles, a.seqs);
     if (a.d == DP) att_split_kernel<BF, DP, true><<<grid, 64 * SP_WAVES, 0, st>>>(a, s, part, stat, scores);
@@ -386,7 +401,7 @@ AttSplit bwla_att_split(const AttArgs& a, bool weights) {
     s.pitch = (a.max_len + 31) & ~31;
     const int dp = a.d <= 64 ? 64 : a.d <= 128 ? 128 : 256;
     s.part_bytes = s.splits > 1 ? (size_t)units * s.splits * 16 * dp * 4 : 0;
-    s.stat_bytes = s.splits > 1 ? (size_t)bwla_align256((uint64_t)units * s.splits * 16 * 8) : 0;
+    s.stat_bytes = s.splits > 1 ? (size_t)bwla_align256((uint64_t)units * s.splits * 16 * 16) : 0;
     s.score_bytes = weights ? (size_t)a.seqs * a.hkv * s.rows * s.pitch * 4 : 0;
     return s;
 }

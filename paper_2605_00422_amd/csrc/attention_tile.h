@@ -66,7 +66,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
     const int rows = s.fresh * a.group;
     if (tile * AT_ROWS >= rows) return;
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, hf = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = att_wave(), l32 = lane & 31, hf = lane >> 5;
     const int row = tile * AT_ROWS + wave * 32 + l32;
     const bool live = row < rows;
     const int tok = live ? row / a.group : 0, head = h * a.group + (live ? row - tok * a.group : 0);
@@ -161,7 +161,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
     for (int t = 0; t < DT; ++t)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
-    float m = -INFINITY, l = 0.f;
+    float m = -INFINITY, l = 0.f, lr = 0.f;            // l: sum of the weights, lr: as the second product takes them
 
     if (blocks > 0) {
         find_pages(0);
@@ -184,6 +184,11 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
         }
     }
 
+    // Weights enter the second product rounded to bf16, whose errors (2^-9 of a weight in the mean) average out over
+    // many keys.  Where a row has seen fewer than FEW, both terms of the weights go in (16 bits): the first tokens of
+    // a prompt or a document, at no cost to the others.
+    constexpr int FEW = 64;
+    int had = 0;                                       // keys that the lane's half of the row has seen
     for (int t = 0; t < blocks; ++t) {
         const int buf = t & 1, j0 = first_of(t);
         __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0): this wavefront's copies of the block are there
@@ -194,7 +199,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
             if (t + 2 < blocks) find_pages(t + 2);
         }
         const int* const inf = info + buf * INFO;
-        const bool skip = j0 > w_last && j0 >= s.prefix;
+        const bool skip = j0 > w_last && j0 >= s.prefix;    // (scalars)
         if (!skip) {
             // ---- S^T
             v16f p[KT];
@@ -258,22 +263,33 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
                 }
             }
             // ---- mask: blocks that every row sees whole have none
-            const bool whole = !inf[2 * BK] && !s.doc && w_first >= 0 &&
-                               (j0 + BK <= s.prefix || (j0 + BK - 1 <= w_first && (a.window == INT32_MAX || (!s.pos && j0 > w_last - a.window))));
+            const bool whole = att_uniform(!inf[2 * BK] && !s.doc && w_first >= 0 &&
+                                           (j0 + BK <= s.prefix || (j0 + BK - 1 <= w_first &&
+                                                                    (a.window == INT32_MAX || (!s.pos && j0 > w_last - a.window)))));
             uint32_t used[KT];                         // bit r: some row of the wavefront sees the lane's key r
-            if (!whole) {
+            bool fine = false;                         // weights as two bf16 terms: see below
+            if (whole) {
+                had += BK;
+            } else {
 #pragma unroll
                 for (int k = 0; k < KT; ++k) {
-                    used[k] = 0;
+                    uint32_t mine = 0;                 // bit r: the row sees the lane's key r
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int key = k * 32 + (r & 3) + 8 * (r >> 2) + 4 * hf;
-                        const bool seen = att_sees(me, s.prefix, a.window, j0 + key, inf[key], inf[BK + key]);
-                        p[k][r] = seen ? p[k][r] : -INFINITY;
-                        const uint64_t any = __ballot(seen);
-                        used[k] |= ((hf ? (uint32_t)(any >> 32) : (uint32_t)any) != 0 ? 1u : 0u) << r;
+                    for (int g = 0; g < 4; ++g) {
+                        const v4i kp = *(const v4i*)(inf + k * 32 + 8 * g + 4 * hf), kd = *(const v4i*)(inf + BK + k * 32 + 8 * g + 4 * hf);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const bool seen = att_sees(me, s.prefix, a.window, j0 + k * 32 + 8 * g + 4 * hf + e, kp[e], kd[e]);
+                            p[k][4 * g + e] = seen ? p[k][4 * g + e] : -INFINITY;
+                            mine |= seen ? 1u << (4 * g + e) : 0u;
+                        }
                     }
+                    had += __popc(mine);
+#pragma unroll
+                    for (int o = 1; o < 32; o <<= 1) mine |= __shfl_xor(mine, o, 64);
+                    used[k] = mine;
                 }
+                fine = BF && att_uniform(__any(live & (had < FEW)));
             }
             // ---- running maximum and sum
             float top = -INFINITY;
@@ -287,6 +303,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
                 const float now = fmaxf(m, top);
                 const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
                 l *= f;
+                if constexpr (BF) lr *= f;
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -309,9 +326,19 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
                     if constexpr (BF) {
 #pragma unroll
                         for (int u = 0; u < 2; ++u) {
-                            v4u pf;
+                            v4u pf, pl;
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) pf[e] = att_pack_bf16(p[k][8 * u + 2 * e], p[k][8 * u + 2 * e + 1]);
+                            for (int e = 0; e < 4; ++e) {
+                                const float w0 = p[k][8 * u + 2 * e], w1 = p[k][8 * u + 2 * e + 1];
+                                pf[e] = att_pack_bf16(w0, w1);
+                                lr = att_add_bf16(pf[e], lr);
+                                if constexpr (decltype(masked)::value) {
+                                    if (fine) {
+                                        pl[e] = att_pack_bf16(w0 - bwla_bf16_to_f32((uint16_t)pf[e]), w1 - bwla_bf16_to_f32((uint16_t)(pf[e] >> 16)));
+                                        lr = att_add_bf16(pl[e], lr);
+                                    }
+                                }
+                            }
 #pragma unroll
                             for (int d = 0; d < DT; ++d) {
                                 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
@@ -330,6 +357,10 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
                                 }
                                 o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, x),
                                                                                __builtin_bit_cast(v8bf, pf), o[d], 0, 0, 0);
+                                if constexpr (decltype(masked)::value) {
+                                    if (fine) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, x),
+                                                                                             __builtin_bit_cast(v8bf, pl), o[d], 0, 0, 0);
+                                }
                             }
                         }
                     } else {
@@ -351,8 +382,9 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
     }
 
     l = half_sum(l);
+    lr = BF ? half_sum(lr) : l;
     if (!live) return;
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float inv = lr > 0.f ? 1.f / lr : 0.f;
     const int64_t at = ((int64_t)(s.row0 + tok) * a.hq + head);
     char* const dst = a.out + at * a.d * ES;
 #pragma unroll

@@ -21,7 +21,7 @@ struct WtShape {
 template <bool BF, int DP, bool EXACT>
 __global__ __launch_bounds__(64 * WT_WAVES) void att_weights_kernel(AttArgs a, int parts, int64_t pitch, float* __restrict__ sums) {
     constexpr int ES = BF ? 2 : 4, CH = DP * ES / 16, KT = WtShape<BF, DP>::KT;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, hf = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = att_wave(), l32 = lane & 31, hf = lane >> 5;
     const int h = blockIdx.y, b = blockIdx.z / parts, part = blockIdx.z - b * parts;
     const AttSeq s = att_seq(a, b);
     const int j0 = (blockIdx.x * WT_WAVES + wave) * 32 * KT;

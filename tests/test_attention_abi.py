@@ -1,0 +1,189 @@
+"""Refusals of the cache, attention, rotation and eviction calls: checked on the host, nothing is enqueued (no GPU)."""
+import ctypes
+import os
+from ctypes import byref, c_size_t, c_void_p
+
+import pytest
+
+from paper_2605_00422_amd import attention_binding as A
+from paper_2605_00422_amd import binding as B
+
+P = c_void_p(1 << 20)                                  # never followed: every call here is refused, or has nothing to do
+OFF = c_void_p((1 << 20) + 8)
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(B.LIB_PATH):
+        from paper_2605_00422_amd.build import build_library
+        build_library()
+    return A.load()
+
+
+def cache(**kw):
+    d = dict(d_k=P, d_v=P, page_stride=8 * 16 * 128, head_stride=16 * 128, slot_stride=128, pages=10, page_size=16, kv_heads=8,
+             head_dim=128, dtype=B.BWLA_X_BF16)
+    return A._Cache(**{**d, **kw})
+
+
+def batch(**kw):
+    d = dict(d_table=P, d_len=P, d_first=P, tokens=5, sequences=2, table_stride=4, max_new=3, max_len=60)
+    return A._Batch(**{**d, **kw})
+
+
+def score(**kw):
+    return A._Score(**{**dict(scale=0.1), **kw})
+
+
+SHAPES = [  # what every call refuses of a cache and a batch
+    (dict(pages=0), {}, B.BWLA_ERR_SHAPE), (dict(page_size=0), {}, B.BWLA_ERR_SHAPE), (dict(kv_heads=0), {}, B.BWLA_ERR_SHAPE),
+    (dict(head_dim=0), {}, B.BWLA_ERR_SHAPE), (dict(head_dim=12), {}, B.BWLA_ERR_UNSUPPORTED), (dict(head_dim=264, slot_stride=264), {}, B.BWLA_ERR_UNSUPPORTED),
+    (dict(page_size=24), {}, B.BWLA_ERR_UNSUPPORTED), (dict(page_size=4), {}, B.BWLA_ERR_UNSUPPORTED), (dict(dtype=7), {}, B.BWLA_ERR_UNSUPPORTED),
+    ({}, dict(sequences=-1), B.BWLA_ERR_SHAPE), ({}, dict(tokens=-1), B.BWLA_ERR_SHAPE), ({}, dict(max_len=65), B.BWLA_ERR_SHAPE),
+    ({}, dict(max_len=-1), B.BWLA_ERR_SHAPE), ({}, dict(max_new=-1), B.BWLA_ERR_SHAPE),
+    ({}, dict(max_len=(1 << 24) + 1, table_stride=1 << 24), B.BWLA_ERR_UNSUPPORTED), ({}, dict(sequences=70000), B.BWLA_ERR_UNSUPPORTED),
+]
+CACHES = [  # ... of the pointers and strides
+    (dict(d_k=None), {}, B.BWLA_ERR_NULL), (dict(d_v=None), {}, B.BWLA_ERR_NULL), (dict(d_k=OFF), {}, B.BWLA_ERR_ALIGN),
+    (dict(page_stride=-16), {}, B.BWLA_ERR_SHAPE), (dict(slot_stride=64), {}, B.BWLA_ERR_SHAPE), (dict(slot_stride=132), {}, B.BWLA_ERR_ALIGN),
+    (dict(head_stride=2044), {}, B.BWLA_ERR_ALIGN), (dict(page_stride=16388), {}, B.BWLA_ERR_ALIGN),
+    ({}, dict(d_len=None), B.BWLA_ERR_NULL), ({}, dict(d_table=None), B.BWLA_ERR_NULL),
+]
+
+
+def forward(lib, c=None, b=None, s=None, q=P, stride=16 * 128, hq=16, out=P, lse=P, weights=None, ws=P, ws_bytes=1 << 40):
+    ref = lambda x: None if x is False else byref(x)  # noqa: E731
+    return lib.bwla_attention_forward(ref(cache() if c is None else c), ref(batch() if b is None else b), ref(score() if s is None else s),
+                                      q, stride, hq, out, lse, weights, ws, ws_bytes, None)
+
+
+def evict(lib, c=None, b=None, table=P, stride=4, weights=P, keep=20, sinks=2, recent=3, length=P, kept=P, pos=None, pos_stride=0,
+          pos_out=None, ws=P, ws_bytes=1 << 40):
+    return lib.bwla_cache_evict(byref(c or cache()), byref(b or batch()), table, stride, weights, keep, sinks, recent, length, kept, pos,
+                                pos_stride, pos_out, ws, ws_bytes, None)
+
+
+def append(lib, c=None, b=None, position=P, qkv=P, xd=0, stride=32 * 128, hq=16, q=P, weights=None, cpos=None, cstride=0, **kw):
+    d = dict(d_cos=P, d_sin=P, rows=100, pairs=64, axes=1, interleaved=0, sections=(ctypes.c_int32 * 4)(64, 0, 0, 0))
+    return lib.bwla_rope_append(byref(c or cache()), byref(b or batch()), byref(A._Rope(**{**d, **kw})), position, qkv, xd, stride, hq, q,
+                                weights, cpos, cstride, None)
+
+
+@pytest.mark.parametrize("c,b,status", SHAPES + CACHES)
+def test_what_every_call_refuses(lib, c, b, status):
+    c, b = cache(**c), batch(**b)
+    assert forward(lib, c, b) == status
+    assert append(lib, c, b) == status
+    assert evict(lib, c, b) == status
+    assert lib.bwla_attention_weights(byref(c), byref(b), byref(score()), P, 16 * 128, 16, P, P, P, 1 << 40, None) == status
+
+
+@pytest.mark.parametrize("c,b,status", SHAPES)
+def test_sizes_refuse_shapes(lib, c, b, status):
+    c, b, n = cache(**c), batch(**b), c_size_t()
+    assert lib.bwla_attention_workspace_size(byref(c), byref(b), 16, 0, byref(n)) == status
+    assert lib.bwla_attention_weights_workspace_size(byref(c), byref(b), 16, byref(n)) == status
+    assert lib.bwla_cache_evict_workspace_size(byref(c), byref(b), byref(n)) == status
+    assert lib.bwla_attention_workspace_size(byref(cache()), byref(batch()), 16, 0, None) == B.BWLA_ERR_NULL
+    assert lib.bwla_attention_workspace_size(None, byref(batch()), 16, 0, byref(n)) == B.BWLA_ERR_NULL
+    assert lib.bwla_cache_evict_workspace_size(None, byref(batch()), byref(n)) == B.BWLA_ERR_NULL
+
+
+def test_attention_refuses(lib):
+    R = B
+    assert forward(lib, s=False) == R.BWLA_ERR_NULL
+    for bad in (dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=0.1, cap=-1.0),
+                dict(scale=0.1, cap=float("nan")), dict(scale=0.1, window=-1), dict(scale=0.1, d_doc=P, index_stride=59),
+                dict(scale=0.1, d_position=P, index_stride=59)):
+        assert forward(lib, s=A._Score(**bad)) == R.BWLA_ERR_SHAPE, bad
+    assert forward(lib, hq=12, stride=12 * 128) == R.BWLA_ERR_SHAPE          # no multiple of the key-value heads
+    assert forward(lib, hq=2048, stride=2048 * 128) == R.BWLA_ERR_UNSUPPORTED
+    assert forward(lib, stride=16 * 128 - 8) == R.BWLA_ERR_SHAPE
+    assert forward(lib, stride=16 * 128 + 4) == R.BWLA_ERR_ALIGN
+    assert forward(lib, q=OFF) == R.BWLA_ERR_ALIGN and forward(lib, out=OFF) == R.BWLA_ERR_ALIGN
+    assert forward(lib, q=None) == R.BWLA_ERR_NULL and forward(lib, out=None) == R.BWLA_ERR_NULL
+    assert forward(lib, weights=P, lse=None) == R.BWLA_ERR_NULL
+    assert forward(lib, b=batch(d_first=None)) == R.BWLA_ERR_SHAPE            # five rows of two sequences
+    n = c_size_t()
+    long = dict(c=cache(pages=1000), b=batch(table_stride=600, max_len=9000))
+    assert lib.bwla_attention_workspace_size(byref(long["c"]), byref(long["b"]), 16, 1, byref(n)) == 0 and n.value > 0
+    assert forward(lib, **long, weights=P, ws_bytes=n.value - 1) == R.BWLA_ERR_BUFSIZE
+    assert forward(lib, **long, weights=P, ws=None) == R.BWLA_ERR_NULL
+    assert forward(lib, **long, weights=P, ws=OFF) == R.BWLA_ERR_ALIGN
+    w = lambda **k: lib.bwla_attention_weights(byref(cache()), byref(batch()), byref(score()), P, 16 * 128, 16, k.get("lse", P),  # noqa: E731
+                                               k.get("weights", P), P, 1 << 40, None)
+    assert w(lse=None) == R.BWLA_ERR_NULL and w(weights=None) == R.BWLA_ERR_NULL and w(weights=OFF) == R.BWLA_ERR_ALIGN
+
+
+def test_rotation_refuses(lib):
+    sec = lambda *v: (ctypes.c_int32 * 4)(*v)  # noqa: E731
+    assert append(lib, pairs=65, sections=sec(65)) == B.BWLA_ERR_SHAPE
+    assert append(lib, sections=sec(63)) == B.BWLA_ERR_SHAPE
+    assert append(lib, axes=2, sections=sec(65, -1)) == B.BWLA_ERR_SHAPE
+    assert append(lib, axes=0) == B.BWLA_ERR_SHAPE and append(lib, axes=5) == B.BWLA_ERR_SHAPE and append(lib, rows=0) == B.BWLA_ERR_SHAPE
+    assert append(lib, stride=32 * 128 - 4) == B.BWLA_ERR_SHAPE and append(lib, stride=32 * 128 + 2) == B.BWLA_ERR_ALIGN
+    assert append(lib, xd=5) == B.BWLA_ERR_UNSUPPORTED
+    assert append(lib, cpos=P, cstride=59) == B.BWLA_ERR_SHAPE
+    for k in ("qkv", "q", "position"):
+        assert append(lib, **{k: None}) == B.BWLA_ERR_NULL, k
+    assert append(lib, d_cos=None) == B.BWLA_ERR_NULL and append(lib, d_sin=OFF) == B.BWLA_ERR_ALIGN
+    assert append(lib, qkv=OFF) == B.BWLA_ERR_ALIGN and append(lib, weights=OFF) == B.BWLA_ERR_ALIGN
+
+
+def test_eviction_refuses(lib):
+    assert evict(lib, keep=-1) == B.BWLA_ERR_SHAPE and evict(lib, keep=4, sinks=2, recent=3) == B.BWLA_ERR_SHAPE
+    assert evict(lib, sinks=-1) == B.BWLA_ERR_SHAPE and evict(lib, keep=59, stride=3) == B.BWLA_ERR_SHAPE
+    assert evict(lib, pos=P, pos_stride=60) == B.BWLA_ERR_NULL and evict(lib, pos=P, pos_out=P, pos_stride=59) == B.BWLA_ERR_SHAPE
+    assert evict(lib, table=None) == B.BWLA_ERR_NULL and evict(lib, length=None) == B.BWLA_ERR_NULL and evict(lib, weights=None) == B.BWLA_ERR_NULL
+    assert evict(lib, weights=OFF) == B.BWLA_ERR_ALIGN
+    n = c_size_t()
+    assert lib.bwla_cache_evict_workspace_size(byref(cache()), byref(batch()), byref(n)) == 0
+    assert evict(lib, ws_bytes=n.value - 1) == B.BWLA_ERR_BUFSIZE and evict(lib, ws=None) == B.BWLA_ERR_NULL
+
+
+def test_nothing_to_do_is_no_error(lib):
+    none = batch(sequences=0, tokens=0, d_table=None, d_len=None, d_first=None)
+    assert forward(lib, b=none, q=None, out=None) == B.BWLA_OK
+    assert append(lib, b=none, qkv=None, q=None) == B.BWLA_OK and evict(lib, b=none) == B.BWLA_OK
+
+
+def test_binding_refuses_wrong_tensors():
+    import torch
+    k = torch.zeros(4, 2, 16, 64)
+    with pytest.raises(TypeError):
+        A.KVCache(k, k.to(torch.bfloat16))
+    with pytest.raises(TypeError):
+        A.KVCache(k.transpose(2, 3), k.transpose(2, 3))
+    with pytest.raises(TypeError):
+        A.KVCache(k.half(), k.half())
+    c = A.KVCache(k, k.clone())
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    with pytest.raises(TypeError):
+        A.Batch(torch.zeros(2, 4), i(2), max_len=9)
+    with pytest.raises(ValueError):
+        A.Batch(i(2, 4), i(3), max_len=9)
+    with pytest.raises(ValueError):
+        A.Batch(i(2, 4), i(2), first=i(3), max_len=9)
+    with pytest.raises(ValueError):
+        A.Batch(i(2, 4), i(2))
+    b = A.Batch(i(2, 4), i(2), max_len=60)
+    q = torch.zeros(2, 4, 64)
+    for bad in (torch.zeros(3, 4, 64), torch.zeros(2, 4, 32), q.to(torch.bfloat16)):
+        with pytest.raises(TypeError):
+            A.attention_forward(c, b, A.Score(0.1), bad, bad)
+    with pytest.raises(TypeError):
+        A.attention_forward(c, b, A.Score(0.1), q, torch.zeros(2, 4, 64, dtype=torch.bfloat16))
+    with pytest.raises(TypeError):
+        A.attention_forward(c, b, A.Score(0.1), q, q.clone(), lse=torch.zeros(2, 5))
+    with pytest.raises(ValueError):
+        A.attention_forward(c, b, A.Score(0.1, slopes=torch.zeros(3)), q, q.clone())
+    with pytest.raises(ValueError):
+        A.attention_forward(c, b, A.Score(0.1, prefix=i(3)), q, q.clone())
+    with pytest.raises(TypeError):
+        A.Score(0.1, doc=i(2, 8), position=i(2, 9))
+    with pytest.raises(ValueError):
+        A.Rope(torch.zeros(9, 5), torch.zeros(9, 5), [1] * 5)
+    with pytest.raises(TypeError):
+        A.rope_append(c, b, A.Rope(torch.zeros(9, 32), torch.zeros(9, 32)), torch.zeros(2, 8 * 64 + 1), i(1, 2), q)
+    with pytest.raises(TypeError):
+        A.cache_evict(c, b, i(2, 4), c.weights(), 8, 0, 0, i(2), kept=i(2, 9))
