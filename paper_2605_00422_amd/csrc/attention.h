@@ -74,7 +74,7 @@ struct EvictArgs {
     float* weights;
     const int32_t *table, *len, *table_out, *pos;
     int32_t *len_out, *kept, *pos_out;
-    uint32_t* keys;                                        // scratch: seqs x max_len, weights as ordered integers
+    uint32_t* keys;                                        // scratch: seqs x (max_len, padded to four), weights as ordered integers
     int32_t* list;                                         // scratch: seqs x max_len, kept tokens
     int64_t page_bytes, head_bytes, slot_bytes;
     int32_t pages, page_shift, hkv, row_bytes, seqs, table_stride, table_out_stride, max_len;

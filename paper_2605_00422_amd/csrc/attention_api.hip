@@ -109,6 +109,9 @@ size_t forward_bytes(const AttArgs& a, bool weights, int dtype) {
     return weights && a.max_len > 0 ? bwla_att_weights_plan(a, dtype).bytes : 0;
 }
 
+// an integer and a place in the list for each token
+inline size_t evict_bytes(const bwla_kv_batch_t* b) { return (size_t)b->sequences * ((b->max_len + 3) & ~3) * 8; }
+
 inline bwla_status_t done(hipError_t e) { return e == hipSuccess ? BWLA_OK : BWLA_ERR_HIP; }
 
 }  // namespace
@@ -241,7 +244,7 @@ bwla_status_t bwla_cache_evict_workspace_size(const bwla_kv_cache_t* cache, cons
     if (!bytes) return BWLA_ERR_NULL;
     const bwla_status_t st = check_shapes(cache, batch, cache ? cache->kv_heads : 1);
     if (st != BWLA_OK) return st;
-    *bytes = (size_t)batch->sequences * batch->max_len * 8;
+    *bytes = evict_bytes(batch);
     return BWLA_OK;
 }
 
@@ -260,7 +263,7 @@ bwla_status_t bwla_cache_evict(const bwla_kv_cache_t* cache, const bwla_kv_batch
     if (batch->sequences == 0) return BWLA_OK;
     if (!d_len_out || !d_weights || (most > 0 && (!d_table_out || !d_ws))) return BWLA_ERR_NULL;
     if (off16(d_weights) || off16(d_ws)) return BWLA_ERR_ALIGN;
-    if (ws_bytes < (size_t)batch->sequences * batch->max_len * 8) return BWLA_ERR_BUFSIZE;
+    if (ws_bytes < evict_bytes(batch)) return BWLA_ERR_BUFSIZE;
     EvictArgs a = {};
     const int es = elem_bytes(cache->dtype);
     a.k = (char*)cache->d_k;
@@ -274,7 +277,7 @@ bwla_status_t bwla_cache_evict(const bwla_kv_cache_t* cache, const bwla_kv_batch
     a.kept = d_kept;
     a.pos_out = d_position_out;
     a.keys = (uint32_t*)d_ws;
-    a.list = (int32_t*)d_ws + (size_t)batch->sequences * batch->max_len;
+    a.list = (int32_t*)d_ws + (size_t)batch->sequences * ((batch->max_len + 3) & ~3);
     a.page_bytes = cache->page_stride * es;
     a.head_bytes = cache->head_stride * es;
     a.slot_bytes = cache->slot_stride * es;

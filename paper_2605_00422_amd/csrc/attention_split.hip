@@ -16,7 +16,7 @@ namespace {
 
 constexpr int SP_WAVES = 4;
 constexpr int SP_STEP = 32;                    // cached tokens of a step of one wavefront
-constexpr int SP_MAX_CHUNK = 2048;
+constexpr int SP_MAX_CHUNK = 1024;
 
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
@@ -48,18 +48,23 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
     __shared__ __align__(16) float s_o[SP_WAVES][16][DP + 4];
 
     const int lane = threadIdx.x & 63, wave = att_wave(), li = lane & 15, g = lane >> 4;
-    const int split = blockIdx.x, h = blockIdx.y / sp.row_tiles, rt = blockIdx.y - h * sp.row_tiles, b = blockIdx.z;
+    // units (sequence, key-value head, rows) before splits: workgroups are dealt round-robin to the 8 XCDs, and sequences
+    // of different lengths have their last splits in different numbers (8 splits side by side gave one XCD all the
+    // first ones: 64 sequences of 500 to 8192 tokens 300 us, 5320 GB/s only where all were of one length)
+    const int units = a.seqs * a.hkv * sp.row_tiles;
+    const int split = blockIdx.x / units, unit = blockIdx.x - split * units;
+    const int bh = unit / sp.row_tiles, rt = unit - bh * sp.row_tiles, b = bh / a.hkv, h = bh - b * a.hkv;
     const AttSeq s = att_seq(a, b);
     const int rows = s.fresh * a.group, row = rt * 16 + li;
     if (rt * 16 >= rows) return;
-    const int64_t unit = ((int64_t)b * a.hkv + h) * sp.row_tiles + rt;
+    const int64_t at_part = (int64_t)unit * sp.splits + split;
     const int c0 = split * sp.chunk, c1 = min(c0 + sp.chunk, s.n);
     // where no position and no row count says otherwise, keys in front of the first row's window are not read
     const int i_first = s.n - s.fresh + rt * 16 / a.group;
     const int skip_to = (s.pos || a.window == INT32_MAX) ? 0 : i_first - a.window + 1;
     const bool none = c0 >= c1 || (c1 <= skip_to && c0 >= s.prefix);
     if (none && sp.splits > 1) {
-        if (threadIdx.x < 16) stat[(unit * sp.splits + split) * 16 + threadIdx.x] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+        if (threadIdx.x < 16) stat[at_part * 16 + threadIdx.x] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
         if (scores) {                          // (what the sums of weights read of it)
             for (int r = 0; r < 16 && rt * 16 + r < rows; ++r)
                 for (int j = c0 + threadIdx.x; j < c1; j += 64 * SP_WAVES)
@@ -97,10 +102,13 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
     const char* vh = a.v + (int64_t)h * a.head_bytes;
     const int slot_mask = (1 << a.page_shift) - 1;
 
-    for (int j0 = c0 + wave * SP_STEP; j0 < c1; j0 += SP_WAVES * SP_STEP) {
-        // pages hold 8 tokens at least, so a lane's four keys of V lie in one; tokens from c1 on read the last one's row
-        v4u kf[2][KS];
-        uint32_t vf[2][4][U][VD];
+    // The keys of the next step are asked for as soon as this one's scores are there, its values as soon as this one's have
+    // been used: a wavefront always has 8 KiB on the way.  Pages hold 8 tokens at least, so a lane's four keys of V lie in
+    // one; tokens from c1 on read the last one's row.
+    v4u kf[2][KS];
+    uint32_t vf[2][4][U][VD];
+    int page_v[2];
+    auto load_keys = [&](int j0) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const int j = min(j0 + 16 * t + li, c1 - 1);
@@ -112,7 +120,8 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
                 else kf[t][u] = v4u{0, 0, 0, 0};
             }
         }
-        int page_v[2];
+    };
+    auto load_values = [&](int j0) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const int jv = j0 + 16 * t + 4 * g;
@@ -139,6 +148,13 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
                 }
             }
         }
+    };
+    constexpr int STRIDE = SP_WAVES * SP_STEP;
+    if (c0 + wave * SP_STEP < c1) {
+        load_keys(c0 + wave * SP_STEP);
+        load_values(c0 + wave * SP_STEP);
+    }
+    for (int j0 = c0 + wave * SP_STEP; j0 < c1; j0 += STRIDE) {
         float y[2][4];
         bool used[2][4];                       // whether any row sees the key: what an unseen one holds stays out
         float top = -INFINITY;
@@ -176,6 +192,7 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
                 }
             }
         }
+        if (j0 + STRIDE < c1) load_keys(j0 + STRIDE);
         top = xor32(xor16(top, true), true);
         if (__any(top > m)) {
             const float now = fmaxf(m, top);
@@ -234,6 +251,7 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
                             o[u * CW + c] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, w[t][r], o[u * CW + c], 0, 0, 0);
                         }
         }
+        if (j0 + STRIDE < c1) load_values(j0 + STRIDE);
     }
     // ---- the four wavefronts' parts, in their order
     l = xor32(xor16(l, false), false);
@@ -265,7 +283,7 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
                 *(float4*)&s_o[wave][li][u * 16 * CW + 4 * CW * g + CW * r + c] =
                     make_float4(o[u * CW + c][r] * f, o[u * CW + c + 1][r] * f, o[u * CW + c + 2][r] * f, o[u * CW + c + 3][r] * f);
     if (wave == 0 && g == 0) {
-        if (sp.splits > 1) stat[(unit * sp.splits + split) * 16 + li] = make_float4(mm, ll, llr, 0.f);
+        if (sp.splits > 1) stat[at_part * 16 + li] = make_float4(mm, ll, llr, 0.f);
         s_mm[li] = mm;
         s_ll[li] = ll;
         s_llr[li] = llr;
@@ -282,7 +300,7 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
             v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
         }
         if (sp.splits > 1) {
-            *(float4*)(part + ((unit * sp.splits + split) * 16 + r) * DP + c) = v;
+            if (rt * 16 + r < rows) *(float4*)(part + (at_part * 16 + r) * DP + c) = v;
         } else if (rt * 16 + r < rows && c < a.d) {
             const float total = s_ll[r], inv = total > 0.f ? 1.f / s_llr[r] : 0.f;
             const int t = (rt * 16 + r) / a.group, hd = h * a.group + rt * 16 + r - t * a.group;
@@ -294,15 +312,16 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
     }
 }
 
-// One row's parts added up: 8 (4 at 256 columns) groups of threads take every eighth split, four columns a thread.
-template <bool BF, int DP>
-__global__ __launch_bounds__(256) void att_join_kernel(AttArgs a, AttSplit sp, const float* __restrict__ part,
-                                                       const float4* __restrict__ stat) {
-    constexpr int LANES = DP / 4, GROUPS = 256 / LANES;
-    __shared__ float red[8];
-    __shared__ float s_l[GROUPS], s_lr[GROUPS];
+// One row's parts added up.  GROUPS groups of threads take every GROUPS-th split, four columns a thread, with two of their
+// loads in flight; the splits' factors are computed once, in LDS.
+template <bool BF, int DP, int GROUPS>
+__global__ __launch_bounds__(GROUPS * DP / 4) void att_join_kernel(AttArgs a, AttSplit sp, const float* __restrict__ part,
+                                                                   const float4* __restrict__ stat) {
+    constexpr int LANES = DP / 4, THREADS = GROUPS * LANES, WAVES = THREADS / 64;
+    constexpr int MOST = 512;                          // splits whose factors fit
+    __shared__ float red[3 * WAVES], s_f[MOST];
     __shared__ __align__(16) float s_o[GROUPS][DP];
-    const int h = blockIdx.y, b = blockIdx.z, row = blockIdx.x;
+    const int h = blockIdx.y, b = blockIdx.z, row = blockIdx.x, tid = threadIdx.x;
     const AttSeq s = att_seq(a, b);
     if (row >= s.fresh * a.group) return;
     const int rt = row >> 4, r = row & 15;
@@ -310,36 +329,56 @@ __global__ __launch_bounds__(256) void att_join_kernel(AttArgs a, AttSplit sp, c
     const int used = (s.n + sp.chunk - 1) / sp.chunk;
     const float4* st = stat + unit * sp.splits * 16 + r;
     float m = -INFINITY;
-    for (int i = threadIdx.x; i < used; i += 256) m = fmaxf(m, st[i * 16].x);
+    for (int i = tid; i < used; i += THREADS) m = fmaxf(m, st[i * 16].x);
     m = bwla_wave_max(m);
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+    if ((tid & 63) == 0) red[tid >> 6] = m;
     __syncthreads();
-    m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    const int grp = threadIdx.x / LANES, c = threadIdx.x % LANES * 4;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) m = fmaxf(m, red[w]);
+    const int grp = tid / LANES, c = tid % LANES * 4;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     float l = 0.f, lr = 0.f;
-    for (int i = grp; i < used; i += GROUPS) {
-        const float4 x = st[i * 16];
-        if (x.x == -INFINITY) continue;
-        const float f = __builtin_amdgcn_exp2f(x.x - m);
-        l += x.y * f;
-        lr += x.z * f;
-        const float4 p = *(const float4*)(part + ((unit * sp.splits + i) * 16 + r) * DP + c);
-        v.x += p.x * f; v.y += p.y * f; v.z += p.z * f; v.w += p.w * f;
+    for (int i0 = 0; i0 < used; i0 += MOST) {
+        const int up = min(used - i0, MOST);
+        __syncthreads();
+        for (int i = tid; i < up; i += THREADS) {
+            const float4 x = st[(i0 + i) * 16];
+            const float f = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.x - m);
+            s_f[i] = f;
+            l += x.y * f;
+            lr += x.z * f;
+        }
+        __syncthreads();
+        const float* src = part + ((unit * sp.splits + i0) * 16 + r) * DP + c;
+#pragma unroll 2
+        for (int i = grp; i < up; i += GROUPS) {
+            const float f = s_f[i];
+            if (f == 0.f) continue;                    // (nothing was written where nothing is seen)
+            const float4 p = *(const float4*)(src + (int64_t)i * 16 * DP);
+            v.x += p.x * f; v.y += p.y * f; v.z += p.z * f; v.w += p.w * f;
+        }
     }
-    if (c == 0) {
-        s_l[grp] = l;
-        s_lr[grp] = lr;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        l += __shfl_xor(l, o, 64);
+        lr += __shfl_xor(lr, o, 64);
+    }
+    if ((tid & 63) == 0) {
+        red[WAVES + (tid >> 6)] = l;
+        red[2 * WAVES + (tid >> 6)] = lr;
     }
     *(float4*)&s_o[grp][c] = v;
     __syncthreads();
     if (grp != 0 || c >= a.d) return;
     l = lr = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        l += red[WAVES + w];
+        lr += red[2 * WAVES + w];
+    }
     v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) {
-        l += s_l[i];
-        lr += s_lr[i];
         const float4 p = *(const float4*)&s_o[i][c];
         v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
     }
@@ -351,24 +390,36 @@ __global__ __launch_bounds__(256) void att_join_kernel(AttArgs a, AttSplit sp, c
     if (c == 0 && a.lse) a.lse[(int64_t)(s.row0 + t) * a.hq + hd] = l > 0.f ? (m + __log2f(l)) * ATT_LN2 : -INFINITY;
 }
 
-// The rows' weights of each cached token, from the scores that the first launch left, added to the token's sum.
+// The rows' weights of each cached token, from the scores that the first launch left, added to the token's sum.  A thread
+// takes four tokens, which lie in one page.
 __global__ __launch_bounds__(256) void att_sum_kernel(AttArgs a, AttSplit sp, const float* __restrict__ scores) {
-    const int j = blockIdx.x * 256 + threadIdx.x, h = blockIdx.y, b = blockIdx.z;
+    const int j = (blockIdx.x * 256 + threadIdx.x) * 4, h = blockIdx.y, b = blockIdx.z;
     const AttSeq s = att_seq(a, b);
     if (j >= s.n) return;
     const int p = s.table[j >> a.page_shift];
     if ((unsigned)p >= (unsigned)a.pages) return;
     const float* src = scores + (int64_t)(b * a.hkv + h) * sp.rows * sp.pitch + j;
     const int rows = s.fresh * a.group;
-    float sum = 0.f;
+    float4* const w = (float4*)(a.weights + (((int64_t)p * a.hkv + h) << a.page_shift) + (j & ((1 << a.page_shift) - 1)));
+    float4 sum = *w;
+    float4 add = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float* lse = a.lse + (int64_t)s.row0 * a.hq + h * a.group;
+#pragma unroll 4
     for (int r = 0; r < rows; ++r) {
         const int t = r / a.group;
-        const float lse = a.lse[(int64_t)(s.row0 + t) * a.hq + h * a.group + r - t * a.group];
-        const float y = src[(int64_t)r * sp.pitch];
-        sum += y == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(y - lse * ATT_LOG2E);
+        const float l = lse[(int64_t)t * a.hq + r - t * a.group] * ATT_LOG2E;
+        const float4 y = *(const float4*)(src + (int64_t)r * sp.pitch);
+        // (a row that sees nothing has scores of -inf only; behind the sequence's last token lie none)
+        add.x += y.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(y.x - l);
+        add.y += y.y == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(y.y - l);
+        add.z += y.z == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(y.z - l);
+        add.w += y.w == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(y.w - l);
     }
-    float* w = a.weights + (((int64_t)p * a.hkv + h) << a.page_shift) + (j & ((1 << a.page_shift) - 1));
-    *w += sum;
+    sum.x += add.x;
+    if (j + 1 < s.n) sum.y += add.y;
+    if (j + 2 < s.n) sum.z += add.z;
+    if (j + 3 < s.n) sum.w += add.w;
+    *w = sum;
 }
 
 template <bool BF, int DP>
@@ -376,11 +427,16 @@ hipError_t launch(const AttArgs& a, const AttSplit& s, void* ws, hipStream_t st)
     float* part = (float*)ws;
     float4* stat = (float4*)((char*)ws + s.part_bytes);
     float* scores = a.weights ? (float*)((char*)ws + s.part_bytes + s.stat_bytes) : nullptr;
-    const dim3 grid(s.splits, a.hkv * s.row_tiles, a.seqs);
+    const dim3 grid((unsigned)((int64_t)s.splits * a.seqs * a.hkv * s.row_tiles));
     if (a.d == DP) att_split_kernel<BF, DP, true><<<grid, 64 * SP_WAVES, 0, st>>>(a, s, part, stat, scores);
     else att_split_kernel<BF, DP, false><<<grid, 64 * SP_WAVES, 0, st>>>(a, s, part, stat, scores);
-    if (s.splits > 1) att_join_kernel<BF, DP><<<dim3(s.rows, a.hkv, a.seqs), 256, 0, st>>>(a, s, part, stat);
-    if (scores && a.max_len > 0) att_sum_kernel<<<dim3((a.max_len + 255) / 256, a.hkv, a.seqs), 256, 0, st>>>(a, s, scores);
+    // many splits (long caches of few sequences): more threads for each row.  128 splits of 64 rows 13.2 -> 7.2 us, but 4 splits of
+    // 4096 rows 8.8 -> 16.3 us
+    constexpr int FEW = 4, MANY = DP == 256 ? 8 : 16;
+    const dim3 rows(s.rows, a.hkv, a.seqs);
+    if (s.splits > 16) att_join_kernel<BF, DP, MANY><<<rows, MANY * DP / 4, 0, st>>>(a, s, part, stat);
+    else if (s.splits > 1) att_join_kernel<BF, DP, FEW><<<rows, FEW * DP / 4, 0, st>>>(a, s, part, stat);
+    if (scores && a.max_len > 0) att_sum_kernel<<<dim3((a.max_len + 1023) / 1024, a.hkv, a.seqs), 256, 0, st>>>(a, s, scores);
     return hipGetLastError();
 }
 
@@ -394,7 +450,7 @@ AttSplit bwla_att_split(const AttArgs& a, bool weights) {
     s.row_tiles = (s.rows + 15) / 16;
     const int64_t units = (int64_t)a.seqs * a.hkv * s.row_tiles;
     const int64_t step = SP_WAVES * SP_STEP;
-    int64_t chunk = (units * a.max_len + 1023) / 1024;
+    int64_t chunk = (units * a.max_len + 511) / 512;
     chunk = (chunk + step - 1) / step * step;
     s.chunk = (int)(chunk < 2 * step ? 2 * step : chunk > SP_MAX_CHUNK ? SP_MAX_CHUNK : chunk);
     s.splits = a.max_len > 0 ? (a.max_len + s.chunk - 1) / s.chunk : 1;

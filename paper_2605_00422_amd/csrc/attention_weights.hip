@@ -19,7 +19,7 @@ struct WtShape {
 };
 
 template <bool BF, int DP, bool EXACT>
-__global__ __launch_bounds__(64 * WT_WAVES) void att_weights_kernel(AttArgs a, int parts, int64_t pitch, float* __restrict__ sums) {
+__global__ __launch_bounds__(64 * WT_WAVES, DP * (BF ? 1 : 2) > 128 ? 1 : 2) void att_weights_kernel(AttArgs a, int parts, int64_t pitch, float* __restrict__ sums) {
     constexpr int ES = BF ? 2 : 4, CH = DP * ES / 16, KT = WtShape<BF, DP>::KT;
     const int lane = threadIdx.x & 63, wave = att_wave(), l32 = lane & 31, hf = lane >> 5;
     const int h = blockIdx.y, b = blockIdx.z / parts, part = blockIdx.z - b * parts;
@@ -30,7 +30,8 @@ __global__ __launch_bounds__(64 * WT_WAVES) void att_weights_kernel(AttArgs a, i
     const int slot_mask = (1 << a.page_shift) - 1;
 
     v4u kf[KT][CH / 2];
-    AttKey key[KT][16];
+    AttKey key[KT];                                    // lane l32 knows key l32 of each tile
+    bool all = true;
 #pragma unroll
     for (int k = 0; k < KT; ++k) {
         const int j = min(j0 + k * 32 + l32, s.n - 1);
@@ -42,15 +43,11 @@ __global__ __launch_bounds__(64 * WT_WAVES) void att_weights_kernel(AttArgs a, i
             const int at = (2 * c + hf) * 16;
             kf[k][c] = EXACT || at < a.d * ES ? *(const v4u*)(src + at) : v4u{0, 0, 0, 0};
         }
-        // lane l32 knows key l32 of the tile; the lane's accumulators are keys (r & 3) + 8 (r >> 2) + 4 hf
-        const AttKey mine = att_key(a, s, j0 + k * 32 + l32, there);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int from = (r & 3) + 8 * (r >> 2) + 4 * hf;
-            key[k][r].p = __shfl(mine.p, from, 64);
-            key[k][r].doc = __shfl(mine.doc, from, 64);
-        }
+        key[k] = att_key(a, s, j0 + k * 32 + l32, there);
+        all &= key[k].doc >= 0;
     }
+    // keys that every row from some index on sees (without documents, or with a window to keep to: none)
+    const bool plain = att_uniform(__all(all) & !s.doc & (a.window == INT32_MAX));
     float sum[16 * KT];
 #pragma unroll
     for (int e = 0; e < 16 * KT; ++e) sum[e] = 0.f;
@@ -60,22 +57,42 @@ __global__ __launch_bounds__(64 * WT_WAVES) void att_weights_kernel(AttArgs a, i
     if (!s.pos && a.window != INT32_MAX && j0 >= s.prefix) t1 = (int)min((int64_t)t1, (int64_t)j0 + 32 * KT - 1 + a.window - old);
     const int first = t0 * a.group / 32, tiles = t1 > t0 ? (t1 * a.group + 31) / 32 : 0;
     // (from the part's first tile at or behind `first`)
-    for (int tile = first + (part - first % parts + parts) % parts; tile < tiles; tile += parts) {
+    struct Tile {
+        v4u q[CH / 2];
+        float lse, slope;                              // lse in base 2, +inf where the row sees nothing: its weights are 0
+        int tok;
+        bool live;
+    };
+    auto fetch = [&](int tile) {
+        Tile x;
         const int row = tile * 32 + l32;
-        const bool live = row < rows;
-        const int tok = live ? row / a.group : 0, head = h * a.group + (live ? row - tok * a.group : 0);
-        const AttRow me = att_row(s, tok, live);
-        const int64_t at = (int64_t)(s.row0 + tok);
-        const float lse = live ? a.lse[at * a.hq + head] * ATT_LOG2E : 0.f;
-        const float slope = a.slopes ? a.slopes[head] * ATT_LOG2E : 0.f;
-        const bool some = live && lse != -INFINITY;
-        v4u qf[CH / 2];
+        x.live = row < rows;
+        x.tok = x.live ? row / a.group : 0;
+        const int head = h * a.group + (x.live ? row - x.tok * a.group : 0);
+        const int64_t at = (int64_t)(s.row0 + x.tok);
+        const float lse = a.lse[at * a.hq + head] * ATT_LOG2E;
+        x.lse = x.live & (lse != -INFINITY) ? lse : INFINITY;
+        x.slope = a.slopes ? a.slopes[head] * ATT_LOG2E : 0.f;
         const char* qp = a.q + at * a.q_bytes + (int64_t)head * a.d * ES;
 #pragma unroll
         for (int c = 0; c < CH / 2; ++c) {
             const int col = (2 * c + hf) * 16;
-            qf[c] = live && (EXACT || col < a.d * ES) ? *(const v4u*)(qp + col) : v4u{0, 0, 0, 0};
+            x.q[c] = EXACT || col < a.d * ES ? *(const v4u*)(qp + col) : v4u{0, 0, 0, 0};
         }
+        return x;
+    };
+    int tile = first + (part - first % parts + parts) % parts;
+    Tile next;
+    if (tile < tiles) next = fetch(tile);
+    for (; tile < tiles; tile += parts) {
+        const Tile x = next;
+        if (tile + parts < tiles) next = fetch(tile + parts);
+        const auto& qf = x.q;
+        const float lse = x.lse, slope = x.slope;
+        const int first_i = old + tile * 32 / a.group;
+        const bool whole = plain & ((first_i >= j0 + 32 * KT - 1) | (j0 + 32 * KT <= s.prefix));
+        AttRow me{0, 0, 0};
+        if (!whole || a.slopes) me = att_row(s, x.tok, x.live);
 #pragma unroll
         for (int k = 0; k < KT; ++k) {
             v16f p;
@@ -91,14 +108,23 @@ __global__ __launch_bounds__(64 * WT_WAVES) void att_weights_kernel(AttArgs a, i
                         p = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[k][c][e]), __uint_as_float(qf[c][e]), p, 0, 0, 0);
                 }
             }
+            if (a.capped != 0.f) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int j = j0 + k * 32 + (r & 3) + 8 * (r >> 2) + 4 * hf;
-                float y = att_score(a, p[r]);
-                if (a.slopes) y -= slope * fabsf((float)(me.p - key[k][r].p));
-                const bool seen = some && att_sees(me, s.prefix, a.window, j, key[k][r].p, key[k][r].doc);
-                sum[k * 16 + r] += seen ? __builtin_amdgcn_exp2f(y - lse) : 0.f;
+                for (int r = 0; r < 16; ++r) p[r] = a.capped * att_tanh(p[r] * a.c2);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) p[r] *= a.c1;
             }
+            if (!whole || a.slopes) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int from = (r & 3) + 8 * (r >> 2) + 4 * hf;
+                    const int kp = __shfl(key[k].p, from, 64), kd = __shfl(key[k].doc, from, 64);
+                    p[r] = att_sees(me, s.prefix, a.window, j0 + k * 32 + from, kp, kd) ? p[r] - slope * fabsf((float)(me.p - kp)) : -INFINITY;
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sum[k * 16 + r] += __builtin_amdgcn_exp2f(p[r] - lse);
         }
     }
     // the 32 lanes' sums: each step halves what a lane holds, so that lane l32 ends with accumulator l32
@@ -158,9 +184,11 @@ AttWeightsPlan bwla_att_weights_plan(const AttArgs& a, int dtype) {
     const int64_t keys = (wide > 256 ? 1 : 2) * 32 * WT_WAVES;
     const int64_t groups = (a.max_len + keys - 1) / keys * a.hkv * a.seqs;
     const int64_t tiles = ((int64_t)a.max_new * a.group + 31) / 32;
-    // parts until there are two workgroups a compute unit, of eight steps at least
+    // parts until there are two workgroups a compute unit, of four steps at least (0.4 us each at 128 columns), one in
+    // fp32 (3.5 us)
     int64_t parts = (512 + groups - 1) / groups;
-    if (parts > tiles / 8) parts = tiles / 8;
+    const int64_t most = dtype == BWLA_X_BF16 ? tiles / 4 : tiles;
+    if (parts > most) parts = most;
     if (parts > 65535 / a.seqs) parts = 65535 / a.seqs;
     AttWeightsPlan p;
     p.parts = parts < 1 ? 1 : (int)parts;

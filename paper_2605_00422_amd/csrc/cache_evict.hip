@@ -1,34 +1,40 @@
 // Eviction: each sequence's heaviest tokens, moved in order to pages of their own.
 //
 // Three launches: the tokens' weights as integers of the same order (sum over the heads in 64 bits, rounded once);
-// per sequence the keep-th largest of them by a radix selection, eight bits a pass over counts in LDS, and the kept
-// tokens' list by prefix sums in index order, so that ties fall to the lowest index; the copy of keys, values and sums,
-// one thread 16 bytes, from anywhere to anywhere, since the pages written are no others' pages.
+// per sequence the keep-th largest of them by a radix selection (11, 11 and 10 bits a pass over counts in LDS: the first digit
+// holds the exponent and two bits more, so that a pass's additions spread over many words), and the kept tokens' list
+// by prefix sums in index order, so that ties fall to the lowest index; the copy of keys, values and sums, one thread
+// 16 bytes, from anywhere to anywhere, since the pages written are no others' pages.  In the second launch a thread
+// has a run of neighbouring tokens, whose integers stay in registers up to 32 of them.  Short sequences (EV_SHORT) have
+// their integers made there, too, which spares a launch.
 #include "attention.h"
 
 namespace {
 
+constexpr int EV_T = 1024;
+constexpr int EV_SHORT = 2 * EV_T;
+
+// a token's weight as an integer of the same order: 0 where its page does not exist, all ones where it stays anyway
+__device__ __forceinline__ uint32_t evict_key(const EvictArgs& a, int b, int n, int j) {
+    const int p = a.table[(int64_t)b * a.table_stride + (j >> a.page_shift)];
+    if ((unsigned)p >= (unsigned)a.pages) return 0;
+    if (j < a.sinks || j >= n - a.recent) return 0xffffffffu;
+    const float* w = a.weights + (((int64_t)p * a.hkv) << a.page_shift) + (j & ((1 << a.page_shift) - 1));
+    double sum = 0.0;
+#pragma unroll 4
+    for (int h = 0; h < a.hkv; ++h) sum += (double)w[(int64_t)h << a.page_shift];
+    const float f = sum != sum ? -INFINITY : (float)sum + 0.f;         // (+ 0: one zero)
+    const uint32_t u = __float_as_uint(f);
+    return u >> 31 ? ~u : u | 0x80000000u;             // (-inf: 0x007fffff, +inf: 0xff800000)
+}
+
 __global__ __launch_bounds__(256) void evict_keys_kernel(EvictArgs a) {
     const int b = blockIdx.y, j = blockIdx.x * 256 + threadIdx.x;
     const int n = min(max(a.len[b], 0), a.max_len);
-    if (j >= n) return;
-    const int p = a.table[(int64_t)b * a.table_stride + (j >> a.page_shift)];
-    uint32_t key = 0;                                  // below every weight: the page does not exist
-    if ((unsigned)p < (unsigned)a.pages) {
-        const float* w = a.weights + (((int64_t)p * a.hkv) << a.page_shift) + (j & ((1 << a.page_shift) - 1));
-        double sum = 0.0;
-        for (int h = 0; h < a.hkv; ++h) sum += (double)w[(int64_t)h << a.page_shift];
-        const float f = sum != sum ? -INFINITY : (float)sum + 0.f;     // (+ 0: one zero)
-        const uint32_t u = __float_as_uint(f);
-        key = u >> 31 ? ~u : u | 0x80000000u;
-        if (j < a.sinks || j >= n - a.recent) key = 0xffffffffu;
-    }
-    a.keys[(int64_t)b * a.max_len + j] = key;
+    if (j < n) a.keys[(int64_t)b * ((a.max_len + 3) & ~3) + j] = evict_key(a, b, n, j);
 }
 
-constexpr int EV_T = 1024;
-
-// sum of v over the threads before this one, and over all of them; red: 17 words of LDS
+// sum of v over the threads before this one, and over all of them; red: a word of LDS for each wavefront
 __device__ __forceinline__ int scan(int v, int* red, int& total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int x = v;
@@ -50,69 +56,105 @@ __device__ __forceinline__ int scan(int v, int* red, int& total) {
     return before + x - v;
 }
 
+// RUN: integers that a thread holds in registers, 0: none, they are read each time
+template <int RUN>
 __global__ __launch_bounds__(EV_T) void evict_pick_kernel(EvictArgs a) {
-    __shared__ int hist[256];
+    __shared__ int hist[4][2048];                      // four copies: neighbouring lanes mostly have the same first digit
     __shared__ int red[EV_T / 64];
     __shared__ uint32_t s_prefix;
     __shared__ int s_need;
     const int b = blockIdx.x, tid = threadIdx.x;
     const int n = min(max(a.len[b], 0), a.max_len);
-    const uint32_t* keys = a.keys + (int64_t)b * a.max_len;
+    const uint32_t* keys = a.keys + (int64_t)b * ((a.max_len + 3) & ~3);
     int* list = a.list + (int64_t)b * a.max_len;
+    const int run = RUN ? RUN : (n + EV_T - 1) / EV_T, j0 = min(tid * run, n), len = min(run, n - j0);
+
+    uint32_t own[RUN ? RUN : 1];
+    if constexpr (RUN != 0) {
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) own[i] = 0;
+        if constexpr (RUN * EV_T <= EV_SHORT) {
+#pragma unroll
+            for (int i = 0; i < RUN; ++i)
+                if (i < len) own[i] = evict_key(a, b, n, j0 + i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < RUN; i += 4)
+                if (i < len) {                         // (rows are padded to four)
+                    const uint4 x = *(const uint4*)(keys + j0 + i);
+                    own[i] = x.x;
+                    own[i + 1] = i + 1 < len ? x.y : 0;
+                    own[i + 2] = i + 2 < len ? x.z : 0;
+                    own[i + 3] = i + 3 < len ? x.w : 0;
+                }
+        }
+    }
+    auto each = [&](auto f) {                          // f(key, token) in order; tokens that do not exist have key 0
+        if constexpr (RUN != 0) {
+#pragma unroll
+            for (int i = 0; i < RUN; ++i) f(own[i], j0 + i);
+        } else {
+            for (int i = 0; i < len; ++i) f(keys[j0 + i], j0 + i);
+        }
+    };
 
     int mine = 0, exist;
-    for (int j = tid; j < n; j += EV_T) mine += keys[j] != 0;
+    each([&](uint32_t k, int) { mine += k != 0; });
     scan(mine, red, exist);
     const int kept = min(exist, a.keep);
-    // the kept-th largest key, and how many of its equals belong to the kept
+    // the kept-th largest integer, and how many of its equals are kept
     uint32_t limit = 1;
-    int equals = 0;                                    // with exist <= keep: all above 0
-    if (exist > a.keep) {
+    int equals = 0;                                    // exist <= keep: all that is above 0
+    if (exist > a.keep && a.keep > 0) {
         if (tid == 0) { s_prefix = 0; s_need = a.keep; }
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            if (tid < 256) hist[tid] = 0;
+#pragma unroll
+        for (int pass = 0; pass < 3; ++pass) {
+            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
+            for (int i = tid; i < 4 * 2048; i += EV_T) (&hist[0][0])[i] = 0;
             __syncthreads();
             const uint32_t prefix = s_prefix;
-            for (int j = tid; j < n; j += EV_T) {
-                const uint32_t k = keys[j];
-                if (shift == 24 || (k ^ prefix) >> (shift + 8) == 0) atomicAdd(&hist[(k >> shift) & 255], 1);
+            each([&](uint32_t k, int) {
+                if (k != 0 && (pass == 0 || (k ^ prefix) >> (pass == 1 ? 21 : 10) == 0)) atomicAdd(&hist[tid & 3][(k >> shift) & (bins - 1)], 1);
+            });
+            __syncthreads();
+            // digits from the largest down, two a thread: the one in which the count reaches what is needed
+            const int hi = bins - 1 - 2 * tid;
+            int c0 = 0, c1 = 0;
+            if (hi >= 1) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { c0 += hist[i][hi]; c1 += hist[i][hi - 1]; }
             }
-            __syncthreads();
-            // digits from the largest down: the one in which the count reaches what is needed
-            const int c = tid < 256 ? hist[255 - tid] : 0;
             int total;
-            const int before = scan(c, red, total);
-            const int need = s_need;
+            const int before = scan(c0 + c1, red, total), need = s_need;
             __syncthreads();
-            if (tid < 256 && before < need && before + c >= need) {
-                s_prefix = prefix | (uint32_t)(255 - tid) << shift;
-                s_need = need - before;
+            if (before < need && before + c0 + c1 >= need) {
+                const bool second = before + c0 < need;
+                s_prefix = prefix | (uint32_t)(hi - second) << shift;
+                s_need = need - before - (second ? c0 : 0);
             }
             __syncthreads();
         }
         limit = s_prefix;
         equals = s_need;
     }
-    int out = 0, same = 0;                             // kept so far, equals so far
-    for (int j0 = 0; j0 < n; j0 += EV_T) {
-        const int j = j0 + tid;
-        const uint32_t k = j < n ? keys[j] : 0;
-        bool take = k > limit || (equals == 0 && k == limit);
-        if (equals > 0) {
-            int total;
-            const int before = same + scan(k == limit, red, total);
-            take = k > limit || (k == limit && before < equals);
-            same += total;
-        }
-        int total;
-        const int at = out + scan(take, red, total);
+    if (a.keep == 0) limit = 0xffffffffu, equals = -1;
+    // this thread's part: what lies above, and of the equals those that come first
+    int above = 0, same = 0, total;
+    each([&](uint32_t k, int) { above += k > limit; same += k == limit; });
+    int left = 0;                                      // equals that are still to take when this thread's turn comes
+    if (equals > 0) left = equals - scan(same, red, total);
+    else if (equals == 0) left = 1 << 30;
+    else above = 0;
+    int at = scan(above + min(same, max(left, 0)), red, total);
+    each([&](uint32_t k, int j) {
+        const bool take = equals >= 0 && (k > limit || (k == limit && left-- > 0));
         if (take) {
             list[at] = j;
             if (a.kept) a.kept[(int64_t)b * a.keep + at] = j;
             if (a.pos) a.pos_out[(int64_t)b * a.keep + at] = a.pos[(int64_t)b * a.pos_stride + j];
+            ++at;
         }
-        out += total;
-    }
+    });
     for (int i = kept + tid; i < a.keep; i += EV_T) {
         if (a.kept) a.kept[(int64_t)b * a.keep + i] = -1;
         if (a.pos) a.pos_out[(int64_t)b * a.keep + i] = -1;
@@ -142,8 +184,13 @@ __global__ __launch_bounds__(256) void evict_copy_kernel(EvictArgs a, int pieces
 }  // namespace
 
 hipError_t bwla_launch_evict(const EvictArgs& a, hipStream_t st) {
-    if (a.max_len > 0) evict_keys_kernel<<<dim3((a.max_len + 255) / 256, a.seqs), 256, 0, st>>>(a);
-    evict_pick_kernel<<<a.seqs, EV_T, 0, st>>>(a);
+    if (a.max_len > EV_SHORT) evict_keys_kernel<<<dim3((a.max_len + 255) / 256, a.seqs), 256, 0, st>>>(a);
+    if (a.max_len <= EV_SHORT) evict_pick_kernel<2><<<a.seqs, EV_T, 0, st>>>(a);
+    else if (a.max_len <= 4 * EV_T) evict_pick_kernel<4><<<a.seqs, EV_T, 0, st>>>(a);
+    else if (a.max_len <= 8 * EV_T) evict_pick_kernel<8><<<a.seqs, EV_T, 0, st>>>(a);
+    else if (a.max_len <= 16 * EV_T) evict_pick_kernel<16><<<a.seqs, EV_T, 0, st>>>(a);
+    else if (a.max_len <= 32 * EV_T) evict_pick_kernel<32><<<a.seqs, EV_T, 0, st>>>(a);
+    else evict_pick_kernel<0><<<a.seqs, EV_T, 0, st>>>(a);
     const int pieces = a.row_bytes / 16;
     const int64_t work = (int64_t)(a.keep < a.max_len ? a.keep : a.max_len) * pieces;
     if (work > 0) evict_copy_kernel<<<dim3((unsigned)((work + 255) / 256), a.hkv, a.seqs), 256, 0, st>>>(a, pieces);
