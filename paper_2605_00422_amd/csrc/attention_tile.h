@@ -16,6 +16,7 @@ namespace {
 
 constexpr int AT_WAVES = 4;
 constexpr int AT_ROWS = 32 * AT_WAVES;
+constexpr int AT_MAP = 4096;                           // blocks of keys that the map of active ones covers; those behind count as active
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ float half_max(float v) {
@@ -27,6 +28,21 @@ __device__ __forceinline__ float half_sum(float v) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// Workgroups are dealt round-robin to the 8 XCDs, units (sequence, key-value head) to workgroups, so that an XCD keeps to
+// some of them, whose keys and values then stay in its own L2.  Later tiles of rows see more keys.  ORDER_DOWN: the longest
+// first, which evens out where there are many workgroups; ORDER_FOLD: where all run at once, the first half of them from the
+// longest down, the second from the shortest up, so that a compute unit gets a long one and a short one.
+enum { ORDER_DOWN = 0, ORDER_FOLD = 1 };
+__device__ __forceinline__ void att_order(int id, int tiles, int units, int order, int& unit, int& tile) {
+    const int k = id / units;
+    unit = id - k * units;
+    const int half = tiles / 2;
+    tile = order == ORDER_FOLD && k >= tiles - half ? k - (tiles - half) : tiles - 1 - k;
+}
+inline int att_order_of(int tiles, int units, int per_cu) {
+    return (int64_t)tiles * units <= (int64_t)per_cu * bwla_device_cus() ? ORDER_FOLD : ORDER_DOWN;
+}
+
 template <bool BF, int DP>
 struct AtShape {
     static constexpr int ES = BF ? 2 : 4;
@@ -35,350 +51,384 @@ struct AtShape {
     static constexpr int CH = ROWB / 16;               // 16-byte pieces of a row
     static constexpr int TILE = BK * ROWB;             // bytes of a block of keys, and of values
     static constexpr int COPIES = BK * CH / (64 * AT_WAVES);
-    static constexpr int LDS = 4 * TILE + 2 * (2 * BK + 4) * 4;
+    static constexpr int LDS = 4 * TILE + AT_MAP / 8 + 2 * AT_WAVES * 4;       // two blocks of each, the map of active blocks
 };
 
 // BF: bf16 (else fp32); DP: columns, 64, 128 or 256; EXACT: d == DP; GENERAL: a cap or a bias
 template <bool BF, int DP, bool EXACT, bool GENERAL>
-__global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_kernel(AttArgs a, int tiles, int units) {
+__global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_kernel(AttArgs a, int tiles, int units, int order) {
     using S = AtShape<BF, DP>;
-    constexpr int ES = S::ES, BK = S::BK, ROWB = S::ROWB, CH = S::CH, KT = BK / 32, DT = DP / 32;
+    constexpr int ES = S::ES, BK = S::BK, ROWB = S::ROWB, CH = S::CH, KT = BK / 32, DT = DP / 32, CS = CH / 2;
     extern __shared__ __align__(16) char smem[];
     char* const ks = smem;                             // [2][BK][ROWB]
     char* const vs = smem + 2 * S::TILE;
-    int* const info = (int*)(smem + 4 * S::TILE);      // [2][BK positions, BK documents, flag]
-    constexpr int INFO = 2 * BK + 4;
 
-    // workgroups are dealt round-robin to the 8 XCDs: each takes whole (sequence, key-value head) units, whose
-    // keys and values then stay in its own L2, the longest rows first
     int unit, tile;
-    if (units % 8 == 0 || units >= 32) {
-        const int x = blockIdx.x & 7, k = blockIdx.x >> 3;
-        unit = k / tiles * 8 + x;
-        tile = tiles - 1 - k % tiles;
-    } else {
-        unit = blockIdx.x % units;
-        tile = tiles - 1 - blockIdx.x / units;
-    }
+    att_order(blockIdx.x, tiles, units, order, unit, tile);
     if (unit >= units || tile < 0) return;
     const int b = unit / a.hkv, h = unit - b * a.hkv;
     const AttSeq s = att_seq(a, b);
     const int rows = s.fresh * a.group;
     if (tile * AT_ROWS >= rows) return;
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = att_wave(), l32 = lane & 31, hf = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = att_wave(), l32 = lane & 31, hf = lane >> 5;
     const int row = tile * AT_ROWS + wave * 32 + l32;
     const bool live = row < rows;
     const int tok = live ? row / a.group : 0, head = h * a.group + (live ? row - tok * a.group : 0);
     const AttRow me = att_row(s, tok, live);
     const float slope = GENERAL && a.slopes ? a.slopes[head] * ATT_LOG2E : 0.f;
+    v4u qf[CS];
+    {
+        const char* qp = a.q + (int64_t)(s.row0 + tok) * a.q_bytes + (int64_t)head * a.d * ES;
+#pragma unroll
+        for (int c = 0; c < CS; ++c) {
+            const int at = (2 * c + hf) * 16;
+            qf[c] = live && (EXACT || at < a.d * ES) ? *(const v4u*)(qp + at) : v4u{0, 0, 0, 0};
+        }
+    }
     // indexes of the first and last row of this wavefront, and of the workgroup
     const int old = s.n - s.fresh;
     const int w_first = old + min(tile * AT_ROWS + wave * 32, rows - 1) / a.group;
     const int w_last = old + min(tile * AT_ROWS + wave * 32 + 31, rows - 1) / a.group;
     const int g_first = max(old + tile * AT_ROWS / a.group, 0);
     const int g_last = old + min(tile * AT_ROWS + AT_ROWS - 1, rows - 1) / a.group;
-
     // blocks of keys: those of the prefix, then from the first row's window to the last row's index
-    const int hi = max((g_last + BK) / BK, 0);
     const int pb = min((max(s.prefix, 0) + BK - 1) / BK, (s.n + BK - 1) / BK);
     int lo = s.pos || a.window == INT32_MAX ? 0 : max(g_first - a.window + 1, 0) / BK;
     if (lo < pb) lo = pb;
-    const int blocks = pb + max(hi - lo, 0);
-
-    v4u qf[CH / 2];
-    {
-        const char* qp = a.q + (int64_t)(s.row0 + tok) * a.q_bytes + (int64_t)head * a.d * ES;
+    const int end = max((g_last + BK) / BK, pb);
+    // documents: the range of the workgroup's, and the wavefront's if its rows are all in one (else -3)
+    int one_doc = 0;
+    if (s.doc) {
+        uint32_t* const active = (uint32_t*)(smem + 4 * S::TILE);              // a bit for each block that may matter
+        int* const range = (int*)(active + AT_MAP / 32);
+        int dmin = live && me.doc >= 0 ? me.doc : INT32_MAX, dmax = live ? me.doc : -2;
+        const int first_doc = __builtin_amdgcn_readfirstlane(me.doc);
+        one_doc = att_uniform(__all(!live | (me.doc == first_doc)) && first_doc >= 0) ? first_doc : -3;
 #pragma unroll
-        for (int t = 0; t < CH / 2; ++t) {
-            const int c = (2 * t + hf) * 16;
-            qf[t] = live && (EXACT || c < a.d * ES) ? *(const v4u*)(qp + c) : v4u{0, 0, 0, 0};
+        for (int i = 1; i < 64; i <<= 1) {
+            dmin = min(dmin, __shfl_xor(dmin, i, 64));
+            dmax = max(dmax, __shfl_xor(dmax, i, 64));
         }
+        if (lane == 0) { range[wave] = dmin; range[AT_WAVES + wave] = dmax; }
+        for (int i = threadIdx.x; i < AT_MAP / 32; i += 64 * AT_WAVES) active[i] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < AT_WAVES; ++w) {
+            dmin = min(dmin, range[w]);
+            dmax = max(dmax, range[AT_WAVES + w]);
+        }
+#pragma unroll 8
+        for (int t = wave; t < min(end, AT_MAP); t += AT_WAVES) {
+            const int j = t * BK + lane % BK;
+            const int d = s.doc[min(j, s.n - 1)];
+            const bool any = __any((j < s.n) & (d >= dmin) & (d <= dmax));
+            if (lane == 0 && any) atomicOr(&active[t / 32], 1u << (t & 31));
+        }
+        __syncthreads();
     }
+    // the block behind t, `end` where there is none
+    auto behind = [&](int t) {
+        for (;;) {
+            ++t;
+            if (t >= pb && t < lo) t = lo;
+            if (t >= end) return end;
+            if (!s.doc || t >= AT_MAP) return t;
+            const uint32_t* const active = (const uint32_t*)(smem + 4 * S::TILE);
+            const uint32_t left = (uint32_t)__builtin_amdgcn_readfirstlane((int)active[t / 32]) >> (t & 31);
+            if (left & 1) return t;
+            t = left ? t + __builtin_ctz(left) - 1 : (t | 31);
+        }
+    };
+
     const char* const kh = a.k + (int64_t)h * a.head_bytes;
     const char* const vh = a.v + (int64_t)h * a.head_bytes;
     const int slot_mask = (1 << a.page_shift) - 1;
-    auto first_of = [&](int t) { return (t < pb ? t : lo + t - pb) * BK; };
 
-    // ---- copies of a block: thread's piece i is piece (i 4 + wave) 64 + lane of the tile
-    constexpr int KSW = (CH < 16 ? CH : 16) - 1;                             // keys: piece ^ (key & KSW)
-    constexpr int VSW = BF ? (CH < 16 ? 3 : 7) : 0;                          // values: piece ^ (key & VSW) * 2
-    int page[S::COPIES];
-    auto key_of = [&](int i) { return ((i * AT_WAVES + wave) * 64 + lane) / CH; };
-    auto find_pages = [&](int t) {
-#pragma unroll
-        for (int i = 0; i < S::COPIES; ++i) {
-            const int j = min(first_of(t) + key_of(i), s.n - 1);
-            const int p = s.table[j >> a.page_shift];
-            page[i] = (unsigned)p < (unsigned)a.pages ? p : 0;               // (read, and not used)
-        }
+    // ---- copies.  Lane l looks up where key l of a block lies; a lane that copies a piece of a key's row has it from there.
+    // Pieces lie in LDS at piece ^ (key & KSW) of a row of keys, piece ^ (key & VSW) * 2 of values.
+    constexpr int KSW = (CH < 16 ? CH : 16) - 1, VSW = BF ? (CH < 16 ? 3 : 7) : 0;
+    struct Found { int page, pos, doc; };
+    auto look = [&](int t) {                           // (kept as loaded: nothing here waits)
+        Found f;
+        const int j = t * BK + lane % BK, in = min(j, s.n - 1);
+        f.page = s.table[in >> a.page_shift];
+        f.pos = s.pos ? s.pos[in] : j;
+        f.doc = s.doc ? s.doc[in] : 0;
+        if (j >= s.n) f.doc = -1;
+        return f;
     };
-    auto copy_block = [&](int t, int buf) {
+    struct Key { int64_t at; int p, doc; };            // doc: -1 where the key does not exist
+    auto settle = [&](const Found& f, int t) {
+        Key k;
+        const int j = min(t * BK + lane % BK, s.n - 1);
+        const bool there = (unsigned)f.page < (unsigned)a.pages;
+        k.at = (int64_t)(there ? f.page : 0) * a.page_bytes + (int64_t)(j & slot_mask) * a.slot_bytes;   // (read, and not used)
+        k.p = max(f.pos, 0);
+        k.doc = there ? max(f.doc, -1) : -1;
+        return k;
+    };
+    auto copy = [&](int64_t at, int buf) {
 #pragma unroll
         for (int i = 0; i < S::COPIES; ++i) {
-            const int key = key_of(i), piece = ((i * AT_WAVES + wave) * 64 + lane) % CH;
-            const int j = min(first_of(t) + key, s.n - 1);
-            const int64_t at = (int64_t)page[i] * a.page_bytes + (int64_t)(j & slot_mask) * a.slot_bytes;
+            const int key = ((i * AT_WAVES + wave) * 64 + lane) / CH, piece = lane % CH;
+            const int64_t off = ((int64_t)__shfl((int)(at >> 32), key, 64) << 32) | (uint32_t)__shfl((int)at, key, 64);
             const int pk = piece ^ (key & KSW), pv = piece ^ (key & VSW) * 2;
             const int dst = buf * S::TILE + (i * AT_WAVES + wave) * 1024;
             if (EXACT || pk * 16 < a.d * ES)
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(kh + at + pk * 16),
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(kh + off + pk * 16),
                                                  (__attribute__((address_space(3))) void*)(ks + dst), 16, 0, 0);
             if (EXACT || pv * 16 < a.d * ES)
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(vh + at + pv * 16),
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(vh + off + pv * 16),
                                                  (__attribute__((address_space(3))) void*)(vs + dst), 16, 0, 0);
         }
     };
-    // position and document of the block's keys, by the first BK threads
-    // (looked up in front of the copies that are issued after it, and waited for behind the block's products)
-    int key_page = 0, key_pos = 0, key_doc = 0;
-    auto find_key = [&](int t) {
-        if (tid < BK) {
-            const int j = first_of(t) + tid, in = min(j, s.n - 1);
-            key_page = j < s.n ? s.table[in >> a.page_shift] : -1;
-            key_pos = s.pos ? s.pos[in] : j;
-            key_doc = s.doc ? s.doc[in] : 0;
-        }
-    };
-    auto put_key = [&](int buf) {
-        if (tid < BK) {
-            const bool there = (unsigned)key_page < (unsigned)a.pages;
-            info[buf * INFO + tid] = max(key_pos, 0);
-            info[buf * INFO + BK + tid] = there ? max(key_doc, -1) : -1;
-            const bool gone = __any(!there);
-            if (tid == 0) info[buf * INFO + 2 * BK] = gone;
-        }
-    };
-
     if constexpr (!EXACT) {                            // columns that no copy fills count as zero
-        for (int i = tid; i < 2 * BK * CH; i += 64 * AT_WAVES) {
+        for (int i = threadIdx.x; i < 2 * BK * CH; i += 64 * AT_WAVES) {
             const int key = i / CH % BK, piece = i % CH;
             if ((piece ^ (key & KSW)) * 16 >= a.d * ES) *(v4u*)(ks + i * 16) = v4u{0, 0, 0, 0};
         }
     }
+
     v16f o[DT];
 #pragma unroll
-    for (int t = 0; t < DT; ++t)
+    for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
+        for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
     float m = -INFINITY, l = 0.f, lr = 0.f;            // l: sum of the weights, lr: as the second product takes them
+    // Weights enter the second product rounded to bf16, whose errors (2^-9 of a weight in the mean) average out over
+    // many keys.  Where a row has seen fewer than FEW (in a lane's half), what the rounding lost goes in as well: the first
+    // tokens of a prompt or a document, at no cost to the others.
+    constexpr int FEW = 64;
+    int had = 0;
 
-    if (blocks > 0) {
-        find_pages(0);
-        find_key(0);
-        copy_block(0, 0);
-        put_key(0);
-        if (blocks > 1) find_pages(1);
-    }
     // where lane (i = lane & 15 of each 16) of a transposing read takes its 8 bytes: key 4 hf + (i >> 2), columns
     // 16 (lane >> 4 & 1) + 4 (i & 3) of a column tile
     const int tk = 4 * hf + ((lane & 15) >> 2);
     int vofs[DT];
 #pragma unroll
-    for (int t = 0; t < DT; ++t) {
-        if constexpr (BF) {
-            const int piece = (4 * t + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (tk & VSW) * 2;
-            vofs[t] = tk * ROWB + piece * 16 + (lane & 1) * 8;
-        } else {
-            vofs[t] = 4 * hf * ROWB + (32 * t + l32) * 4;
-        }
+    for (int d = 0; d < DT; ++d) {
+        if constexpr (BF) vofs[d] = tk * ROWB + ((4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (tk & VSW) * 2) * 16 + (lane & 1) * 8;
+        else vofs[d] = 4 * hf * ROWB + (32 * d + l32) * 4;
     }
 
-    // Weights enter the second product rounded to bf16, whose errors (2^-9 of a weight in the mean) average out over
-    // many keys.  Where a row has seen fewer than FEW, both terms of the weights go in (16 bits): the first tokens of
-    // a prompt or a document, at no cost to the others.
-    constexpr int FEW = 64;
-    int had = 0;                                       // keys that the lane's half of the row has seen
-    for (int t = 0; t < blocks; ++t) {
-        const int buf = t & 1, j0 = first_of(t);
-        __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0): this wavefront's copies of the block are there
-        bwla_lds_barrier();                            // ... everyone's are, and the other buffer is free
-        if (t + 1 < blocks) {
-            find_key(t + 1);
-            copy_block(t + 1, buf ^ 1);
-            if (t + 2 < blocks) find_pages(t + 2);
-        }
-        const int* const inf = info + buf * INFO;
-        const bool skip = j0 > w_last && j0 >= s.prefix;    // (scalars)
-        if (!skip) {
-            // ---- S^T
-            v16f p[KT];
+    typedef v16f Scores[KT];
+    typedef v4u Packed[BF ? 2 * KT : 4 * KT];          // weights as operands: 16 keys each; fp32: as they are
+    auto products = [&](const char* kb, Scores& out) {
 #pragma unroll
-            for (int k = 0; k < KT; ++k) {
+        for (int k = 0; k < KT; ++k) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) p[k][r] = 0.f;
-                const char* src = ks + buf * S::TILE + (k * 32 + l32) * ROWB;
+            for (int r = 0; r < 16; ++r) out[k][r] = 0.f;
+            const char* src = kb + (k * 32 + l32) * ROWB;
 #pragma unroll
-                for (int c = 0; c < CH / 2; ++c) {
-                    const v4u kf = *(const v4u*)(src + ((2 * c + hf) ^ (l32 & KSW)) * 16);
-                    if constexpr (BF) {
-                        p[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, kf),
-                                                                       __builtin_bit_cast(v8bf, qf[c]), p[k], 0, 0, 0);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            p[k] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(qf[c][e]),
-                                                                        p[k], 0, 0, 0);
-                    }
-                }
-            }
-            // ---- scores
-            float c1 = a.c1;
-            if constexpr (GENERAL) {
-                c1 = 1.f;
-                if (a.capped != 0.f) {
-                    const float C = a.capped, c3 = a.c2 * (2.f * ATT_LOG2E);
-#pragma unroll
-                    for (int k = 0; k < KT; ++k)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            if constexpr (BF) {        // (an error of 1e-7 C: weights are rounded to 8 bits)
-                                const float e = __builtin_amdgcn_exp2f(p[k][r] * c3);
-                                p[k][r] = fmaf(-2.f * C, __builtin_amdgcn_rcpf(1.f + e), C);
-                            } else {
-                                p[k][r] = C * att_tanh(p[k][r] * a.c2);
-                            }
-                        }
+            for (int c = 0; c < CS; ++c) {
+                const v4u kf = *(const v4u*)(src + ((2 * c + hf) ^ (l32 & KSW)) * 16);
+                if constexpr (BF) {
+                    out[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, kf), __builtin_bit_cast(v8bf, qf[c]), out[k], 0, 0, 0);
                 } else {
 #pragma unroll
-                    for (int k = 0; k < KT; ++k)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) p[k][r] *= a.c1;
-                }
-                if (a.slopes) {
-                    if (s.pos) {
-#pragma unroll
-                        for (int k = 0; k < KT; ++k)
-#pragma unroll
-                            for (int r = 0; r < 16; ++r)
-                                p[k][r] -= slope * fabsf((float)(me.p - inf[k * 32 + (r & 3) + 8 * (r >> 2) + 4 * hf]));
-                    } else {
-                        const float away = (float)(me.p - j0 - 4 * hf);
-#pragma unroll
-                        for (int k = 0; k < KT; ++k)
-#pragma unroll
-                            for (int r = 0; r < 16; ++r)
-                                p[k][r] = fmaf(-slope, fabsf(away - (float)(k * 32 + (r & 3) + 8 * (r >> 2))), p[k][r]);
-                    }
+                    for (int e = 0; e < 4; ++e)
+                        out[k] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(qf[c][e]), out[k], 0, 0, 0);
                 }
             }
-            // ---- mask: blocks that every row sees whole have none
-            const bool whole = att_uniform(!inf[2 * BK] && !s.doc && w_first >= 0 &&
-                                           (j0 + BK <= s.prefix || (j0 + BK - 1 <= w_first &&
-                                                                    (a.window == INT32_MAX || (!s.pos && j0 > w_last - a.window)))));
-            uint32_t used[KT];                         // bit r: some row of the wavefront sees the lane's key r
-            bool fine = false;                         // weights as two bf16 terms: see below
-            if (whole) {
-                had += BK;
-            } else {
-#pragma unroll
-                for (int k = 0; k < KT; ++k) {
-                    uint32_t mine = 0;                 // bit r: the row sees the lane's key r
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        const v4i kp = *(const v4i*)(inf + k * 32 + 8 * g + 4 * hf), kd = *(const v4i*)(inf + BK + k * 32 + 8 * g + 4 * hf);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const bool seen = att_sees(me, s.prefix, a.window, j0 + k * 32 + 8 * g + 4 * hf + e, kp[e], kd[e]);
-                            p[k][4 * g + e] = seen ? p[k][4 * g + e] : -INFINITY;
-                            mine |= seen ? 1u << (4 * g + e) : 0u;
-                        }
-                    }
-                    had += __popc(mine);
-#pragma unroll
-                    for (int o = 1; o < 32; o <<= 1) mine |= __shfl_xor(mine, o, 64);
-                    used[k] = mine;
-                }
-                fine = BF && att_uniform(__any(live & (had < FEW)));
-            }
-            // ---- running maximum and sum
-            float top = -INFINITY;
-#pragma unroll
-            for (int k = 0; k < KT; ++k)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) top = fmaxf(top, p[k][r]);
-            top = half_max(top) * c1;
-            // the maximum moves on only when it is off by 2^8, which the fp32 sums and products hold as well
-            if (__any(top > m + 8.f)) {
-                const float now = fmaxf(m, top);
-                const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
-                l *= f;
-                if constexpr (BF) lr *= f;
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o[d][r] *= f;
-                m = now;
-            }
-            const float base = m == -INFINITY ? 0.f : m;
+        }
+    };
+    // cap and bias (without either, scores stay products until their weights are taken)
+    auto transform = [&](Scores& sc, int j0, int kp) {
+        if (a.capped != 0.f) {
+            const float C = a.capped, c3 = a.c2 * (2.f * ATT_LOG2E);
 #pragma unroll
             for (int k = 0; k < KT; ++k)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    p[k][r] = __builtin_amdgcn_exp2f(fmaf(p[k][r], c1, -base));
-                    l += p[k][r];
+                    if constexpr (BF)                  // (an error of 1e-7 of the cap: weights are rounded to 8 bits)
+                        sc[k][r] = fmaf(-2.f * C, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(sc[k][r] * c3)), C);
+                    else
+                        sc[k][r] = C * att_tanh(sc[k][r] * a.c2);
                 }
-            // ---- O^T += V^T P^T; values of keys that no row sees stay out (they may be anything)
-            const char* const vb = vs + buf * S::TILE;
-            auto products = [&](auto masked) {
+        } else {
 #pragma unroll
-                for (int k = 0; k < KT; ++k) {
-                    if constexpr (BF) {
+            for (int k = 0; k < KT; ++k)
 #pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            v4u pf, pl;
+                for (int r = 0; r < 16; ++r) sc[k][r] *= a.c1;
+        }
+        if (a.slopes && s.pos) {
+#pragma unroll
+            for (int k = 0; k < KT; ++k)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    sc[k][r] = fmaf(-slope, fabsf((float)(me.p - __shfl(kp, k * 32 + (r & 3) + 8 * (r >> 2) + 4 * hf, 64))), sc[k][r]);
+        } else if (a.slopes) {
+            const float away = (float)(me.p - j0 - 4 * hf);
+#pragma unroll
+            for (int k = 0; k < KT; ++k)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    sc[k][r] = fmaf(-slope, fabsf(away - (float)(k * 32 + (r & 3) + 8 * (r >> 2))), sc[k][r]);
+        }
+    };
+    // weights of a block's scores, and their sums; LOW: instead, what the weights lose when rounded
+    auto weigh = [&](const Scores& sc, Packed& out, auto low) {
+        const float c1 = GENERAL ? 1.f : a.c1, base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int k = 0; k < KT; ++k)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                float w[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    w[e] = __builtin_amdgcn_exp2f(fmaf(sc[k][8 * u + e], c1, -base));
+                    if constexpr (!decltype(low)::value) l += w[e];
+                }
+                if constexpr (BF) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        uint32_t p = att_pack_bf16(w[2 * e], w[2 * e + 1]);
+                        if constexpr (decltype(low)::value)
+                            p = att_pack_bf16(w[2 * e] - __uint_as_float(p << 16), w[2 * e + 1] - __uint_as_float(p & 0xffff0000u));
+                        out[2 * k + u][e] = p;
+                        lr = att_add_bf16(p, lr);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) out[4 * k + 2 * u + e / 4][e % 4] = __float_as_uint(w[e]);
+                }
+            }
+    };
+    // O^T += V^T P^T; masked: values of keys that no row sees stay out (they may be anything)
+    auto values = [&](const char* vb, const Packed& p, auto masked, uint32_t used) {
+#pragma unroll
+        for (int k = 0; k < KT; ++k) {
+            if constexpr (BF) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+                        const char* at = vb + vofs[d] + (k * 32 + 16 * u) * ROWB;
+                        const v2u x0 = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)at));
+                        const v2u x1 = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(at + 8 * ROWB)));
+                        v4u x = {x0[0], x0[1], x1[0], x1[1]};
+                        if constexpr (decltype(masked)::value) {
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
-                                const float w0 = p[k][8 * u + 2 * e], w1 = p[k][8 * u + 2 * e + 1];
-                                pf[e] = att_pack_bf16(w0, w1);
-                                lr = att_add_bf16(pf[e], lr);
-                                if constexpr (decltype(masked)::value) {
-                                    if (fine) {
-                                        pl[e] = att_pack_bf16(w0 - bwla_bf16_to_f32((uint16_t)pf[e]), w1 - bwla_bf16_to_f32((uint16_t)(pf[e] >> 16)));
-                                        lr = att_add_bf16(pl[e], lr);
-                                    }
-                                }
-                            }
-#pragma unroll
-                            for (int d = 0; d < DT; ++d) {
-                                typedef uint32_t v2u __attribute__((ext_vector_type(2)));
-                                const char* src = vb + vofs[d] + (k * 32 + 16 * u) * ROWB;
-                                const v2u x0 = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                    (__attribute__((address_space(3))) v4s*)src));
-                                const v2u x1 = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                    (__attribute__((address_space(3))) v4s*)(src + 8 * ROWB)));
-                                v4u x = {x0[0], x0[1], x1[0], x1[1]};
-                                if constexpr (decltype(masked)::value) {
-#pragma unroll
-                                    for (int e = 0; e < 4; ++e) {
-                                        const uint32_t w = used[k] >> (8 * u + 2 * e);
-                                        x[e] &= ((w & 1) ? 0xffffu : 0u) | ((w & 2) ? 0xffff0000u : 0u);
-                                    }
-                                }
-                                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, x),
-                                                                               __builtin_bit_cast(v8bf, pf), o[d], 0, 0, 0);
-                                if constexpr (decltype(masked)::value) {
-                                    if (fine) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, x),
-                                                                                             __builtin_bit_cast(v8bf, pl), o[d], 0, 0, 0);
-                                }
+                                const uint32_t w = used >> (16 * k + 8 * u + 2 * e);
+                                x[e] &= ((w & 1) ? 0xffffu : 0u) | ((w & 2) ? 0xffff0000u : 0u);
                             }
                         }
-                    } else {
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-#pragma unroll
-                            for (int d = 0; d < DT; ++d) {
-                                float x = *(const float*)(vb + vofs[d] + (k * 32 + (r & 3) + 8 * (r >> 2)) * ROWB);
-                                if constexpr (decltype(masked)::value) x = (used[k] >> r) & 1 ? x : 0.f;
-                                o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p[k][r], o[d], 0, 0, 0);
-                            }
+                        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, x), __builtin_bit_cast(v8bf, p[2 * k + u]), o[d], 0, 0, 0);
                     }
-                }
-            };
-            if (whole) products(std::false_type{});
-            else products(std::true_type{});
+            } else {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        float x = *(const float*)(vb + vofs[d] + (k * 32 + (r & 3) + 8 * (r >> 2)) * ROWB);
+                        if constexpr (decltype(masked)::value) x = (used >> (16 * k + r)) & 1 ? x : 0.f;
+                        o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, __uint_as_float(p[4 * k + r / 4][r % 4]), o[d], 0, 0, 0);
+                    }
+            }
         }
-        if (t + 1 < blocks) put_key(buf ^ 1);
+    };
+    // The maximum moves only when it is off by 2^8, which the fp32 sums and products hold as well; what was summed with the
+    // old one follows.
+    auto raise = [&](const Scores& sc) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < KT; ++k)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, sc[k][r]);
+        top = half_max(top) * (GENERAL ? 1.f : a.c1);
+        if (__builtin_expect(att_uniform(__any(top > m + 8.f)), 0)) {
+            const float now = fmaxf(m, top);
+            const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
+            m = now;
+            l *= f;
+            lr *= f;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[d][r] *= f;
+        }
+    };
+
+    // blocks t, t1, t2, t3 in turn: in work, copied, found, looked up
+    int t = behind(-1), t1 = t < end ? behind(t) : end, t2 = t1 < end ? behind(t1) : end;
+    Key now{0, 0, -1}, next{0, 0, -1};                 // keys of t and t1
+    Found far{0, 0, 0};                                // ... of t2, as loaded
+    if (t < end) {
+        now = settle(look(t), t);
+        copy(now.at, 0);
+        if (t1 < end) next = settle(look(t1), t1);
+        if (t2 < end) far = look(t2);
+    }
+    for (int buf = 0; t < end; buf ^= 1) {
+        const int j0 = t * BK, t3 = t2 < end ? behind(t2) : end;
+        __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0): this wavefront's copies of the block are there
+        bwla_lds_barrier();                            // ... everyone's are, and the other buffer is free
+        if (t1 < end) copy(next.at, buf ^ 1);
+        Key after = next;
+        if (t2 < end) after = settle(far, t2);
+        if (t3 < end) far = look(t3);
+        if (j0 <= w_last || j0 < s.prefix) {
+            const char* const kb = ks + buf * S::TILE;
+            const char* const vb = vs + buf * S::TILE;
+            // where all keys exist, in the one document of all rows and in reach of their windows, a row sees those up to its
+            // index, or all of the prefix; whole: every row of the wavefront sees every key
+            const bool plain = att_uniform(__all(s.doc ? now.doc == one_doc : now.doc >= 0) && w_first >= 0 &&
+                                           (a.window == INT32_MAX || (!s.pos && j0 > w_last - a.window) || j0 + BK <= s.prefix));
+            const bool whole = plain && (j0 + BK - 1 <= w_first || j0 + BK <= s.prefix);
+            Scores sc;
+            Packed p;
+            uint32_t used = 0;                         // bit i: some row of the wavefront sees the lane's key i
+            bool fine = false;
+            products(kb, sc);
+            if constexpr (GENERAL) transform(sc, j0, now.p);
+            if (!whole) {
+                if (plain) {
+                    const int most = max(me.i, live ? s.prefix - 1 : -1) - j0 - 4 * hf;
+#pragma unroll
+                    for (int k = 0; k < KT; ++k)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) sc[k][r] = k * 32 + (r & 3) + 8 * (r >> 2) <= most ? sc[k][r] : -INFINITY;
+                    had += min(max((most & ~3) / 2 + 4, 0), BK / 2);           // (four too many at most)
+                } else {
+                    uint32_t bits = 0;                 // bit i: the row sees the lane's key i
+#pragma unroll 8
+                    for (int i = 0; i < 16 * KT; ++i) {
+                        const int at = (i >> 4) * 32 + (i & 3) + 8 * ((i >> 2) & 3) + 4 * hf;
+                        const int kp = __shfl(now.p, at, 64), kd = __shfl(now.doc, at, 64);
+                        bits |= att_sees(me, s.prefix, a.window, j0 + at, kp, kd) ? 1u << i : 0u;
+                    }
+#pragma unroll
+                    for (int k = 0; k < KT; ++k)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) sc[k][r] = (bits >> (16 * k + r)) & 1 ? sc[k][r] : -INFINITY;
+                    had += __popc(bits);
+                    used = bits;
+#pragma unroll
+                    for (int i = 1; i < 32; i <<= 1) used |= __shfl_xor(used, i, 64);
+                }
+                fine = BF && att_uniform(__any(live & (had < FEW)));
+            } else {
+                had += BK / 2;
+            }
+            raise(sc);
+            weigh(sc, p, std::false_type{});
+            if (plain) values(vb, p, std::false_type{}, 0);
+            else values(vb, p, std::true_type{}, used);
+            if constexpr (BF) {
+                if (__builtin_expect(fine, 0)) {
+                    weigh(sc, p, std::true_type{});
+                    values(vb, p, std::true_type{}, plain ? ~0u : used);
+                }
+            }
+        }
+        now = next;
+        next = after;
+        t = t1;
+        t1 = t2;
+        t2 = t3;
     }
 
     l = half_sum(l);
@@ -405,13 +455,13 @@ template <bool BF, int DP>
 hipError_t at_launch(const AttArgs& a, hipStream_t st) {
     const int tiles = (int)(((int64_t)a.max_new * a.group + AT_ROWS - 1) / AT_ROWS);
     const int units = a.seqs * a.hkv;
-    const int64_t grid = (int64_t)tiles * (units % 8 == 0 || units >= 32 ? (units + 7) / 8 * 8 : units);
+    const int order = att_order_of(tiles, units, DP == 256 ? 1 : 2);
     constexpr int lds = AtShape<BF, DP>::LDS;
     const bool general = a.capped != 0.f || a.slopes, exact = a.d == DP;
     auto go = [&](auto kernel) {
         const hipError_t e = bwla_ensure_lds((const void*)kernel, lds);
         if (e != hipSuccess) return e;
-        kernel<<<dim3((unsigned)grid), 64 * AT_WAVES, lds, st>>>(a, tiles, units);
+        kernel<<<dim3((unsigned)((int64_t)tiles * units)), 64 * AT_WAVES, lds, st>>>(a, tiles, units, order);
         return hipGetLastError();
     };
     if (exact) return general ? go(att_tile_kernel<BF, DP, true, true>) : go(att_tile_kernel<BF, DP, true, false>);
