@@ -159,6 +159,15 @@ __device__ __forceinline__ float att_score(const AttArgs& a, float prod) {
     return a.capped != 0.f ? a.capped * att_tanh(prod * a.c2) : prod * a.c1;
 }
 
+// 16 bytes a lane from memory to LDS: lane i's go to dst + 16 i (dst is uniform).  In assembly, since the compiler lets the
+// transposing LDS reads wait for every such copy on the way, also those to other buffers (vmcnt(0) in front of each block's second
+// product: 954 us for a prompt of 8192 with 32 heads).  The caller waits (vmcnt) before the barrier behind which the copy is read;
+// nothing is returned in registers.
+__device__ __forceinline__ void att_copy16(const char* src, const char* dst) {
+    const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)dst);
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(to) : "memory", "m0");
+}
+
 __device__ __forceinline__ uint32_t att_pack_bf16(float lo, float hi) {
     typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
     v2bf r;

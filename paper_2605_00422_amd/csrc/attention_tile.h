@@ -51,7 +51,7 @@ struct AtShape {
     static constexpr int CH = ROWB / 16;               // 16-byte pieces of a row
     static constexpr int TILE = BK * ROWB;             // bytes of a block of keys, and of values
     static constexpr int COPIES = BK * CH / (64 * AT_WAVES);
-    static constexpr int LDS = 4 * TILE + AT_MAP / 8 + 2 * AT_WAVES * 4;       // two blocks of each, the map of active blocks
+    static constexpr int LDS = 4 * TILE + AT_MAP / 8 + 2 * AT_WAVES * 4 + 8 * AT_WAVES;    // two blocks of each, a map of blocks, words of the wavefronts
 };
 
 // BF: bf16 (else fp32); DP: columns, 64, 128 or 256; EXACT: d == DP; GENERAL: a cap or a bias
@@ -97,33 +97,39 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
     int lo = s.pos || a.window == INT32_MAX ? 0 : max(g_first - a.window + 1, 0) / BK;
     if (lo < pb) lo = pb;
     const int end = max((g_last + BK) / BK, pb);
-    // documents: the range of the workgroup's, and the wavefront's if its rows are all in one (else -3)
+    // rows that see nothing whatever the block: what they gather on the way is dropped at the end
+    const bool blind = me.doc < 0;
+    // documents: the one of all the workgroup's rows (else -3), and the blocks that may hold keys of theirs
     int one_doc = 0;
     if (s.doc) {
         uint32_t* const active = (uint32_t*)(smem + 4 * S::TILE);              // a bit for each block that may matter
         int* const range = (int*)(active + AT_MAP / 32);
-        int dmin = live && me.doc >= 0 ? me.doc : INT32_MAX, dmax = live ? me.doc : -2;
-        const int first_doc = __builtin_amdgcn_readfirstlane(me.doc);
-        one_doc = att_uniform(__all(!live | (me.doc == first_doc)) && first_doc >= 0) ? first_doc : -3;
+        int dmin = blind ? INT32_MAX : me.doc, dmax = me.doc;
 #pragma unroll
         for (int i = 1; i < 64; i <<= 1) {
             dmin = min(dmin, __shfl_xor(dmin, i, 64));
             dmax = max(dmax, __shfl_xor(dmax, i, 64));
         }
         if (lane == 0) { range[wave] = dmin; range[AT_WAVES + wave] = dmax; }
-        for (int i = threadIdx.x; i < AT_MAP / 32; i += 64 * AT_WAVES) active[i] = 0;
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < AT_WAVES; ++w) {
             dmin = min(dmin, range[w]);
             dmax = max(dmax, range[AT_WAVES + w]);
         }
-#pragma unroll 8
-        for (int t = wave; t < min(end, AT_MAP); t += AT_WAVES) {
-            const int j = t * BK + lane % BK;
-            const int d = s.doc[min(j, s.n - 1)];
-            const bool any = __any((j < s.n) & (d >= dmin) & (d <= dmax));
-            if (lane == 0 && any) atomicOr(&active[t / 32], 1u << (t & 31));
+        one_doc = __builtin_amdgcn_readfirstlane(dmin == dmax ? dmin : -3);
+        // a wavefront looks at 32 blocks, whose word it writes, eight loads at a time on the way
+        for (int w = wave; w < (min(end, AT_MAP) + 31) / 32; w += AT_WAVES) {
+            uint32_t word = 0;
+#pragma unroll
+            for (int i0 = 0; i0 < 32; i0 += 8) {
+                int d[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[i] = s.doc[min((w * 32 + i0 + i) * BK + lane % BK, s.n - 1)];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) word |= __any((d[i] >= dmin) & (d[i] <= dmax)) ? 1u << (i0 + i) : 0u;
+            }
+            if (lane == 0) active[w] = word;
         }
         __syncthreads();
     }
@@ -155,32 +161,32 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
         f.page = s.table[in >> a.page_shift];
         f.pos = s.pos ? s.pos[in] : j;
         f.doc = s.doc ? s.doc[in] : 0;
-        if (j >= s.n) f.doc = -1;
         return f;
     };
     struct Key { int64_t at; int p, doc; };            // doc: -1 where the key does not exist
     auto settle = [&](const Found& f, int t) {
         Key k;
         const int j = min(t * BK + lane % BK, s.n - 1);
-        const bool there = (unsigned)f.page < (unsigned)a.pages;
+        const bool there = (unsigned)f.page < (unsigned)a.pages && t * BK + lane % BK < s.n;
         k.at = (int64_t)(there ? f.page : 0) * a.page_bytes + (int64_t)(j & slot_mask) * a.slot_bytes;   // (read, and not used)
         k.p = max(f.pos, 0);
         k.doc = there ? max(f.doc, -1) : -1;
         return k;
     };
+    // (an instruction of a wavefront copies the rows of 64 / CH keys, or part of one; those of instruction i + 1 are STEP keys on,
+    // which for most shapes leaves the order of their pieces)
+    constexpr int PER = 64 / CH, STEP = AT_WAVES * 64 / CH;
+    static_assert(CH <= 64, "a row is one instruction's at most");
+    const int key0 = wave * PER + lane / CH, piece = lane % CH;
     auto copy = [&](int64_t at, int buf) {
 #pragma unroll
         for (int i = 0; i < S::COPIES; ++i) {
-            const int key = ((i * AT_WAVES + wave) * 64 + lane) / CH, piece = lane % CH;
+            const int key = key0 + i * STEP;
             const int64_t off = ((int64_t)__shfl((int)(at >> 32), key, 64) << 32) | (uint32_t)__shfl((int)at, key, 64);
-            const int pk = piece ^ (key & KSW), pv = piece ^ (key & VSW) * 2;
+            const int pk = piece ^ ((STEP % (KSW + 1) == 0 ? key0 : key) & KSW), pv = piece ^ ((STEP % (VSW + 1) == 0 ? key0 : key) & VSW) * 2;
             const int dst = buf * S::TILE + (i * AT_WAVES + wave) * 1024;
-            if (EXACT || pk * 16 < a.d * ES)
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(kh + off + pk * 16),
-                                                 (__attribute__((address_space(3))) void*)(ks + dst), 16, 0, 0);
-            if (EXACT || pv * 16 < a.d * ES)
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(vh + off + pv * 16),
-                                                 (__attribute__((address_space(3))) void*)(vs + dst), 16, 0, 0);
+            if (EXACT || pk * 16 < a.d * ES) att_copy16(kh + pk * 16 + off, ks + dst);
+            if (EXACT || pv * 16 < a.d * ES) att_copy16(vh + pv * 16 + off, vs + dst);
         }
     };
     if constexpr (!EXACT) {                            // columns that no copy fills count as zero
@@ -219,6 +225,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
         for (int k = 0; k < KT; ++k) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) out[k][r] = 0.f;
+            if (k > 0) __builtin_amdgcn_sched_barrier(0);                      // (one tile's operands in registers at a time)
             const char* src = kb + (k * 32 + l32) * ROWB;
 #pragma unroll
             for (int c = 0; c < CS; ++c) {
@@ -267,7 +274,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
                     sc[k][r] = fmaf(-slope, fabsf(away - (float)(k * 32 + (r & 3) + 8 * (r >> 2))), sc[k][r]);
         }
     };
-    // weights of a block's scores, and their sums; LOW: instead, what the weights lose when rounded
+    // weights of a block's scores, and their sums; low: what the weights lose when rounded
     auto weigh = [&](const Scores& sc, Packed& out, auto low) {
         const float c1 = GENERAL ? 1.f : a.c1, base = m == -INFINITY ? 0.f : m;
 #pragma unroll
@@ -295,8 +302,8 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
                 }
             }
     };
-    // O^T += V^T P^T; masked: values of keys that no row sees stay out (they may be anything)
-    auto values = [&](const char* vb, const Packed& p, auto masked, uint32_t used) {
+    // O^T += V^T P^T
+    auto values = [&](const char* vb, const Packed& p) {
 #pragma unroll
         for (int k = 0; k < KT; ++k) {
             if constexpr (BF) {
@@ -308,14 +315,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
                         const char* at = vb + vofs[d] + (k * 32 + 16 * u) * ROWB;
                         const v2u x0 = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)at));
                         const v2u x1 = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(at + 8 * ROWB)));
-                        v4u x = {x0[0], x0[1], x1[0], x1[1]};
-                        if constexpr (decltype(masked)::value) {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const uint32_t w = used >> (16 * k + 8 * u + 2 * e);
-                                x[e] &= ((w & 1) ? 0xffffu : 0u) | ((w & 2) ? 0xffff0000u : 0u);
-                            }
-                        }
+                        const v4u x = {x0[0], x0[1], x1[0], x1[1]};
                         o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, x), __builtin_bit_cast(v8bf, p[2 * k + u]), o[d], 0, 0, 0);
                     }
             } else {
@@ -323,8 +323,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
                 for (int r = 0; r < 16; ++r)
 #pragma unroll
                     for (int d = 0; d < DT; ++d) {
-                        float x = *(const float*)(vb + vofs[d] + (k * 32 + (r & 3) + 8 * (r >> 2)) * ROWB);
-                        if constexpr (decltype(masked)::value) x = (used >> (16 * k + r)) & 1 ? x : 0.f;
+                        const float x = *(const float*)(vb + vofs[d] + (k * 32 + (r & 3) + 8 * (r >> 2)) * ROWB);
                         o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, __uint_as_float(p[4 * k + r / 4][r % 4]), o[d], 0, 0, 0);
                     }
             }
@@ -357,72 +356,85 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
     Key now{0, 0, -1}, next{0, 0, -1};                 // keys of t and t1
     Found far{0, 0, 0};                                // ... of t2, as loaded
     if (t < end) {
-        now = settle(look(t), t);
+        const Found f0 = look(t), f1 = look(min(t1, end - 1));
+        far = look(min(t2, end - 1));
+        now = settle(f0, t);
         copy(now.at, 0);
-        if (t1 < end) next = settle(look(t1), t1);
-        if (t2 < end) far = look(t2);
+        next = settle(f1, min(t1, end - 1));
     }
+    constexpr uint64_t ALL = BK == 64 ? ~0ull : (1ull << BK) - 1;
     for (int buf = 0; t < end; buf ^= 1) {
         const int j0 = t * BK, t3 = t2 < end ? behind(t2) : end;
+        const char* const kb = ks + buf * S::TILE;
+        const char* const vb = vs + buf * S::TILE;
         __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0): this wavefront's copies of the block are there
         bwla_lds_barrier();                            // ... everyone's are, and the other buffer is free
-        if (t1 < end) copy(next.at, buf ^ 1);
         Key after = next;
         if (t2 < end) after = settle(far, t2);
         if (t3 < end) far = look(t3);
-        if (j0 <= w_last || j0 < s.prefix) {
-            const char* const kb = ks + buf * S::TILE;
-            const char* const vb = vs + buf * S::TILE;
-            // where all keys exist, in the one document of all rows and in reach of their windows, a row sees those up to its
-            // index, or all of the prefix; whole: every row of the wavefront sees every key
-            const bool plain = att_uniform(__all(s.doc ? now.doc == one_doc : now.doc >= 0) && w_first >= 0 &&
-                                           (a.window == INT32_MAX || (!s.pos && j0 > w_last - a.window) || j0 + BK <= s.prefix));
-            const bool whole = plain && (j0 + BK - 1 <= w_first || j0 + BK <= s.prefix);
+        if (t1 < end) copy(next.at, buf ^ 1);
+        // Even: every key exists, is of the one document of the workgroup's rows (where these are told apart) and in reach of
+        // their windows, so that a row sees those up to its index, or all of the prefix.  Else each wavefront works out what
+        // each of its rows sees (a bit for each key), and values of keys that no row of the workgroup sees are cleared: they
+        // may be anything, and a weight of 0 does not make 0 of that.
+        const bool even = att_uniform(__all(s.doc ? now.doc == one_doc : now.doc >= 0) &&
+                                      (a.window == INT32_MAX || (!s.pos && j0 > g_last - a.window) || j0 + BK <= s.prefix));
+        uint64_t ok = ALL, any = ALL;
+        if (__builtin_expect(!even, 0)) {
+            any = 0;
+            for (int r = 0; r < 32; ++r) {
+                const AttRow row{__builtin_amdgcn_readlane(me.i, r), __builtin_amdgcn_readlane(me.p, r), __builtin_amdgcn_readlane(me.doc, r)};
+                const uint64_t bits = __ballot(att_sees(row, s.prefix, a.window, j0 + lane % BK, now.p, now.doc)) & ALL;
+                any |= bits;
+                ok = l32 == r ? bits : ok;
+            }
+            uint64_t* const seen = (uint64_t*)(smem + 4 * S::TILE + AT_MAP / 8 + 2 * AT_WAVES * 4);
+            if (lane == 0) seen[wave] = any;
+            bwla_lds_barrier();
+            const uint64_t all = seen[0] | seen[1] | seen[2] | seen[3];
+            static_assert(AT_WAVES == 4, "one word each");
+            for (int i = lane; i < BK / AT_WAVES * CH; i += 64) {
+                const int key = wave * (BK / AT_WAVES) + i / CH;
+                if (!((all >> key) & 1)) *(v4u*)(vs + buf * S::TILE + key * ROWB + i % CH * 16) = v4u{0, 0, 0, 0};
+            }
+            bwla_lds_barrier();
+        }
+        if (att_uniform(even ? j0 <= w_last || j0 < s.prefix : any != 0)) {
             Scores sc;
             Packed p;
-            uint32_t used = 0;                         // bit i: some row of the wavefront sees the lane's key i
             bool fine = false;
             products(kb, sc);
             if constexpr (GENERAL) transform(sc, j0, now.p);
-            if (!whole) {
-                if (plain) {
-                    const int most = max(me.i, live ? s.prefix - 1 : -1) - j0 - 4 * hf;
+            if (__builtin_expect(even && (j0 + BK - 1 <= w_first || j0 + BK <= s.prefix), 1)) {
+                had += BK / 2;                         // (every row sees every key)
+            } else {
+                if (even) {
+                    const int most = max(me.i, s.prefix - 1) - j0 - 4 * hf;
 #pragma unroll
                     for (int k = 0; k < KT; ++k)
 #pragma unroll
                         for (int r = 0; r < 16; ++r) sc[k][r] = k * 32 + (r & 3) + 8 * (r >> 2) <= most ? sc[k][r] : -INFINITY;
                     had += min(max((most & ~3) / 2 + 4, 0), BK / 2);           // (four too many at most)
                 } else {
-                    uint32_t bits = 0;                 // bit i: the row sees the lane's key i
-#pragma unroll 8
-                    for (int i = 0; i < 16 * KT; ++i) {
-                        const int at = (i >> 4) * 32 + (i & 3) + 8 * ((i >> 2) & 3) + 4 * hf;
-                        const int kp = __shfl(now.p, at, 64), kd = __shfl(now.doc, at, 64);
-                        bits |= att_sees(me, s.prefix, a.window, j0 + at, kp, kd) ? 1u << i : 0u;
+#pragma unroll
+                    for (int k = 0; k < KT; ++k) {
+                        const uint32_t mine = (uint32_t)(ok >> (32 * k)) >> (4 * hf);
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) sc[k][r] = (mine >> ((r & 3) + 8 * (r >> 2))) & 1 ? sc[k][r] : -INFINITY;
+                        had += __popc(mine & 0x0f0f0f0fu);
                     }
-#pragma unroll
-                    for (int k = 0; k < KT; ++k)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) sc[k][r] = (bits >> (16 * k + r)) & 1 ? sc[k][r] : -INFINITY;
-                    had += __popc(bits);
-                    used = bits;
-#pragma unroll
-                    for (int i = 1; i < 32; i <<= 1) used |= __shfl_xor(used, i, 64);
                 }
-                fine = BF && att_uniform(__any(live & (had < FEW)));
-            } else {
-                had += BK / 2;
+                fine = BF && att_uniform(__any(!blind & (had < FEW)));
             }
             raise(sc);
-            weigh(sc, p, std::false_type{});
-            if (plain) values(vb, p, std::false_type{}, 0);
-            else values(vb, p, std::true_type{}, used);
             if constexpr (BF) {
                 if (__builtin_expect(fine, 0)) {
                     weigh(sc, p, std::true_type{});
-                    values(vb, p, std::true_type{}, plain ? ~0u : used);
+                    values(vb, p);
                 }
             }
+            weigh(sc, p, std::false_type{});
+            values(vb, p);
         }
         now = next;
         next = after;
@@ -433,6 +445,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
 
     l = half_sum(l);
     lr = BF ? half_sum(lr) : l;
+    if (blind) l = lr = 0.f;
     if (!live) return;
     const float inv = lr > 0.f ? 1.f / lr : 0.f;
     const int64_t at = ((int64_t)(s.row0 + tok) * a.hq + head);
