@@ -225,7 +225,6 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
         for (int k = 0; k < KT; ++k) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) out[k][r] = 0.f;
-            if (k > 0) __builtin_amdgcn_sched_barrier(0);                      // (one tile's operands in registers at a time)
             const char* src = kb + (k * 32 + l32) * ROWB;
 #pragma unroll
             for (int c = 0; c < CS; ++c) {
@@ -302,31 +301,39 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
                 }
             }
     };
-    // O^T += V^T P^T
-    auto values = [&](const char* vb, const Packed& p) {
+    // O^T += V^T P^T, in two halves for bf16: operands of 32 keys, and their products
+    struct Operands { v4u x[BF ? 2 * DT : 1]; };
+    auto fetch = [&](const char* vb, int k) {
+        Operands f;
+        if constexpr (BF) {
 #pragma unroll
-        for (int k = 0; k < KT; ++k) {
-            if constexpr (BF) {
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
+                for (int d = 0; d < DT; ++d) {
+                    typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+                    const char* at = vb + vofs[d] + (k * 32 + 16 * u) * ROWB;
+                    const v2u x0 = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)at));
+                    const v2u x1 = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(at + 8 * ROWB)));
+                    f.x[u * DT + d] = v4u{x0[0], x0[1], x1[0], x1[1]};
+                }
+        }
+        return f;
+    };
+    auto values = [&](const Operands& f, const char* vb, const Packed& p, int k) {
+        if constexpr (BF) {
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        typedef uint32_t v2u __attribute__((ext_vector_type(2)));
-                        const char* at = vb + vofs[d] + (k * 32 + 16 * u) * ROWB;
-                        const v2u x0 = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)at));
-                        const v2u x1 = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(at + 8 * ROWB)));
-                        const v4u x = {x0[0], x0[1], x1[0], x1[1]};
-                        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, x), __builtin_bit_cast(v8bf, p[2 * k + u]), o[d], 0, 0, 0);
-                    }
-            } else {
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
+                for (int d = 0; d < DT; ++d)
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, f.x[u * DT + d]), __builtin_bit_cast(v8bf, p[2 * k + u]), o[d], 0, 0, 0);
+        } else {
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        const float x = *(const float*)(vb + vofs[d] + (k * 32 + (r & 3) + 8 * (r >> 2)) * ROWB);
-                        o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, __uint_as_float(p[4 * k + r / 4][r % 4]), o[d], 0, 0, 0);
-                    }
-            }
+            for (int r = 0; r < 16; ++r)
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    const float x = *(const float*)(vb + vofs[d] + (k * 32 + (r & 3) + 8 * (r >> 2)) * ROWB);
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, __uint_as_float(p[4 * k + r / 4][r % 4]), o[d], 0, 0, 0);
+                }
         }
     };
     // The maximum moves only when it is off by 2^8, which the fp32 sums and products hold as well; what was summed with the
@@ -362,6 +369,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
         copy(now.at, 0);
         next = settle(f1, min(t1, end - 1));
     }
+    constexpr int AHEAD = 6;                           // operands of the first product read ahead of it
     constexpr uint64_t ALL = BK == 64 ? ~0ull : (1ull << BK) - 1;
     for (int buf = 0; t < end; buf ^= 1) {
         const int j0 = t * BK, t3 = t2 < end ? behind(t2) : end;
@@ -404,6 +412,16 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
             Packed p;
             bool fine = false;
             products(kb, sc);
+            // (the compiler would read each operand right in front of its product and wait: 130 cycles each)
+            if constexpr (BF) {
+                __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+                for (int i = 0; i < KT * CS - AHEAD; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                }
+                __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+            }
             if constexpr (GENERAL) transform(sc, j0, now.p);
             if (__builtin_expect(even && (j0 + BK - 1 <= w_first || j0 + BK <= s.prefix), 1)) {
                 had += BK / 2;                         // (every row sees every key)
@@ -430,11 +448,23 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
             if constexpr (BF) {
                 if (__builtin_expect(fine, 0)) {
                     weigh(sc, p, std::true_type{});
-                    values(vb, p);
+#pragma unroll
+                    for (int k = 0; k < KT; ++k) values(fetch(vb, k), vb, p, k);
                 }
+                // (a half's operands are on their way while the weights are taken, the other's during the first half's products:
+                // left to itself the compiler reads each in front of its product, and waits)
+                const Operands f0 = fetch(vb, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                weigh(sc, p, std::false_type{});
+                const Operands f1 = fetch(vb, 1);
+                __builtin_amdgcn_sched_barrier(0);
+                values(f0, vb, p, 0);
+                values(f1, vb, p, 1);
+            } else {
+                weigh(sc, p, std::false_type{});
+#pragma unroll
+                for (int k = 0; k < KT; ++k) values(Operands{}, vb, p, k);
             }
-            weigh(sc, p, std::false_type{});
-            values(vb, p);
         }
         now = next;
         next = after;
