@@ -6,6 +6,7 @@
 // (C = cap log2 e, c2 = scale / cap), minus slope log2(e) |p - r| with a bias.
 #pragma once
 #include <type_traits>
+#include <utility>
 
 #include "bwla_internal.h"
 
@@ -163,9 +164,17 @@ __device__ __forceinline__ float att_score(const AttArgs& a, float prod) {
 // transposing LDS reads wait for every such copy on the way, also those to other buffers (vmcnt(0) in front of each block's second
 // product: 954 us for a prompt of 8192 with 32 heads).  The caller waits (vmcnt) before the barrier behind which the copy is read;
 // nothing is returned in registers.
-__device__ __forceinline__ void att_copy16(const char* src, const char* dst) {
-    const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)dst);
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(to) : "memory", "m0");
+// dst: att_lds_address of where the first copy goes, ofs: bytes from there
+__device__ __forceinline__ uint32_t att_lds_address(const char* p) {
+    return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p);
+}
+template <int OFS>
+__device__ __forceinline__ void att_copy16(const char* src, uint32_t dst) {
+    asm volatile("s_add_u32 m0, %1, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(dst), "i"(OFS) : "memory", "m0", "scc");
+}
+template <int... I, typename F>
+__device__ __forceinline__ void att_each(std::integer_sequence<int, I...>, F f) {
+    (f(std::integral_constant<int, I>{}), ...);
 }
 
 __device__ __forceinline__ uint32_t att_pack_bf16(float lo, float hi) {

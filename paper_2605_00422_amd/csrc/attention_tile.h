@@ -29,18 +29,26 @@ __device__ __forceinline__ float half_sum(float v) {
 }
 
 // Workgroups are dealt round-robin to the 8 XCDs, units (sequence, key-value head) to workgroups, so that an XCD keeps to
-// some of them, whose keys and values then stay in its own L2.  Later tiles of rows see more keys.  ORDER_DOWN: the longest
-// first, which evens out where there are many workgroups; ORDER_FOLD: where all run at once, the first half of them from the
-// longest down, the second from the shortest up, so that a compute unit gets a long one and a short one.
-enum { ORDER_DOWN = 0, ORDER_FOLD = 1 };
-__device__ __forceinline__ void att_order(int id, int tiles, int units, int order, int& unit, int& tile) {
-    const int k = id / units;
-    unit = id - k * units;
-    const int half = tiles / 2;
-    tile = order == ORDER_FOLD && k >= tiles - half ? k - (tiles - half) : tiles - 1 - k;
+// some units at a time, as few as keep it busy: their rows walk over the same keys and values at about the same time, which
+// its own L2 then has (all units at once: 770 us for a prompt of 8192 with 32 heads, bound by what lies behind the L2).
+// Later tiles of rows see more keys: the longest first, which evens out where there are many workgroups, or, where all run
+// at once, the first half of them from the longest down and the second from the shortest up, so that a compute unit gets a
+// long one and a short one.
+struct AtOrder {
+    int tiles, units, together, fold;
+};
+inline AtOrder at_order_of(int tiles, int units, int per_cu) {
+    const int cus = bwla_device_cus(), each = (per_cu * cus / 8 + tiles - 1) / tiles;
+    AtOrder o{tiles, units, 8 * each < units ? 8 * each : units, 0};
+    o.fold = (int64_t)tiles * units <= (int64_t)per_cu * cus;
+    return o;
 }
-inline int att_order_of(int tiles, int units, int per_cu) {
-    return (int64_t)tiles * units <= (int64_t)per_cu * bwla_device_cus() ? ORDER_FOLD : ORDER_DOWN;
+__device__ __forceinline__ void at_place(int id, const AtOrder& o, int& unit, int& tile) {
+    const int size = o.together * o.tiles, group = id / size, at = id - group * size;
+    const int width = min(o.together, o.units - group * o.together), k = at / width;
+    unit = group * o.together + at - k * width;
+    const int half = o.tiles / 2;
+    tile = o.fold && k >= o.tiles - half ? k - (o.tiles - half) : o.tiles - 1 - k;
 }
 
 template <bool BF, int DP>
@@ -56,7 +64,7 @@ struct AtShape {
 
 // BF: bf16 (else fp32); DP: columns, 64, 128 or 256; EXACT: d == DP; GENERAL: a cap or a bias
 template <bool BF, int DP, bool EXACT, bool GENERAL>
-__global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_kernel(AttArgs a, int tiles, int units, int order) {
+__global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_kernel(AttArgs a, AtOrder order) {
     using S = AtShape<BF, DP>;
     constexpr int ES = S::ES, BK = S::BK, ROWB = S::ROWB, CH = S::CH, KT = BK / 32, DT = DP / 32, CS = CH / 2;
     extern __shared__ __align__(16) char smem[];
@@ -64,8 +72,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
     char* const vs = smem + 2 * S::TILE;
 
     int unit, tile;
-    att_order(blockIdx.x, tiles, units, order, unit, tile);
-    if (unit >= units || tile < 0) return;
+    at_place(blockIdx.x, order, unit, tile);
     const int b = unit / a.hkv, h = unit - b * a.hkv;
     const AttSeq s = att_seq(a, b);
     const int rows = s.fresh * a.group;
@@ -178,16 +185,17 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
     constexpr int PER = 64 / CH, STEP = AT_WAVES * 64 / CH;
     static_assert(CH <= 64, "a row is one instruction's at most");
     const int key0 = wave * PER + lane / CH, piece = lane % CH;
+    const uint32_t lds0 = att_lds_address(ks + wave * 1024);
     auto copy = [&](int64_t at, int buf) {
-#pragma unroll
-        for (int i = 0; i < S::COPIES; ++i) {
+        const uint32_t to = lds0 + buf * S::TILE;
+        att_each(std::make_integer_sequence<int, S::COPIES>{}, [&](auto n) {
+            constexpr int i = decltype(n)::value;
             const int key = key0 + i * STEP;
             const int64_t off = ((int64_t)__shfl((int)(at >> 32), key, 64) << 32) | (uint32_t)__shfl((int)at, key, 64);
             const int pk = piece ^ ((STEP % (KSW + 1) == 0 ? key0 : key) & KSW), pv = piece ^ ((STEP % (VSW + 1) == 0 ? key0 : key) & VSW) * 2;
-            const int dst = buf * S::TILE + (i * AT_WAVES + wave) * 1024;
-            if (EXACT || pk * 16 < a.d * ES) att_copy16(kh + pk * 16 + off, ks + dst);
-            if (EXACT || pv * 16 < a.d * ES) att_copy16(vh + pv * 16 + off, vs + dst);
-        }
+            if (EXACT || pk * 16 < a.d * ES) att_copy16<i * AT_WAVES * 1024>(kh + pk * 16 + off, to);
+            if (EXACT || pv * 16 < a.d * ES) att_copy16<i * AT_WAVES * 1024 + 2 * S::TILE>(vh + pv * 16 + off, to);
+        });
     };
     if constexpr (!EXACT) {                            // columns that no copy fills count as zero
         for (int i = threadIdx.x; i < 2 * BK * CH; i += 64 * AT_WAVES) {
@@ -218,90 +226,76 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
         else vofs[d] = 4 * hf * ROWB + (32 * d + l32) * 4;
     }
 
-    typedef v16f Scores[KT];
-    typedef v4u Packed[BF ? 2 * KT : 4 * KT];          // weights as operands: 16 keys each; fp32: as they are
-    auto products = [&](const char* kb, Scores& out) {
+    // ---- the steps of a tile of 32 keys
+    typedef v4u Packed[BF ? 2 : 4];                    // weights as operands: 16 keys each; fp32: as they are
+    auto products = [&](const char* kb, int k, v16f& sc) {
 #pragma unroll
-        for (int k = 0; k < KT; ++k) {
+        for (int r = 0; r < 16; ++r) sc[r] = 0.f;
+        const char* src = kb + (k * 32 + l32) * ROWB;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) out[k][r] = 0.f;
-            const char* src = kb + (k * 32 + l32) * ROWB;
+        for (int c = 0; c < CS; ++c) {
+            const v4u kf = *(const v4u*)(src + ((2 * c + hf) ^ (l32 & KSW)) * 16);
+            if constexpr (BF) {
+                sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, kf), __builtin_bit_cast(v8bf, qf[c]), sc, 0, 0, 0);
+            } else {
 #pragma unroll
-            for (int c = 0; c < CS; ++c) {
-                const v4u kf = *(const v4u*)(src + ((2 * c + hf) ^ (l32 & KSW)) * 16);
-                if constexpr (BF) {
-                    out[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, kf), __builtin_bit_cast(v8bf, qf[c]), out[k], 0, 0, 0);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        out[k] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(qf[c][e]), out[k], 0, 0, 0);
-                }
+                for (int e = 0; e < 4; ++e)
+                    sc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(qf[c][e]), sc, 0, 0, 0);
             }
         }
     };
-    // cap and bias (without either, scores stay products until their weights are taken)
-    auto transform = [&](Scores& sc, int j0, int kp) {
+    // cap and bias (without either, scores stay products until their weights are taken); j0: the tile's first key
+    auto transform = [&](v16f& sc, int k, int j0, int kp) {
         if (a.capped != 0.f) {
             const float C = a.capped, c3 = a.c2 * (2.f * ATT_LOG2E);
 #pragma unroll
-            for (int k = 0; k < KT; ++k)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    if constexpr (BF)                  // (an error of 1e-7 of the cap: weights are rounded to 8 bits)
-                        sc[k][r] = fmaf(-2.f * C, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(sc[k][r] * c3)), C);
-                    else
-                        sc[k][r] = C * att_tanh(sc[k][r] * a.c2);
-                }
+            for (int r = 0; r < 16; ++r) {
+                if constexpr (BF)                      // (an error of 1e-7 of the cap: weights are rounded to 8 bits)
+                    sc[r] = fmaf(-2.f * C, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(sc[r] * c3)), C);
+                else
+                    sc[r] = C * att_tanh(sc[r] * a.c2);
+            }
         } else {
 #pragma unroll
-            for (int k = 0; k < KT; ++k)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) sc[k][r] *= a.c1;
+            for (int r = 0; r < 16; ++r) sc[r] *= a.c1;
         }
         if (a.slopes && s.pos) {
 #pragma unroll
-            for (int k = 0; k < KT; ++k)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    sc[k][r] = fmaf(-slope, fabsf((float)(me.p - __shfl(kp, k * 32 + (r & 3) + 8 * (r >> 2) + 4 * hf, 64))), sc[k][r]);
+            for (int r = 0; r < 16; ++r)
+                sc[r] = fmaf(-slope, fabsf((float)(me.p - __shfl(kp, k * 32 + (r & 3) + 8 * (r >> 2) + 4 * hf, 64))), sc[r]);
         } else if (a.slopes) {
             const float away = (float)(me.p - j0 - 4 * hf);
 #pragma unroll
-            for (int k = 0; k < KT; ++k)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    sc[k][r] = fmaf(-slope, fabsf(away - (float)(k * 32 + (r & 3) + 8 * (r >> 2))), sc[k][r]);
+            for (int r = 0; r < 16; ++r) sc[r] = fmaf(-slope, fabsf(away - (float)((r & 3) + 8 * (r >> 2))), sc[r]);
         }
     };
-    // weights of a block's scores, and their sums; low: what the weights lose when rounded
-    auto weigh = [&](const Scores& sc, Packed& out, auto low) {
+    // weights of a tile's scores, and their sums; low: what the weights lose when rounded
+    auto weigh = [&](const v16f& sc, Packed& out, auto low) {
         const float c1 = GENERAL ? 1.f : a.c1, base = m == -INFINITY ? 0.f : m;
 #pragma unroll
-        for (int k = 0; k < KT; ++k)
+        for (int u = 0; u < 2; ++u) {
+            float w[8];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                float w[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    w[e] = __builtin_amdgcn_exp2f(fmaf(sc[k][8 * u + e], c1, -base));
-                    if constexpr (!decltype(low)::value) l += w[e];
-                }
-                if constexpr (BF) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        uint32_t p = att_pack_bf16(w[2 * e], w[2 * e + 1]);
-                        if constexpr (decltype(low)::value)
-                            p = att_pack_bf16(w[2 * e] - __uint_as_float(p << 16), w[2 * e + 1] - __uint_as_float(p & 0xffff0000u));
-                        out[2 * k + u][e] = p;
-                        lr = att_add_bf16(p, lr);
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) out[4 * k + 2 * u + e / 4][e % 4] = __float_as_uint(w[e]);
-                }
+            for (int e = 0; e < 8; ++e) {
+                w[e] = __builtin_amdgcn_exp2f(fmaf(sc[8 * u + e], c1, -base));
+                if constexpr (!decltype(low)::value) l += w[e];
             }
+            if constexpr (BF) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    uint32_t p = att_pack_bf16(w[2 * e], w[2 * e + 1]);
+                    if constexpr (decltype(low)::value)
+                        p = att_pack_bf16(w[2 * e] - __uint_as_float(p << 16), w[2 * e + 1] - __uint_as_float(p & 0xffff0000u));
+                    out[u][e] = p;
+                    lr = att_add_bf16(p, lr);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) out[2 * u + e / 4][e % 4] = __float_as_uint(w[e]);
+            }
+        }
     };
-    // O^T += V^T P^T, in two halves for bf16: operands of 32 keys, and their products
+    // O^T += V^T P^T: operands, and their products
     struct Operands { v4u x[BF ? 2 * DT : 1]; };
     auto fetch = [&](const char* vb, int k) {
         Operands f;
@@ -325,27 +319,27 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, f.x[u * DT + d]), __builtin_bit_cast(v8bf, p[2 * k + u]), o[d], 0, 0, 0);
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, f.x[u * DT + d]), __builtin_bit_cast(v8bf, p[u]), o[d], 0, 0, 0);
         } else {
 #pragma unroll
             for (int r = 0; r < 16; ++r)
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
                     const float x = *(const float*)(vb + vofs[d] + (k * 32 + (r & 3) + 8 * (r >> 2)) * ROWB);
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, __uint_as_float(p[4 * k + r / 4][r % 4]), o[d], 0, 0, 0);
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, __uint_as_float(p[r / 4][r % 4]), o[d], 0, 0, 0);
                 }
         }
     };
     // The maximum moves only when it is off by 2^8, which the fp32 sums and products hold as well; what was summed with the
     // old one follows.
-    auto raise = [&](const Scores& sc) {
+    // (first: what has to be added with the old one before)
+    auto raise = [&](const v16f& sc, auto first) {
         float top = -INFINITY;
 #pragma unroll
-        for (int k = 0; k < KT; ++k)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) top = fmaxf(top, sc[k][r]);
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, sc[r]);
         top = half_max(top) * (GENERAL ? 1.f : a.c1);
         if (__builtin_expect(att_uniform(__any(top > m + 8.f)), 0)) {
+            first();
             const float now = fmaxf(m, top);
             const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
             m = now;
@@ -369,7 +363,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
         copy(now.at, 0);
         next = settle(f1, min(t1, end - 1));
     }
-    constexpr int AHEAD = 6;                           // operands of the first product read ahead of it
+    constexpr int AHEAD = CS < 4 ? CS : 4;             // operands of the first product read ahead of it
     constexpr uint64_t ALL = BK == 64 ? ~0ull : (1ull << BK) - 1;
     for (int buf = 0; t < end; buf ^= 1) {
         const int j0 = t * BK, t3 = t2 < end ? behind(t2) : end;
@@ -408,62 +402,83 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
             bwla_lds_barrier();
         }
         if (att_uniform(even ? j0 <= w_last || j0 < s.prefix : any != 0)) {
-            Scores sc;
-            Packed p;
-            bool fine = false;
-            products(kb, sc);
-            // (the compiler would read each operand right in front of its product and wait: 130 cycles each)
-            if constexpr (BF) {
+            const bool whole = even && (j0 + BK - 1 <= w_first || j0 + BK <= s.prefix);        // every row sees every key
+            // a tile's scores made ready: cap, bias, mask, and a maximum that will do for them
+            auto ready = [&](v16f& sc, int k, auto first) {
+                if constexpr (GENERAL) transform(sc, k, j0 + k * 32, now.p);
+                bool fine = false;
+                if (__builtin_expect(whole, 1)) {
+                    had += 16;
+                } else {
+                    if (even) {
+                        const int most = max(me.i, s.prefix - 1) - j0 - k * 32 - 4 * hf;
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) sc[r] = (r & 3) + 8 * (r >> 2) <= most ? sc[r] : -INFINITY;
+                        had += min(max((most & ~3) / 2 + 4, 0), 16);           // (four too many at most)
+                    } else {
+                        const uint32_t mine = (uint32_t)(ok >> (32 * k)) >> (4 * hf);
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) sc[r] = (mine >> ((r & 3) + 8 * (r >> 2))) & 1 ? sc[r] : -INFINITY;
+                        had += __popc(mine & 0x0f0f0f0fu);
+                    }
+                    fine = BF && att_uniform(__any(!blind & (had < FEW)));
+                }
+                raise(sc, first);
+                if constexpr (BF) {
+                    if (__builtin_expect(fine, 0)) {
+                        Packed p;
+                        weigh(sc, p, std::true_type{});
+                        values(fetch(vb, k), vb, p, k);
+                    }
+                }
+            };
+            if constexpr (KT == 2) {
+                // The weights of one tile are taken while the other's products run; operands are read ahead.  The compiler has to
+                // be told: left to itself it reads each operand right in front of its product and waits (130 cycles each).
+                v16f s0, s1;
+                Packed p0, p1;
+                products(kb, 0, s0);
                 __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
 #pragma unroll
-                for (int i = 0; i < KT * CS - AHEAD; ++i) {
+                for (int i = 0; i < CS - AHEAD; ++i) {
                     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
                     __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
                 }
                 __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
-            }
-            if constexpr (GENERAL) transform(sc, j0, now.p);
-            if (__builtin_expect(even && (j0 + BK - 1 <= w_first || j0 + BK <= s.prefix), 1)) {
-                had += BK / 2;                         // (every row sees every key)
-            } else {
-                if (even) {
-                    const int most = max(me.i, s.prefix - 1) - j0 - 4 * hf;
+                ready(s0, 0, [] {});
+                products(kb, 1, s1);
+                weigh(s0, p0, std::false_type{});
+                asm volatile("" : "+v"(p0[0]), "+v"(p0[1]), "+v"(l));          // (here, and not where they are used)
+                __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 1);
 #pragma unroll
-                    for (int k = 0; k < KT; ++k)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) sc[k][r] = k * 32 + (r & 3) + 8 * (r >> 2) <= most ? sc[k][r] : -INFINITY;
-                    had += min(max((most & ~3) / 2 + 4, 0), BK / 2);           // (four too many at most)
-                } else {
-#pragma unroll
-                    for (int k = 0; k < KT; ++k) {
-                        const uint32_t mine = (uint32_t)(ok >> (32 * k)) >> (4 * hf);
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) sc[k][r] = (mine >> ((r & 3) + 8 * (r >> 2))) & 1 ? sc[k][r] : -INFINITY;
-                        had += __popc(mine & 0x0f0f0f0fu);
-                    }
+                for (int i = 0; i < CS; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+                    if (i < CS - AHEAD) __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+                    __builtin_amdgcn_sched_group_barrier(0x002, 72 / CS, 1);
                 }
-                fine = BF && att_uniform(__any(!blind & (had < FEW)));
-            }
-            raise(sc);
-            if constexpr (BF) {
-                if (__builtin_expect(fine, 0)) {
-                    weigh(sc, p, std::true_type{});
-#pragma unroll
-                    for (int k = 0; k < KT; ++k) values(fetch(vb, k), vb, p, k);
-                }
-                // (a half's operands are on their way while the weights are taken, the other's during the first half's products:
-                // left to itself the compiler reads each in front of its product, and waits)
+                ready(s1, 1, [&] {
+                    values(fetch(vb, 0), vb, p0, 0);
+                    p0[0] = p0[1] = v4u{0, 0, 0, 0};
+                });
                 const Operands f0 = fetch(vb, 0);
                 __builtin_amdgcn_sched_barrier(0);
-                weigh(sc, p, std::false_type{});
+                values(f0, vb, p0, 0);
+                weigh(s1, p1, std::false_type{});
+#pragma unroll
+                for (int i = 0; i < 2 * DT; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 2);
+                    __builtin_amdgcn_sched_group_barrier(0x002, 72 / (2 * DT), 2);
+                }
                 const Operands f1 = fetch(vb, 1);
                 __builtin_amdgcn_sched_barrier(0);
-                values(f0, vb, p, 0);
-                values(f1, vb, p, 1);
+                values(f1, vb, p1, 1);
             } else {
+                v16f sc;
+                Packed p;
+                products(kb, 0, sc);
+                ready(sc, 0, [] {});
                 weigh(sc, p, std::false_type{});
-#pragma unroll
-                for (int k = 0; k < KT; ++k) values(Operands{}, vb, p, k);
+                values(fetch(vb, 0), vb, p, 0);
             }
         }
         now = next;
@@ -498,13 +513,13 @@ template <bool BF, int DP>
 hipError_t at_launch(const AttArgs& a, hipStream_t st) {
     const int tiles = (int)(((int64_t)a.max_new * a.group + AT_ROWS - 1) / AT_ROWS);
     const int units = a.seqs * a.hkv;
-    const int order = att_order_of(tiles, units, DP == 256 ? 1 : 2);
+    const AtOrder order = at_order_of(tiles, units, DP == 256 ? 1 : 2);
     constexpr int lds = AtShape<BF, DP>::LDS;
     const bool general = a.capped != 0.f || a.slopes, exact = a.d == DP;
     auto go = [&](auto kernel) {
         const hipError_t e = bwla_ensure_lds((const void*)kernel, lds);
         if (e != hipSuccess) return e;
-        kernel<<<dim3((unsigned)((int64_t)tiles * units)), 64 * AT_WAVES, lds, st>>>(a, tiles, units, order);
+        kernel<<<dim3((unsigned)((int64_t)tiles * units)), 64 * AT_WAVES, lds, st>>>(a, order);
         return hipGetLastError();
     };
     if (exact) return general ? go(att_tile_kernel<BF, DP, true, true>) : go(att_tile_kernel<BF, DP, true, false>);
