@@ -33,11 +33,9 @@ struct AttArgs {
     float c1, c2, capped;                                  // capped: C, 0: no cap
 };
 
-// launchers (attention_tile_*.hip, attention_split.hip, attention_weights.hip, attention_rope.hip, cache_evict.hip)
-hipError_t bwla_launch_attention_tile(const AttArgs& a, int dtype, hipStream_t st);
-hipError_t bwla_launch_attention_tile_f32(const AttArgs& a, hipStream_t st);
+// launchers (attention_tile*.hip, attention_split.hip, attention_weights.hip, attention_rope.hip, cache_evict.hip)
 
-// few rows over a long cache: how the cache's length is split
+// how a cache's length is split
 struct AttSplit {
     int chunk, splits;       // cached tokens of one workgroup; workgroups along the longest sequence
     int rows;                // rows of a sequence and key-value head: new tokens x group
@@ -45,9 +43,16 @@ struct AttSplit {
     int pitch;               // cached tokens of a row of the scores that the sums of weights read
     size_t part_bytes, stat_bytes, score_bytes;
 };
+// few rows
 AttSplit bwla_att_split(const AttArgs& a, bool weights);
 bool bwla_att_is_split(const AttArgs& a);
 hipError_t bwla_launch_attention_split(const AttArgs& a, const AttSplit& s, int dtype, void* ws, hipStream_t st);
+// many rows
+AttSplit bwla_att_tile_split(const AttArgs& a);
+hipError_t bwla_launch_attention_tile(const AttArgs& a, const AttSplit& s, int dtype, void* ws, hipStream_t st);
+hipError_t bwla_launch_attention_tile_f32(const AttArgs& a, const AttSplit& s, void* ws, hipStream_t st);
+// the parts of either added up
+hipError_t bwla_launch_attention_join(const AttArgs& a, const AttSplit& s, int dtype, void* ws, hipStream_t st);
 
 struct AttWeightsPlan {
     int parts;               // the rows of a sequence and key-value head are dealt out over this many workgroups

@@ -1,6 +1,7 @@
 // C ABI of the cache, the rotary positions, the attention and the eviction: validation on the host, then launches.
 // Nothing here allocates device memory, synchronizes or throws.
 #include <math.h>
+#include <algorithm>
 
 #include "attention.h"
 
@@ -106,7 +107,9 @@ size_t forward_bytes(const AttArgs& a, bool weights, int dtype) {
         const AttSplit p = bwla_att_split(a, weights);
         return p.part_bytes + p.stat_bytes + p.score_bytes;
     }
-    return weights && a.max_len > 0 ? bwla_att_weights_plan(a, dtype).bytes : 0;
+    // (the sums of weights, if wanted, use the same memory afterwards)
+    const AttSplit p = bwla_att_tile_split(a);
+    return std::max(p.part_bytes + p.stat_bytes, weights && a.max_len > 0 ? bwla_att_weights_plan(a, dtype).bytes : 0);
 }
 
 // an integer and a place in the list for each token
@@ -208,7 +211,7 @@ bwla_status_t bwla_attention_forward(const bwla_kv_cache_t* cache, const bwla_kv
     a.weights = d_weights;
     const hipStream_t s = (hipStream_t)stream;
     if (bwla_att_is_split(a)) return done(bwla_launch_attention_split(a, bwla_att_split(a, d_weights != nullptr), cache->dtype, d_ws, s));
-    const hipError_t e = bwla_launch_attention_tile(a, cache->dtype, s);
+    const hipError_t e = bwla_launch_attention_tile(a, bwla_att_tile_split(a), cache->dtype, d_ws, s);
     if (e != hipSuccess || !d_weights || a.max_len == 0) return done(e);
     return done(bwla_launch_attention_weights(a, cache->dtype, d_ws, s));
 }

@@ -56,14 +56,15 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
     const int bh = unit / sp.row_tiles, rt = unit - bh * sp.row_tiles, b = bh / a.hkv, h = bh - b * a.hkv;
     const AttSeq s = att_seq(a, b);
     const int rows = s.fresh * a.group, row = rt * 16 + li;
-    if (rt * 16 >= rows) return;
+    const bool parts = s.n > sp.chunk;         // (a sequence of one part is done here)
+    if (rt * 16 >= rows || (!parts && split > 0)) return;
     const int64_t at_part = (int64_t)unit * sp.splits + split;
     const int c0 = split * sp.chunk, c1 = min(c0 + sp.chunk, s.n);
     // where no position and no row count says otherwise, keys in front of the first row's window are not read
     const int i_first = s.n - s.fresh + rt * 16 / a.group;
     const int skip_to = (s.pos || a.window == INT32_MAX) ? 0 : i_first - a.window + 1;
     const bool none = c0 >= c1 || (c1 <= skip_to && c0 >= s.prefix);
-    if (none && sp.splits > 1) {
+    if (none && parts) {
         if (threadIdx.x < 16) stat[at_part * 16 + threadIdx.x] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
         if (scores) {                          // (what the sums of weights read of it)
             for (int r = 0; r < 16 && rt * 16 + r < rows; ++r)
@@ -283,7 +284,7 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
                 *(float4*)&s_o[wave][li][u * 16 * CW + 4 * CW * g + CW * r + c] =
                     make_float4(o[u * CW + c][r] * f, o[u * CW + c + 1][r] * f, o[u * CW + c + 2][r] * f, o[u * CW + c + 3][r] * f);
     if (wave == 0 && g == 0) {
-        if (sp.splits > 1) stat[at_part * 16 + li] = make_float4(mm, ll, llr, 0.f);
+        if (parts) stat[at_part * 16 + li] = make_float4(mm, ll, llr, 0.f);
         s_mm[li] = mm;
         s_ll[li] = ll;
         s_llr[li] = llr;
@@ -299,7 +300,7 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
             const float4 x = *(const float4*)&s_o[w][r][c];
             v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
         }
-        if (sp.splits > 1) {
+        if (parts) {
             if (rt * 16 + r < rows) *(float4*)(part + (at_part * 16 + r) * DP + c) = v;
         } else if (rt * 16 + r < rows && c < a.d) {
             const float total = s_ll[r], inv = total > 0.f ? 1.f / s_llr[r] : 0.f;
@@ -326,6 +327,7 @@ __global__ __launch_bounds__(GROUPS * DP / 4) void att_join_kernel(AttArgs a, At
     if (row >= s.fresh * a.group) return;
     const int rt = row >> 4, r = row & 15;
     const int64_t unit = ((int64_t)b * a.hkv + h) * sp.row_tiles + rt;
+    if (s.n <= sp.chunk) return;                       // (one part: written by its workgroup)
     const int used = (s.n + sp.chunk - 1) / sp.chunk;
     const float4* st = stat + unit * sp.splits * 16 + r;
     float m = -INFINITY;
@@ -390,6 +392,39 @@ __global__ __launch_bounds__(GROUPS * DP / 4) void att_join_kernel(AttArgs a, At
     if (c == 0 && a.lse) a.lse[(int64_t)(s.row0 + t) * a.hq + hd] = l > 0.f ? (m + __log2f(l)) * ATT_LN2 : -INFINITY;
 }
 
+// The same where rows are many and splits few: DP / 4 threads a row, which take the splits in turn.
+template <bool BF, int DP>
+__global__ __launch_bounds__(256) void att_join_rows_kernel(AttArgs a, AttSplit sp, const float* __restrict__ part,
+                                                            const float4* __restrict__ stat) {
+    constexpr int LANES = DP / 4, ROWS = 256 / LANES;
+    const int h = blockIdx.y, b = blockIdx.z, row = blockIdx.x * ROWS + threadIdx.x / LANES, c = threadIdx.x % LANES * 4;
+    const AttSeq s = att_seq(a, b);
+    if (row >= s.fresh * a.group || s.n <= sp.chunk || c >= a.d) return;
+    const int used = (s.n + sp.chunk - 1) / sp.chunk;
+    const int64_t at = (((int64_t)b * a.hkv + h) * sp.row_tiles + (row >> 4)) * sp.splits * 16 + (row & 15);
+    float m = -INFINITY;
+#pragma unroll 4
+    for (int i = 0; i < used; ++i) m = fmaxf(m, stat[at + i * 16].x);
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    float l = 0.f, lr = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < used; ++i) {
+        const float4 x = stat[at + i * 16];
+        if (x.x == -INFINITY) continue;                // (nothing was written where nothing is seen)
+        const float f = __builtin_amdgcn_exp2f(x.x - m);
+        const float4 p = *(const float4*)(part + (at + i * 16) * DP + c);
+        l += x.y * f;
+        lr += x.z * f;
+        v.x += p.x * f; v.y += p.y * f; v.z += p.z * f; v.w += p.w * f;
+    }
+    const float inv = l > 0.f ? 1.f / lr : 0.f;
+    const int t = row / a.group, hd = h * a.group + row - t * a.group;
+    const int64_t to = ((int64_t)(s.row0 + t) * a.hq + hd) * a.d + c;
+    if constexpr (BF) *(uint2*)(a.out + to * 2) = make_uint2(att_pack_bf16(v.x * inv, v.y * inv), att_pack_bf16(v.z * inv, v.w * inv));
+    else *(float4*)(a.out + to * 4) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+    if (c == 0 && a.lse) a.lse[(int64_t)(s.row0 + t) * a.hq + hd] = l > 0.f ? (m + __log2f(l)) * ATT_LN2 : -INFINITY;
+}
+
 // The rows' weights of each cached token, from the scores that the first launch left, added to the token's sum.  A thread
 // takes four tokens, which lie in one page.
 __global__ __launch_bounds__(256) void att_sum_kernel(AttArgs a, AttSplit sp, const float* __restrict__ scores) {
@@ -423,6 +458,21 @@ __global__ __launch_bounds__(256) void att_sum_kernel(AttArgs a, AttSplit sp, co
 }
 
 template <bool BF, int DP>
+hipError_t join(const AttArgs& a, const AttSplit& s, void* ws, hipStream_t st) {
+    const float* part = (const float*)ws;
+    const float4* stat = (const float4*)((const char*)ws + s.part_bytes);
+    // Many rows: a few threads each (53280 rows of up to 4 splits 35 -> 16 us, but 4096 rows 7.6 -> 9.0 us).  Few rows of many splits
+    // (long caches of few sequences): more threads (128 splits of 64 rows 13.2 -> 7.2 us, but 4 splits of 4096 rows 8.8 -> 16.3 us)
+    constexpr int FEW = 4, MANY = DP == 256 ? 8 : 16, ROWS = 1024 / DP;
+    const dim3 rows(s.rows, a.hkv, a.seqs);
+    if ((int64_t)s.rows * a.hkv * a.seqs >= 8192)
+        att_join_rows_kernel<BF, DP><<<dim3((s.rows + ROWS - 1) / ROWS, a.hkv, a.seqs), 256, 0, st>>>(a, s, part, stat);
+    else if (s.splits > 16) att_join_kernel<BF, DP, MANY><<<rows, MANY * DP / 4, 0, st>>>(a, s, part, stat);
+    else att_join_kernel<BF, DP, FEW><<<rows, FEW * DP / 4, 0, st>>>(a, s, part, stat);
+    return hipGetLastError();
+}
+
+template <bool BF, int DP>
 hipError_t launch(const AttArgs& a, const AttSplit& s, void* ws, hipStream_t st) {
     float* part = (float*)ws;
     float4* stat = (float4*)((char*)ws + s.part_bytes);
@@ -430,12 +480,7 @@ hipError_t launch(const AttArgs& a, const AttSplit& s, void* ws, hipStream_t st)
     const dim3 grid((unsigned)((int64_t)s.splits * a.seqs * a.hkv * s.row_tiles));
     if (a.d == DP) att_split_kernel<BF, DP, true><<<grid, 64 * SP_WAVES, 0, st>>>(a, s, part, stat, scores);
     else att_split_kernel<BF, DP, false><<<grid, 64 * SP_WAVES, 0, st>>>(a, s, part, stat, scores);
-    // many splits (long caches of few sequences): more threads for each row.  128 splits of 64 rows 13.2 -> 7.2 us, but 4 splits of
-    // 4096 rows 8.8 -> 16.3 us
-    constexpr int FEW = 4, MANY = DP == 256 ? 8 : 16;
-    const dim3 rows(s.rows, a.hkv, a.seqs);
-    if (s.splits > 16) att_join_kernel<BF, DP, MANY><<<rows, MANY * DP / 4, 0, st>>>(a, s, part, stat);
-    else if (s.splits > 1) att_join_kernel<BF, DP, FEW><<<rows, FEW * DP / 4, 0, st>>>(a, s, part, stat);
+    if (s.splits > 1) join<BF, DP>(a, s, ws, st);
     if (scores && a.max_len > 0) att_sum_kernel<<<dim3((a.max_len + 1023) / 1024, a.hkv, a.seqs), 256, 0, st>>>(a, s, scores);
     return hipGetLastError();
 }
@@ -471,4 +516,15 @@ hipError_t bwla_launch_attention_split(const AttArgs& a, const AttSplit& s, int 
     if (a.d <= 64) return launch<false, 64>(a, s, ws, st);
     if (a.d <= 128) return launch<false, 128>(a, s, ws, st);
     return launch<false, 256>(a, s, ws, st);
+}
+
+hipError_t bwla_launch_attention_join(const AttArgs& a, const AttSplit& s, int dtype, void* ws, hipStream_t st) {
+    if (dtype == BWLA_X_BF16) {
+        if (a.d <= 64) return join<true, 64>(a, s, ws, st);
+        if (a.d <= 128) return join<true, 128>(a, s, ws, st);
+        return join<true, 256>(a, s, ws, st);
+    }
+    if (a.d <= 64) return join<false, 64>(a, s, ws, st);
+    if (a.d <= 128) return join<false, 128>(a, s, ws, st);
+    return join<false, 256>(a, s, ws, st);
 }

@@ -28,6 +28,21 @@ __device__ __forceinline__ float half_sum(float v) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// bits of any of the wavefront's rows (lane i has those of row i & 31), a scalar
+__device__ __forceinline__ uint64_t rows_or(uint64_t bits) {
+    uint32_t w[2] = {(uint32_t)bits, (uint32_t)(bits >> 32)};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        w[i] |= __builtin_amdgcn_mov_dpp(w[i], 0x128, 0xf, 0xf, true);         // 16 lanes turned by 8, 4, 2, 1
+        w[i] |= __builtin_amdgcn_mov_dpp(w[i], 0x124, 0xf, 0xf, true);
+        w[i] |= __builtin_amdgcn_mov_dpp(w[i], 0x122, 0xf, 0xf, true);
+        w[i] |= __builtin_amdgcn_mov_dpp(w[i], 0x121, 0xf, 0xf, true);
+        const auto r = __builtin_amdgcn_permlane16_swap(w[i], w[i], false, false);
+        w[i] = __builtin_amdgcn_readfirstlane(r[0] | r[1]);
+    }
+    return ((uint64_t)w[1] << 32) | w[0];
+}
+
 // Workgroups are dealt round-robin to the 8 XCDs, units (sequence, key-value head) to workgroups, so that an XCD keeps to
 // some units at a time, as few as keep it busy: their rows walk over the same keys and values at about the same time, which
 // its own L2 then has (all units at once: 770 us for a prompt of 8192 with 32 heads, bound by what lies behind the L2).
@@ -64,7 +79,8 @@ struct AtShape {
 
 // BF: bf16 (else fp32); DP: columns, 64, 128 or 256; EXACT: d == DP; GENERAL: a cap or a bias
 template <bool BF, int DP, bool EXACT, bool GENERAL>
-__global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_kernel(AttArgs a, AtOrder order) {
+__global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_kernel(AttArgs a, AtOrder order, AttSplit sp, float* __restrict__ part,
+                                                                                float4* __restrict__ stat) {
     using S = AtShape<BF, DP>;
     constexpr int ES = S::ES, BK = S::BK, ROWB = S::ROWB, CH = S::CH, KT = BK / 32, DT = DP / 32, CS = CH / 2;
     extern __shared__ __align__(16) char smem[];
@@ -73,10 +89,15 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
 
     int unit, tile;
     at_place(blockIdx.x, order, unit, tile);
+    const int units = a.seqs * a.hkv, split = unit / units;
+    unit -= split * units;
     const int b = unit / a.hkv, h = unit - b * a.hkv;
     const AttSeq s = att_seq(a, b);
     const int rows = s.fresh * a.group;
-    if (tile * AT_ROWS >= rows) return;
+    // this workgroup's part of the cached tokens, if the sequence has several
+    const bool whole_length = s.n <= sp.chunk;
+    const int from = split * sp.chunk;
+    if (tile * AT_ROWS >= rows || (split > 0 && from >= s.n)) return;
 
     const int lane = threadIdx.x & 63, wave = att_wave(), l32 = lane & 31, hf = lane >> 5;
     const int row = tile * AT_ROWS + wave * 32 + l32;
@@ -103,11 +124,10 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
     const int pb = min((max(s.prefix, 0) + BK - 1) / BK, (s.n + BK - 1) / BK);
     int lo = s.pos || a.window == INT32_MAX ? 0 : max(g_first - a.window + 1, 0) / BK;
     if (lo < pb) lo = pb;
-    const int end = max((g_last + BK) / BK, pb);
+    const int end = min(max((g_last + BK) / BK, pb), (int)(((int64_t)from + sp.chunk + BK - 1) / BK));
     // rows that see nothing whatever the block: what they gather on the way is dropped at the end
     const bool blind = me.doc < 0;
-    // documents: the one of all the workgroup's rows (else -3), and the blocks that may hold keys of theirs
-    int one_doc = 0;
+    // documents: the blocks that may hold keys of the rows'
     if (s.doc) {
         uint32_t* const active = (uint32_t*)(smem + 4 * S::TILE);              // a bit for each block that may matter
         int* const range = (int*)(active + AT_MAP / 32);
@@ -124,9 +144,8 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
             dmin = min(dmin, range[w]);
             dmax = max(dmax, range[AT_WAVES + w]);
         }
-        one_doc = __builtin_amdgcn_readfirstlane(dmin == dmax ? dmin : -3);
         // a wavefront looks at 32 blocks, whose word it writes, eight loads at a time on the way
-        for (int w = wave; w < (min(end, AT_MAP) + 31) / 32; w += AT_WAVES) {
+        for (int w = from / BK / 32 + wave; w < (min(end, AT_MAP) + 31) / 32; w += AT_WAVES) {
             uint32_t word = 0;
 #pragma unroll
             for (int i0 = 0; i0 < 32; i0 += 8) {
@@ -353,7 +372,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
     };
 
     // blocks t, t1, t2, t3 in turn: in work, copied, found, looked up
-    int t = behind(-1), t1 = t < end ? behind(t) : end, t2 = t1 < end ? behind(t1) : end;
+    int t = behind(from / BK - 1), t1 = t < end ? behind(t) : end, t2 = t1 < end ? behind(t1) : end;
     Key now{0, 0, -1}, next{0, 0, -1};                 // keys of t and t1
     Found far{0, 0, 0};                                // ... of t2, as loaded
     if (t < end) {
@@ -375,20 +394,37 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
         if (t2 < end) after = settle(far, t2);
         if (t3 < end) far = look(t3);
         if (t1 < end) copy(next.at, buf ^ 1);
-        // Even: every key exists, is of the one document of the workgroup's rows (where these are told apart) and in reach of
-        // their windows, so that a row sees those up to its index, or all of the prefix.  Else each wavefront works out what
-        // each of its rows sees (a bit for each key), and values of keys that no row of the workgroup sees are cleared: they
-        // may be anything, and a weight of 0 does not make 0 of that.
-        const bool even = att_uniform(__all(s.doc ? now.doc == one_doc : now.doc >= 0) &&
-                                      (a.window == INT32_MAX || (!s.pos && j0 > g_last - a.window) || j0 + BK <= s.prefix));
+        // Even: every key exists and is of one document, and in reach of the windows, so that a row of that document sees those up
+        // to its index, or all of the prefix.  Else each wavefront works out what each of its rows sees (a bit for each key), and
+        // values of keys that no row of the workgroup sees are cleared: they may be anything, and a weight of 0 does not make 0
+        // of that.
+        const int doc = __builtin_amdgcn_readfirstlane(now.doc);
+        const bool even = doc >= 0 && att_uniform(__all(now.doc == doc) &&
+                                                  (a.window == INT32_MAX || (!s.pos && j0 > g_last - a.window) || j0 + BK <= s.prefix));
+        const bool mine = me.doc == doc;
         uint64_t ok = ALL, any = ALL;
         if (__builtin_expect(!even, 0)) {
-            any = 0;
-            for (int r = 0; r < 32; ++r) {
-                const AttRow row{__builtin_amdgcn_readlane(me.i, r), __builtin_amdgcn_readlane(me.p, r), __builtin_amdgcn_readlane(me.doc, r)};
-                const uint64_t bits = __ballot(att_sees(row, s.prefix, a.window, j0 + lane % BK, now.p, now.doc)) & ALL;
-                any |= bits;
-                ok = l32 == r ? bits : ok;
+            ok = any = 0;
+            if (s.pos && a.window != INT32_MAX) {
+                for (int r = 0; r < 32; ++r) {
+                    const AttRow row{__builtin_amdgcn_readlane(me.i, r), __builtin_amdgcn_readlane(me.p, r), __builtin_amdgcn_readlane(me.doc, r)};
+                    const uint64_t bits = __ballot(att_sees(row, s.prefix, a.window, j0 + lane % BK, now.p, now.doc)) & ALL;
+                    any |= bits;
+                    ok = l32 == r ? bits : ok;
+                }
+            } else {                                   // a step for each of the keys' documents, of which there are few
+                for (uint64_t left = __ballot(now.doc >= 0) & ALL; left;) {
+                    const int one = __builtin_amdgcn_readlane(now.doc, __builtin_ctzll(left));
+                    const uint64_t bits = __ballot(now.doc == one) & ALL;
+                    ok = me.doc == one ? bits : ok;
+                    left &= ~bits;
+                }
+                const int up = me.i - j0, from = up >= a.window ? up - a.window + 1 : 0, pre = s.prefix - j0;
+                uint64_t reach = up >= 63 ? ~0ull : up < 0 ? 0 : (2ull << up) - 1;
+                reach = from > 63 ? 0 : reach >> from << from;
+                reach |= pre > 63 ? ~0ull : pre <= 0 ? 0 : (1ull << pre) - 1;
+                ok &= reach;
+                any = rows_or(ok);
             }
             uint64_t* const seen = (uint64_t*)(smem + 4 * S::TILE + AT_MAP / 8 + 2 * AT_WAVES * 4);
             if (lane == 0) seen[wave] = any;
@@ -401,8 +437,9 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
             }
             bwla_lds_barrier();
         }
-        if (att_uniform(even ? j0 <= w_last || j0 < s.prefix : any != 0)) {
-            const bool whole = even && (j0 + BK - 1 <= w_first || j0 + BK <= s.prefix);        // every row sees every key
+        if (att_uniform(even ? __any(mine) && (j0 <= w_last || j0 < s.prefix) : any != 0)) {
+            // every row sees every key
+            const bool whole = even && att_uniform(__all(mine | blind)) && (j0 + BK - 1 <= w_first || j0 + BK <= s.prefix);
             // a tile's scores made ready: cap, bias, mask, and a maximum that will do for them
             auto ready = [&](v16f& sc, int k, auto first) {
                 if constexpr (GENERAL) transform(sc, k, j0 + k * 32, now.p);
@@ -411,7 +448,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
                     had += 16;
                 } else {
                     if (even) {
-                        const int most = max(me.i, s.prefix - 1) - j0 - k * 32 - 4 * hf;
+                        const int most = (mine ? max(me.i, s.prefix - 1) : -1) - j0 - k * 32 - 4 * hf;
 #pragma unroll
                         for (int r = 0; r < 16; ++r) sc[r] = (r & 3) + 8 * (r >> 2) <= most ? sc[r] : -INFINITY;
                         had += min(max((most & ~3) / 2 + 4, 0), 16);           // (four too many at most)
@@ -437,6 +474,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
                 // be told: left to itself it reads each operand right in front of its product and waits (130 cycles each).
                 v16f s0, s1;
                 Packed p0, p1;
+                __builtin_amdgcn_s_setprio(1);
                 products(kb, 0, s0);
                 __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
 #pragma unroll
@@ -445,7 +483,9 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
                     __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
                 }
                 __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+                __builtin_amdgcn_s_setprio(0);
                 ready(s0, 0, [] {});
+                __builtin_amdgcn_s_setprio(1);
                 products(kb, 1, s1);
                 weigh(s0, p0, std::false_type{});
                 asm volatile("" : "+v"(p0[0]), "+v"(p0[1]), "+v"(l));          // (here, and not where they are used)
@@ -456,10 +496,12 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
                     if (i < CS - AHEAD) __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
                     __builtin_amdgcn_sched_group_barrier(0x002, 72 / CS, 1);
                 }
+                __builtin_amdgcn_s_setprio(0);
                 ready(s1, 1, [&] {
                     values(fetch(vb, 0), vb, p0, 0);
                     p0[0] = p0[1] = v4u{0, 0, 0, 0};
                 });
+                __builtin_amdgcn_s_setprio(1);
                 const Operands f0 = fetch(vb, 0);
                 __builtin_amdgcn_sched_barrier(0);
                 values(f0, vb, p0, 0);
@@ -472,6 +514,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
                 const Operands f1 = fetch(vb, 1);
                 __builtin_amdgcn_sched_barrier(0);
                 values(f1, vb, p1, 1);
+                __builtin_amdgcn_s_setprio(0);
             } else {
                 v16f sc;
                 Packed p;
@@ -492,6 +535,18 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
     lr = BF ? half_sum(lr) : l;
     if (blind) l = lr = 0.f;
     if (!live) return;
+    if (!whole_length) {                               // in tiles of 16 rows, as the join reads them
+        const int64_t to = ((int64_t)(unit * sp.row_tiles + row / 16) * sp.splits + split) * 16 + row % 16;
+        if (hf == 0) stat[to] = make_float4(blind ? -INFINITY : m, l, lr, 0.f);
+        if (m != -INFINITY) {
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4)
+                    *(float4*)(part + to * DP + 32 * d + 2 * r + 4 * hf) = make_float4(o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]);
+        }
+        return;
+    }
     const float inv = lr > 0.f ? 1.f / lr : 0.f;
     const int64_t at = ((int64_t)(s.row0 + tok) * a.hq + head);
     char* const dst = a.out + at * a.d * ES;
@@ -510,16 +565,18 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
 }
 
 template <bool BF, int DP>
-hipError_t at_launch(const AttArgs& a, hipStream_t st) {
-    const int tiles = (int)(((int64_t)a.max_new * a.group + AT_ROWS - 1) / AT_ROWS);
-    const int units = a.seqs * a.hkv;
+hipError_t at_launch(const AttArgs& a, const AttSplit& sp, void* ws, hipStream_t st) {
+    const int tiles = (sp.rows + AT_ROWS - 1) / AT_ROWS;
+    const int units = a.seqs * a.hkv * sp.splits;
     const AtOrder order = at_order_of(tiles, units, DP == 256 ? 1 : 2);
     constexpr int lds = AtShape<BF, DP>::LDS;
     const bool general = a.capped != 0.f || a.slopes, exact = a.d == DP;
+    float* const part = (float*)ws;
+    float4* const stat = (float4*)((char*)ws + sp.part_bytes);
     auto go = [&](auto kernel) {
         const hipError_t e = bwla_ensure_lds((const void*)kernel, lds);
         if (e != hipSuccess) return e;
-        kernel<<<dim3((unsigned)((int64_t)tiles * units)), 64 * AT_WAVES, lds, st>>>(a, order);
+        kernel<<<dim3((unsigned)((int64_t)tiles * units)), 64 * AT_WAVES, lds, st>>>(a, order, sp, part, stat);
         return hipGetLastError();
     };
     if (exact) return general ? go(att_tile_kernel<BF, DP, true, true>) : go(att_tile_kernel<BF, DP, true, false>);

@@ -281,6 +281,49 @@ def test_long_caches_are_split_and_joined(A, dtype, lens, news):
     check(Case(dtype, 128, 8, 1, 64, lens, news), A, ("window", "prefix", "cap"))
 
 
+MANY_ROWS = [  # (layout, cached, new): few workgroups, so that the cached tokens are dealt out over several and their parts added up
+    (("bf16", 128, 4, 2, 16), [1500, 40, 0, 700], [80, 40, 0, 33]),
+    (("bf16", 80, 6, 2, 8), [1100, 257], [70, 257]),
+    (("bf16", 256, 8, 1, 32), [900], [60]),
+    (("f32", 128, 4, 2, 16), [900, 513], [50, 51]),
+    (("f32", 40, 7, 1, 16), [520], [300]),
+]
+
+
+@pytest.mark.parametrize("names", [(), ("cap", "slopes"), ("window", "prefix"), ("runs",), ("doc",), ("window", "position"),
+                                   ("cap", "slopes", "window", "prefix", "doc", "position")])
+@pytest.mark.parametrize("layout,lens,news", MANY_ROWS)
+def test_many_rows_over_parts_of_the_cache(A, layout, lens, news, names):
+    c = Case(*layout, lens, news, seed=21)
+    assert A.attention_workspace_size(A.KVCache(c.k, c.v), c.batch(A), c.hq, False) > 0
+    out = check(c, A, names)
+    assert c.torch.equal(out, check(c, A, names))
+
+
+@pytest.mark.parametrize("layout,lens,news", [
+    (("bf16", 64, 14, 2, 16), [600], [600]),                                   # rows enough for the other join
+    (("f32", 8, 14, 2, 16), [600], [600]),
+    (("bf16", 8, 33, 33, 16), [2500, 100, 130, 7], [129, 100, 129, 7]),        # sequences of very different lengths
+])
+def test_many_rows_joined(A, layout, lens, news):
+    c = Case(*layout, lens, news, seed=22)
+    assert A.attention_workspace_size(A.KVCache(c.k, c.v), c.batch(A), c.hq, False) > 0
+    check(c, A)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("names", [(), ("prefix",), ("window",), ("position", "window")])
+@pytest.mark.parametrize("run", [1, 5, 40, 200])
+def test_rows_of_several_documents(A, dtype, names, run):
+    """Short documents, of which many lie in a block, and longer ones, whose ends lie inside a workgroup's rows."""
+    class Runs(Case):
+        def options(self, rng, names):
+            kw, oracle = super().options(rng, names)
+            doc = np.stack([(np.arange(max(self.lens)) + 3) // run % 9 for _ in self.lens])
+            return {**kw, "doc": self.i32(doc)}, lambda b: {**oracle(b), "doc": doc[b]}
+    check(Runs(dtype, 64, 4, 2, 16, [450, 130], [450, 60], seed=23), A, names)
+
+
 def test_the_same_call_gives_the_same_bits(A):
     import torch
     for lens, news in (([2000, 37], [1, 1]), ([500, 300], [200, 300])):
