@@ -165,6 +165,75 @@ __device__ __forceinline__ float att_score(const AttArgs& a, float prod) {
     return a.capped != 0.f ? a.capped * att_tanh(prod * a.c2) : prod * a.c1;
 }
 
+// Products of 32 keys (rows of the tile) and 32 rows (lanes, in both halves alike) into scores: cap and bias.  (Without either they
+// stay products until their weights are taken.)  The tile's keys are number 32 k .. of those behind j0, of which lane i knows the
+// position of key i; mp: the row's position.
+template <bool BF>
+__device__ __forceinline__ void att_transform(const AttArgs& a, v16f& sc, int mp, float slope, int j0, int k, int kp, bool moved) {
+    const int hf = (threadIdx.x >> 5) & 1;
+    if (a.capped != 0.f) {
+        const float C = a.capped, c3 = a.c2 * (2.f * ATT_LOG2E);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            if constexpr (BF)                          // (an error of 1e-7 of the cap: weights are rounded to 8 bits)
+                sc[r] = fmaf(-2.f * C, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(sc[r] * c3)), C);
+            else
+                sc[r] = C * att_tanh(sc[r] * a.c2);
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[r] *= a.c1;
+    }
+    if (a.slopes && moved) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            sc[r] = fmaf(-slope, fabsf((float)(mp - __shfl(kp, k * 32 + (r & 3) + 8 * (r >> 2) + 4 * hf, 64))), sc[r]);
+    } else if (a.slopes) {
+        const float away = (float)(mp - j0 - k * 32 - 4 * hf);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[r] = fmaf(-slope, fabsf(away - (float)((r & 3) + 8 * (r >> 2))), sc[r]);
+    }
+}
+// What rows (lane i: row i & 31) see of 64 keys (lane i: key j0 + i, and its position and document): a bit for each key
+__device__ __forceinline__ uint64_t att_seen(const AttArgs& a, const AttSeq& s, const AttRow& me, int j0, int kp, int kdoc) {
+    const int lane = threadIdx.x & 63;
+    uint64_t ok = 0;
+    if (s.pos && a.window != INT32_MAX) {
+        for (int r = 0; r < 32; ++r) {
+            const AttRow row{__builtin_amdgcn_readlane(me.i, r), __builtin_amdgcn_readlane(me.p, r), __builtin_amdgcn_readlane(me.doc, r)};
+            const uint64_t bits = __ballot(att_sees(row, s.prefix, a.window, j0 + lane, kp, kdoc));
+            ok = (lane & 31) == r ? bits : ok;
+        }
+        return ok;
+    }
+    for (uint64_t left = __ballot(kdoc >= 0); left;) { // a step for each of the keys' documents, of which there are few
+        const int one = __builtin_amdgcn_readlane(kdoc, __builtin_ctzll(left));
+        const uint64_t bits = __ballot(kdoc == one);
+        ok = me.doc == one ? bits : ok;
+        left &= ~bits;
+    }
+    const int up = me.i - j0, from = up >= a.window ? up - a.window + 1 : 0, pre = s.prefix - j0;
+    uint64_t reach = up >= 63 ? ~0ull : up < 0 ? 0 : (2ull << up) - 1;
+    reach = from > 63 ? 0 : reach >> from << from;
+    reach |= pre > 63 ? ~0ull : pre <= 0 ? 0 : (1ull << pre) - 1;
+    return ok & reach;
+}
+// bits of any of the wavefront's rows (lane i has those of row i & 31), a scalar
+__device__ __forceinline__ uint64_t att_rows_or(uint64_t bits) {
+    uint32_t w[2] = {(uint32_t)bits, (uint32_t)(bits >> 32)};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        w[i] |= __builtin_amdgcn_mov_dpp(w[i], 0x128, 0xf, 0xf, true);         // 16 lanes turned by 8, 4, 2, 1
+        w[i] |= __builtin_amdgcn_mov_dpp(w[i], 0x124, 0xf, 0xf, true);
+        w[i] |= __builtin_amdgcn_mov_dpp(w[i], 0x122, 0xf, 0xf, true);
+        w[i] |= __builtin_amdgcn_mov_dpp(w[i], 0x121, 0xf, 0xf, true);
+        const auto r = __builtin_amdgcn_permlane16_swap(w[i], w[i], false, false);
+        w[i] = __builtin_amdgcn_readfirstlane(r[0] | r[1]);
+    }
+    return ((uint64_t)w[1] << 32) | w[0];
+}
+
+
 // 16 bytes a lane from memory to LDS: lane i's go to dst + 16 i (dst is uniform).  In assembly, since the compiler lets the
 // transposing LDS reads wait for every such copy on the way, also those to other buffers (vmcnt(0) in front of each block's second
 // product: 954 us for a prompt of 8192 with 32 heads).  The caller waits (vmcnt) before the barrier behind which the copy is read;

@@ -28,21 +28,6 @@ __device__ __forceinline__ float half_sum(float v) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// bits of any of the wavefront's rows (lane i has those of row i & 31), a scalar
-__device__ __forceinline__ uint64_t rows_or(uint64_t bits) {
-    uint32_t w[2] = {(uint32_t)bits, (uint32_t)(bits >> 32)};
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        w[i] |= __builtin_amdgcn_mov_dpp(w[i], 0x128, 0xf, 0xf, true);         // 16 lanes turned by 8, 4, 2, 1
-        w[i] |= __builtin_amdgcn_mov_dpp(w[i], 0x124, 0xf, 0xf, true);
-        w[i] |= __builtin_amdgcn_mov_dpp(w[i], 0x122, 0xf, 0xf, true);
-        w[i] |= __builtin_amdgcn_mov_dpp(w[i], 0x121, 0xf, 0xf, true);
-        const auto r = __builtin_amdgcn_permlane16_swap(w[i], w[i], false, false);
-        w[i] = __builtin_amdgcn_readfirstlane(r[0] | r[1]);
-    }
-    return ((uint64_t)w[1] << 32) | w[0];
-}
-
 // Workgroups are dealt round-robin to the 8 XCDs, units (sequence, key-value head) to workgroups, so that an XCD keeps to
 // some units at a time, as few as keep it busy: their rows walk over the same keys and values at about the same time, which
 // its own L2 then has (all units at once: 770 us for a prompt of 8192 with 32 heads, bound by what lies behind the L2).
@@ -263,31 +248,6 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
             }
         }
     };
-    // cap and bias (without either, scores stay products until their weights are taken); j0: the tile's first key
-    auto transform = [&](v16f& sc, int k, int j0, int kp) {
-        if (a.capped != 0.f) {
-            const float C = a.capped, c3 = a.c2 * (2.f * ATT_LOG2E);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                if constexpr (BF)                      // (an error of 1e-7 of the cap: weights are rounded to 8 bits)
-                    sc[r] = fmaf(-2.f * C, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(sc[r] * c3)), C);
-                else
-                    sc[r] = C * att_tanh(sc[r] * a.c2);
-            }
-        } else {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) sc[r] *= a.c1;
-        }
-        if (a.slopes && s.pos) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                sc[r] = fmaf(-slope, fabsf((float)(me.p - __shfl(kp, k * 32 + (r & 3) + 8 * (r >> 2) + 4 * hf, 64))), sc[r]);
-        } else if (a.slopes) {
-            const float away = (float)(me.p - j0 - 4 * hf);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) sc[r] = fmaf(-slope, fabsf(away - (float)((r & 3) + 8 * (r >> 2))), sc[r]);
-        }
-    };
     // weights of a tile's scores, and their sums; low: what the weights lose when rounded
     auto weigh = [&](const v16f& sc, Packed& out, auto low) {
         const float c1 = GENERAL ? 1.f : a.c1, base = m == -INFINITY ? 0.f : m;
@@ -404,28 +364,8 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
         const bool mine = me.doc == doc;
         uint64_t ok = ALL, any = ALL;
         if (__builtin_expect(!even, 0)) {
-            ok = any = 0;
-            if (s.pos && a.window != INT32_MAX) {
-                for (int r = 0; r < 32; ++r) {
-                    const AttRow row{__builtin_amdgcn_readlane(me.i, r), __builtin_amdgcn_readlane(me.p, r), __builtin_amdgcn_readlane(me.doc, r)};
-                    const uint64_t bits = __ballot(att_sees(row, s.prefix, a.window, j0 + lane % BK, now.p, now.doc)) & ALL;
-                    any |= bits;
-                    ok = l32 == r ? bits : ok;
-                }
-            } else {                                   // a step for each of the keys' documents, of which there are few
-                for (uint64_t left = __ballot(now.doc >= 0) & ALL; left;) {
-                    const int one = __builtin_amdgcn_readlane(now.doc, __builtin_ctzll(left));
-                    const uint64_t bits = __ballot(now.doc == one) & ALL;
-                    ok = me.doc == one ? bits : ok;
-                    left &= ~bits;
-                }
-                const int up = me.i - j0, from = up >= a.window ? up - a.window + 1 : 0, pre = s.prefix - j0;
-                uint64_t reach = up >= 63 ? ~0ull : up < 0 ? 0 : (2ull << up) - 1;
-                reach = from > 63 ? 0 : reach >> from << from;
-                reach |= pre > 63 ? ~0ull : pre <= 0 ? 0 : (1ull << pre) - 1;
-                ok &= reach;
-                any = rows_or(ok);
-            }
+            ok = att_seen(a, s, me, j0, now.p, now.doc) & ALL;
+            any = att_rows_or(ok);
             uint64_t* const seen = (uint64_t*)(smem + 4 * S::TILE + AT_MAP / 8 + 2 * AT_WAVES * 4);
             if (lane == 0) seen[wave] = any;
             bwla_lds_barrier();
@@ -442,7 +382,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
             const bool whole = even && att_uniform(__all(mine | blind)) && (j0 + BK - 1 <= w_first || j0 + BK <= s.prefix);
             // a tile's scores made ready: cap, bias, mask, and a maximum that will do for them
             auto ready = [&](v16f& sc, int k, auto first) {
-                if constexpr (GENERAL) transform(sc, k, j0 + k * 32, now.p);
+                if constexpr (GENERAL) att_transform<BF>(a, sc, me.p, slope, j0, k, now.p, s.pos != nullptr);
                 bool fine = false;
                 if (__builtin_expect(whole, 1)) {
                     had += 16;

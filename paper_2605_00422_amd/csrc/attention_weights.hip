@@ -14,24 +14,31 @@ typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
 template <bool BF, int DP>
 struct WtShape {
-    static constexpr int KT = (BF ? DP : 2 * DP) > 256 ? 1 : 2;        // tiles of 32 keys of a wavefront
+    static constexpr int ES = BF ? 2 : 4;
+    static constexpr int KT = BF && DP <= 128 ? 2 : 1;                  // tiles of 32 keys of a wavefront
     static constexpr int KEYS = 32 * KT * WT_WAVES;                     // cached tokens of a workgroup
+    static constexpr int RT = BF ? 2 : 1, ROWS = 32 * RT;               // tiles of rows, and rows, of a step
+    static constexpr int ROWB = DP * ES, CH = ROWB / 16;                // bytes and 16-byte pieces of a row in LDS
+    static constexpr int TILE = ROWS * ROWB;
+    static constexpr int COPIES = ROWS * CH / (64 * WT_WAVES);
+    static constexpr int LDS = 2 * TILE;
 };
 
-template <bool BF, int DP, bool EXACT>
-__global__ __launch_bounds__(64 * WT_WAVES, DP * (BF ? 1 : 2) > 128 ? 1 : 2) void att_weights_kernel(AttArgs a, int parts, int64_t pitch, float* __restrict__ sums) {
-    constexpr int ES = BF ? 2 : 4, CH = DP * ES / 16, KT = WtShape<BF, DP>::KT;
+// GENERAL: a cap or a bias
+template <bool BF, int DP, bool EXACT, bool GENERAL>
+__global__ __launch_bounds__(64 * WT_WAVES, BF ? (DP <= 128 ? 3 : 2) : DP == 256 ? 1 : 2) void att_weights_kernel(AttArgs a, int parts, int64_t pitch, float* __restrict__ sums) {
+    using S = WtShape<BF, DP>;
+    constexpr int ES = S::ES, KT = S::KT, RT = S::RT, ROWS = S::ROWS, CH = S::CH, CS = CH / 2, KSW = (CH < 16 ? CH : 16) - 1;
+    extern __shared__ __align__(16) char qs[];          // [2][ROWS][ROWB], pieces of a row at piece ^ (row & KSW)
     const int lane = threadIdx.x & 63, wave = att_wave(), l32 = lane & 31, hf = lane >> 5;
     const int h = blockIdx.y, b = blockIdx.z / parts, part = blockIdx.z - b * parts;
     const AttSeq s = att_seq(a, b);
-    const int j0 = (blockIdx.x * WT_WAVES + wave) * 32 * KT;
-    if (j0 >= s.n) return;                             // (no barrier in this kernel)
+    const int g0 = blockIdx.x * S::KEYS, j0 = g0 + wave * 32 * KT;
+    if (g0 >= s.n) return;
     const int rows = s.fresh * a.group, old = s.n - s.fresh;
     const int slot_mask = (1 << a.page_shift) - 1;
 
-    v4u kf[KT][CH / 2];
-    AttKey key[KT];                                    // lane l32 knows key l32 of each tile
-    bool all = true;
+    v4u kf[KT][CS];
 #pragma unroll
     for (int k = 0; k < KT; ++k) {
         const int j = min(j0 + k * 32 + l32, s.n - 1);
@@ -39,94 +46,140 @@ __global__ __launch_bounds__(64 * WT_WAVES, DP * (BF ? 1 : 2) > 128 ? 1 : 2) voi
         const bool there = (unsigned)p < (unsigned)a.pages;
         const char* src = a.k + (int64_t)(there ? p : 0) * a.page_bytes + (int64_t)h * a.head_bytes + (int64_t)(j & slot_mask) * a.slot_bytes;
 #pragma unroll
-        for (int c = 0; c < CH / 2; ++c) {
+        for (int c = 0; c < CS; ++c) {
             const int at = (2 * c + hf) * 16;
             kf[k][c] = EXACT || at < a.d * ES ? *(const v4u*)(src + at) : v4u{0, 0, 0, 0};
         }
-        key[k] = att_key(a, s, j0 + k * 32 + l32, there);
-        all &= key[k].doc >= 0;
     }
-    // keys that every row from some index on sees (without documents, or with a window to keep to: none)
-    const bool plain = att_uniform(__all(all) & !s.doc & (a.window == INT32_MAX));
+    // lane i knows key i; whether they are keys that every row from some index on sees (without documents, or with a window to keep
+    // to: none)
+    AttKey key;
+    {
+        const int j = j0 + (KT == 2 ? lane : l32);
+        key = att_key(a, s, j, j < s.n && (unsigned)s.table[min(j, s.n - 1) >> a.page_shift] < (unsigned)a.pages);
+    }
+    const bool plain = att_uniform(__all(key.doc >= 0) & !s.doc & (a.window == INT32_MAX));
     float sum[16 * KT];
 #pragma unroll
     for (int e = 0; e < 16 * KT; ++e) sum[e] = 0.f;
 
-    // tokens that can see a key of this wavefront
-    int t0 = j0 < s.prefix ? 0 : max(j0 - old, 0), t1 = s.fresh;
-    if (!s.pos && a.window != INT32_MAX && j0 >= s.prefix) t1 = (int)min((int64_t)t1, (int64_t)j0 + 32 * KT - 1 + a.window - old);
-    const int first = t0 * a.group / 32, tiles = t1 > t0 ? (t1 * a.group + 31) / 32 : 0;
-    // (from the part's first tile at or behind `first`)
-    struct Tile {
-        v4u q[CH / 2];
-        float lse, slope;                              // lse in base 2, +inf where the row sees nothing: its weights are 0
-        int tok;
-        bool live;
+    // tokens that can see a key from j on, up to (not with) the one that sees none of `keys` of them; the workgroup's steps
+    auto from_token = [&](int j) { return j < s.prefix ? 0 : max(j - old, 0); };
+    auto to_token = [&](int j, int keys) {
+        return !s.pos && a.window != INT32_MAX && j >= s.prefix ? (int)min((int64_t)s.fresh, (int64_t)j + keys - 1 + a.window - old) : s.fresh;
     };
-    auto fetch = [&](int tile) {
-        Tile x;
-        const int row = tile * 32 + l32;
-        x.live = row < rows;
-        x.tok = x.live ? row / a.group : 0;
-        const int head = h * a.group + (x.live ? row - x.tok * a.group : 0);
-        const int64_t at = (int64_t)(s.row0 + x.tok);
-        const float lse = a.lse[at * a.hq + head] * ATT_LOG2E;
-        x.lse = x.live & (lse != -INFINITY) ? lse : INFINITY;
-        x.slope = a.slopes ? a.slopes[head] * ATT_LOG2E : 0.f;
-        const char* qp = a.q + at * a.q_bytes + (int64_t)head * a.d * ES;
+    const int t0 = from_token(g0), t1 = to_token(g0, S::KEYS);
+    const int first = t0 * a.group / ROWS, steps = t1 > t0 ? (t1 * a.group + ROWS - 1) / ROWS : 0;
+    const int w_row0 = from_token(j0) * a.group, w_row1 = j0 < s.n ? to_token(j0, 32 * KT) * a.group : 0;
+    const uint32_t magic = (uint32_t)((0x100000000ull + a.group - 1) / a.group);       // 2^32 / group (group 1: 0, and not used)
+    auto token_of = [&](int row) {
+        if (a.group == 1) return row;
+        const int t = (int)__umulhi((uint32_t)row, magic);                             // at most one too many
+        return t * a.group > row ? t - 1 : t;
+    };
+    const int head0 = h * a.group;
+    auto head_of = [&](int row, int t) { return head0 + row - t * a.group; };
+
+    const int piece = lane % CH, key0 = (wave * 64 + lane) / CH;
+    const uint32_t lds0 = att_lds_address(qs + wave * 1024);
+    auto copy = [&](int step, int buf) {               // (rows behind the last one: the last one's, which count for nothing)
+        att_each(std::make_integer_sequence<int, S::COPIES>{}, [&](auto n) {
+            constexpr int i = decltype(n)::value;
+            const int r = key0 + i * (WT_WAVES * 64 / CH), row = min(step * ROWS + r, rows - 1), t = token_of(row);
+            const char* src = a.q + (int64_t)(s.row0 + t) * a.q_bytes + (int64_t)head_of(row, t) * a.d * ES;
+            const int at = (piece ^ (r & KSW)) * 16;
+            if (EXACT || at < a.d * ES) att_copy16<i * WT_WAVES * 1024>(src + at, lds0 + buf * S::TILE);
+        });
+    };
+    if constexpr (!EXACT) {                            // columns that no copy fills count as zero
+        for (int i = threadIdx.x; i < 2 * ROWS * CH; i += 64 * WT_WAVES)
+            if ((i % CH ^ (i / CH & KSW)) * 16 >= a.d * ES) *(v4u*)(qs + i * 16) = v4u{0, 0, 0, 0};
+    }
+    struct Rows {
+        float lse[RT];                                 // in base 2, +inf where the row sees nothing: its weights are 0
+    };
+    auto look = [&](int step) {
+        Rows x;
 #pragma unroll
-        for (int c = 0; c < CH / 2; ++c) {
-            const int col = (2 * c + hf) * 16;
-            x.q[c] = EXACT || col < a.d * ES ? *(const v4u*)(qp + col) : v4u{0, 0, 0, 0};
+        for (int r = 0; r < RT; ++r) {
+            const int row = step * ROWS + r * 32 + l32, in = min(row, rows - 1), t = token_of(in);
+            const float lse = a.lse[(int64_t)(s.row0 + t) * a.hq + head_of(in, t)];
+            x.lse[r] = row < rows ? lse : -INFINITY;
         }
         return x;
     };
-    int tile = first + (part - first % parts + parts) % parts;
-    Tile next;
-    if (tile < tiles) next = fetch(tile);
-    for (; tile < tiles; tile += parts) {
-        const Tile x = next;
-        if (tile + parts < tiles) next = fetch(tile + parts);
-        const auto& qf = x.q;
-        const float lse = x.lse, slope = x.slope;
-        const int first_i = old + tile * 32 / a.group;
-        const bool whole = plain & ((first_i >= j0 + 32 * KT - 1) | (j0 + 32 * KT <= s.prefix));
-        AttRow me{0, 0, 0};
-        if (!whole || a.slopes) me = att_row(s, x.tok, x.live);
+    int step = first + (part - first % parts + parts) % parts;
+    Rows next;
+    if (step < steps) {
+        copy(step, 0);
+        next = look(step);
+    }
+    for (int buf = 0; step < steps; step += parts, buf ^= 1) {
+        __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0): this wavefront's copies of the step are there
+        bwla_lds_barrier();                            // ... everyone's are, and the other buffer is free
+        const Rows x = next;
+        if (step + parts < steps) {
+            copy(step + parts, buf ^ 1);
+            next = look(step + parts);
+        }
+#pragma unroll 1
+        for (int r = 0; r < RT; ++r) {
+            const int row0 = step * ROWS + r * 32;
+            if (att_uniform(row0 + 31 < w_row0 || row0 >= w_row1)) continue;
+            float lse = (RT == 2 && r ? x.lse[RT - 1] : x.lse[0]) * ATT_LOG2E;
+            lse = lse == -INFINITY ? INFINITY : lse;
+            const char* src = qs + buf * S::TILE + (r * 32 + l32) * S::ROWB;
+            const int first_i = old + token_of(row0);
+            const bool whole = plain & ((first_i >= j0 + 32 * KT - 1) | (j0 + 32 * KT <= s.prefix));
+            v16f p[KT];
 #pragma unroll
-        for (int k = 0; k < KT; ++k) {
-            v16f p;
+            for (int k = 0; k < KT; ++k)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) p[r] = 0.f;
+                for (int e = 0; e < 16; ++e) p[k][e] = 0.f;
 #pragma unroll
-            for (int c = 0; c < CH / 2; ++c) {
-                if constexpr (BF) {
-                    p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, kf[k][c]), __builtin_bit_cast(v8bf, qf[c]), p, 0, 0, 0);
-                } else {
+            for (int c = 0; c < CS; ++c) {
+                if constexpr (!BF) {                   // (or all would be read ahead, into registers that there are not)
+                    if (c % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                }
+                const v4u q = *(const v4u*)(src + ((2 * c + hf) ^ (l32 & KSW)) * 16);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        p = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[k][c][e]), __uint_as_float(qf[c][e]), p, 0, 0, 0);
+                for (int k = 0; k < KT; ++k) {
+                    if constexpr (BF) {
+                        p[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, kf[k][c]), __builtin_bit_cast(v8bf, q), p[k], 0, 0, 0);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            p[k] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[k][c][e]), __uint_as_float(q[e]), p[k], 0, 0, 0);
+                    }
                 }
             }
-            if (a.capped != 0.f) {
+            AttRow me{0, 0, 0};
+            if (GENERAL || !whole) {
+                const int row = row0 + l32, in = min(row, rows - 1), tok = token_of(in);
+                me = att_row(s, tok, row < rows);
+                if constexpr (GENERAL) {
+                    const float slope = a.slopes ? a.slopes[head_of(in, tok)] * ATT_LOG2E : 0.f;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) p[r] = a.capped * att_tanh(p[r] * a.c2);
-            } else {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) p[r] *= a.c1;
-            }
-            if (!whole || a.slopes) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int from = (r & 3) + 8 * (r >> 2) + 4 * hf;
-                    const int kp = __shfl(key[k].p, from, 64), kd = __shfl(key[k].doc, from, 64);
-                    p[r] = att_sees(me, s.prefix, a.window, j0 + k * 32 + from, kp, kd) ? p[r] - slope * fabsf((float)(me.p - kp)) : -INFINITY;
+                    for (int k = 0; k < KT; ++k) att_transform<BF>(a, p[k], me.p, slope, j0, k, key.p, s.pos != nullptr);
                 }
             }
+            if (__builtin_expect(!att_uniform(whole), 0)) {
+                const uint64_t ok = att_seen(a, s, me, j0, key.p, key.doc);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) sum[k * 16 + r] += __builtin_amdgcn_exp2f(p[r] - lse);
+                for (int k = 0; k < KT; ++k) {
+                    const uint32_t mine = (uint32_t)(ok >> (32 * k)) >> (4 * hf);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) p[k][e] = (mine >> ((e & 3) + 8 * (e >> 2))) & 1 ? p[k][e] : -INFINITY;
+                }
+            }
+            const float c1 = GENERAL ? 1.f : a.c1;
+#pragma unroll
+            for (int k = 0; k < KT; ++k)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sum[k * 16 + e] += __builtin_amdgcn_exp2f(fmaf(p[k][e], c1, -lse));
         }
     }
+    if (j0 >= s.n) return;
     // the 32 lanes' sums: each step halves what a lane holds, so that lane l32 ends with accumulator l32
     if constexpr (KT == 2) {
 #pragma unroll
@@ -168,11 +221,19 @@ __global__ __launch_bounds__(256) void att_weights_add_kernel(AttArgs a, int par
 
 template <bool BF, int DP>
 hipError_t launch(const AttArgs& a, int parts, void* ws, hipStream_t st) {
-    constexpr int keys = WtShape<BF, DP>::KEYS;
+    constexpr int keys = WtShape<BF, DP>::KEYS, lds = WtShape<BF, DP>::LDS;
     const int64_t pitch = (a.max_len + 31) & ~31;
     const dim3 grid((a.max_len + keys - 1) / keys, a.hkv, a.seqs * parts);
-    if (a.d == DP) att_weights_kernel<BF, DP, true><<<grid, 64 * WT_WAVES, 0, st>>>(a, parts, pitch, (float*)ws);
-    else att_weights_kernel<BF, DP, false><<<grid, 64 * WT_WAVES, 0, st>>>(a, parts, pitch, (float*)ws);
+    auto go = [&](auto kernel) {
+        const hipError_t e = bwla_ensure_lds((const void*)kernel, lds);
+        if (e != hipSuccess) return e;
+        kernel<<<grid, 64 * WT_WAVES, lds, st>>>(a, parts, pitch, (float*)ws);
+        return hipGetLastError();
+    };
+    hipError_t e;
+    if (a.capped != 0.f || a.slopes) e = a.d == DP ? go(att_weights_kernel<BF, DP, true, true>) : go(att_weights_kernel<BF, DP, false, true>);
+    else e = a.d == DP ? go(att_weights_kernel<BF, DP, true, false>) : go(att_weights_kernel<BF, DP, false, false>);
+    if (e != hipSuccess) return e;
     if (parts > 1) att_weights_add_kernel<<<dim3((a.max_len + 255) / 256, a.hkv, a.seqs), 256, 0, st>>>(a, parts, pitch, (const float*)ws);
     return hipGetLastError();
 }
@@ -180,14 +241,13 @@ hipError_t launch(const AttArgs& a, int parts, void* ws, hipStream_t st) {
 }  // namespace
 
 AttWeightsPlan bwla_att_weights_plan(const AttArgs& a, int dtype) {
-    const int wide = dtype == BWLA_X_BF16 ? a.d : 2 * a.d;
-    const int64_t keys = (wide > 256 ? 1 : 2) * 32 * WT_WAVES;
+    const bool bf = dtype == BWLA_X_BF16;
+    const int64_t keys = (bf && a.d <= 128 ? 2 : 1) * 32 * WT_WAVES;
     const int64_t groups = (a.max_len + keys - 1) / keys * a.hkv * a.seqs;
-    const int64_t tiles = ((int64_t)a.max_new * a.group + 31) / 32;
-    // parts until there are two workgroups a compute unit, of four steps at least (0.4 us each at 128 columns), one in
-    // fp32 (3.5 us)
+    const int64_t steps = ((int64_t)a.max_new * a.group + (bf ? 63 : 31)) / (bf ? 64 : 32);
+    // parts until there are two workgroups a compute unit, of two steps at least, one in fp32
     int64_t parts = (512 + groups - 1) / groups;
-    const int64_t most = dtype == BWLA_X_BF16 ? tiles / 4 : tiles;
+    const int64_t most = bf ? steps / 2 : steps;
     if (parts > most) parts = most;
     if (parts > 65535 / a.seqs) parts = 65535 / a.seqs;
     AttWeightsPlan p;
