@@ -129,17 +129,14 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
             dmin = min(dmin, range[w]);
             dmax = max(dmax, range[AT_WAVES + w]);
         }
-        // a wavefront looks at 32 blocks, whose word it writes, eight loads at a time on the way
+        // a wavefront looks at 32 blocks, whose word it writes, all loads on the way at once
         for (int w = from / BK / 32 + wave; w < (min(end, AT_MAP) + 31) / 32; w += AT_WAVES) {
             uint32_t word = 0;
+            int d[32];
 #pragma unroll
-            for (int i0 = 0; i0 < 32; i0 += 8) {
-                int d[8];
+            for (int i = 0; i < 32; ++i) d[i] = s.doc[min((w * 32 + i) * BK + lane % BK, s.n - 1)];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) d[i] = s.doc[min((w * 32 + i0 + i) * BK + lane % BK, s.n - 1)];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) word |= __any((d[i] >= dmin) & (d[i] <= dmax)) ? 1u << (i0 + i) : 0u;
-            }
+            for (int i = 0; i < 32; ++i) word |= __any((d[i] >= dmin) & (d[i] <= dmax)) ? 1u << i : 0u;
             if (lane == 0) active[w] = word;
         }
         __syncthreads();
