@@ -481,3 +481,70 @@ def test_refusals_come_as_errors(A):
         A.attention_forward(cache, batch, A.Score(0.1), q, torch.empty_like(q), None, cache.weights())
     with pytest.raises(B.BwlaError):
         A.attention_forward(cache, batch, A.Score(0.1), q, torch.empty_like(q), None, None, None)
+
+
+# ---------------------------------------------------------------- all of it, between two layers
+def test_attention_block_against_the_oracle_step_by_step(A):
+    """A prompt, its cache cut, a decoding step: each operator's outputs against the oracle's on what it read (bf16, all of a
+    kernel's bounds as above); the layers on either side are other tests' matter."""
+    import torch
+    from paper_2605_00422_amd import attention_block as T
+    hq, hkv, d, page, hidden, m, keep = 4, 2, 64, 16, 512, 200, 40
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    k, v = (torch.full((20, hkv, page, d), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    rope = T.tables(torch, m + 8, d, "cuda")
+    block = T.AttentionBlock(T.random_layer(torch, gen, (hq + 2 * hkv) * d, hidden, 8, "cuda"),
+                             T.random_layer(torch, gen, hidden, hq * d, 8, "cuda"), A.KVCache(k, v), rope, hq)
+    table, length = i32([list(range(13))]), i32([m])
+    cos, sin = rope.cos.cpu().numpy(), rope.sin.cpu().numpy()
+
+    def cached(pages, n):
+        return (np.concatenate([x[p].float().cpu().numpy().transpose(1, 0, 2) for p in pages])[:n] for x in (k, v))
+
+    def check_call(rows, pages, n, position):
+        _, qkv, q, out, lse, _ = block._rows[rows]
+        heads = qkv.cpu().numpy().astype(np.float64).reshape(rows, hq + 2 * hkv, d)
+        turned = orc.rotate(heads[:, :hq + hkv], cos, sin, [position], [d // 2])
+        kb, vb = cached(pages, n)
+        most = np.abs(heads).max()
+        for got, want in ((q.float().cpu().numpy(), turned[:, :hq]), (kb[n - rows:], turned[:, hq:]), (vb[n - rows:], heads[:, hq + hkv:])):
+            assert np.all(np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + 8 * U * most)
+        want, want_lse, sums, vabs, qk, top = orc.attend(q.float().cpu().numpy(), kb, vb, d ** -0.5)
+        rel = np.expm1(4 * (d + 4) * U * qk + 16 * U * top) + (2 * n + 16) * U
+        assert np.all(np.abs(out.float().cpu().numpy() - want) <= vabs * (rel[..., None] + 2.0 ** -9) + np.abs(want) * 2.0 ** -8 + 1e-30)
+        assert np.all(np.abs(lse.cpu().numpy() - want_lse) <= rel + 8 * U * (np.abs(want_lse) + 1))
+        return sums, (rel + 8 * U * (np.abs(want_lse) + top)).max() + (rows * 2 + 8) * U
+
+    x, y = torch.randn(m, hidden, generator=gen, device="cuda").bfloat16(), torch.empty(m, hidden, device="cuda")
+    batch = A.Batch(table, length, i32([0, m]), tokens=m, max_new=m, max_len=m)
+    block(x, batch, i32([list(range(m))]), y)
+    want, bound = check_call(m, range(13), m, list(range(m)))
+    sums = np.concatenate([block.sums[p].cpu().numpy().T for p in range(13)])[:m]
+    assert np.all(np.abs(sums - want) <= want * bound)
+    assert torch.isfinite(y).all()
+    _, _, _, out, _, act = block._rows[m]
+    again = torch.empty_like(y)                        # the output layer read what the attention wrote
+    from paper_2605_00422_amd import binding as B
+    assert torch.equal(y, B.decode_forward(block.o, out.view(m, -1), act, again))
+    stay = orc.kept(sums, keep, 4, 8)
+    k0, v0 = cached(range(13), m)
+    table_out, left = i32([[13, 14, 15, 16]]), i32([0])
+    block.cut(batch, table_out, keep, 4, 8, left)
+    k1, v1 = cached(range(13, 17), keep)
+    assert int(left) == keep and np.array_equal(k1, k0[stay]) and np.array_equal(v1, v0[stay])
+    left += 1
+    x, y = torch.randn(1, hidden, generator=gen, device="cuda").bfloat16(), torch.empty(1, hidden, device="cuda")
+    block(x, A.Batch(table_out, left, max_len=keep + 1), i32([[m]]), y)
+    check_call(1, range(13, 17), keep + 1, [m])
+    assert torch.isfinite(y).all()
+
+
+def test_attention_block_example(A):
+    import torch
+    from paper_2605_00422_amd import attention_block as T
+    ys, lens = T.main()
+    assert [tuple(y.shape) for y in ys] == [(300, 512), (77, 512)] + [(2, 512)] * 16 and all(torch.isfinite(y).all() for y in ys)
+    assert lens.tolist() == [[64 + i, 64 + i] for i in range(1, 17)]
+    again, _ = T.main()
+    assert all(torch.equal(a, b) for a, b in zip(ys, again))
