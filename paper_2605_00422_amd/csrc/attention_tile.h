@@ -28,26 +28,25 @@ __device__ __forceinline__ float half_sum(float v) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Workgroups are dealt round-robin to the 8 XCDs, units (sequence, key-value head) to workgroups, so that an XCD keeps to
-// some units at a time, as few as keep it busy: their rows walk over the same keys and values at about the same time, which
-// its own L2 then has (all units at once: 770 us for a prompt of 8192 with 32 heads, bound by what lies behind the L2).
-// Later tiles of rows see more keys: the longest first, which evens out where there are many workgroups, or, where all run
-// at once, the first half of them from the longest down and the second from the shortest up, so that a compute unit gets a
-// long one and a short one.
+// Workgroups are dealt round-robin to the 8 XCDs, and units (sequence, key-value head) to workgroups, so that the rows of one unit mostly
+// lie on one XCD, whose L2 then has their keys and values.  (A few units at a time instead of all: 795 -> 810 us for a prompt of 8192
+// with 32 heads.)  The parts of a divided cache come one after the other, the first, which all sequences have, in front (all units
+// and parts at once: 296 -> 391 us for four chunks behind caches of 900 to 7001 tokens).  With each tile the units are turned by one
+// an XCD, whose shader engines are dealt workgroups in turn as well: else each of the four has a sequence for itself, and where the
+// shortest is done the next workgroup still waits for its own (297 -> 358 us there).  Later tiles of rows see more keys: the longest
+// first, which evens out where there are many workgroups, or, where all run at once, the first half of them from the longest down
+// and the second from the shortest up, so that a compute unit gets a long one and a short one.
 struct AtOrder {
-    int tiles, units, together, fold;
+    int tiles, units, fold;
 };
-inline AtOrder at_order_of(int tiles, int units, int per_cu) {
-    const int cus = bwla_device_cus(), each = (per_cu * cus / 8 + tiles - 1) / tiles;
-    AtOrder o{tiles, units, 8 * each < units ? 8 * each : units, 0};
-    o.fold = (int64_t)tiles * units <= (int64_t)per_cu * cus;
-    return o;
+inline AtOrder at_order_of(int tiles, int units, int splits, int per_cu) {
+    return AtOrder{tiles, units, (int64_t)tiles * units * splits <= (int64_t)per_cu * bwla_device_cus()};
 }
-__device__ __forceinline__ void at_place(int id, const AtOrder& o, int& unit, int& tile) {
-    const int size = o.together * o.tiles, group = id / size, at = id - group * size;
-    const int width = min(o.together, o.units - group * o.together), k = at / width;
-    unit = group * o.together + at - k * width;
-    const int half = o.tiles / 2;
+__device__ __forceinline__ void at_place(int id, const AtOrder& o, int& split, int& unit, int& tile) {
+    const int size = o.units * o.tiles;
+    split = id / size;
+    const int at = id - split * size, k = at / o.units, half = o.tiles / 2;
+    unit = (int)((unsigned)(at - k * o.units + 8 * k) % (unsigned)o.units);
     tile = o.fold && k >= o.tiles - half ? k - (o.tiles - half) : o.tiles - 1 - k;
 }
 
@@ -72,10 +71,8 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
     char* const ks = smem;                             // [2][BK][ROWB]
     char* const vs = smem + 2 * S::TILE;
 
-    int unit, tile;
-    at_place(blockIdx.x, order, unit, tile);
-    const int units = a.seqs * a.hkv, split = unit / units;
-    unit -= split * units;
+    int split, unit, tile;
+    at_place(blockIdx.x, order, split, unit, tile);
     const int b = unit / a.hkv, h = unit - b * a.hkv;
     const AttSeq s = att_seq(a, b);
     const int rows = s.fresh * a.group;
@@ -407,6 +404,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
                 }
             };
             if constexpr (KT == 2) {
+                // (Priority for what is mostly products over the other wavefronts' sums and copies: 832 -> 808 us.)
                 // The weights of one tile are taken while the other's products run; operands are read ahead.  The compiler has to
                 // be told: left to itself it reads each operand right in front of its product and waits (130 cycles each).
                 v16f s0, s1;
@@ -504,8 +502,8 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
 template <bool BF, int DP>
 hipError_t at_launch(const AttArgs& a, const AttSplit& sp, void* ws, hipStream_t st) {
     const int tiles = (sp.rows + AT_ROWS - 1) / AT_ROWS;
-    const int units = a.seqs * a.hkv * sp.splits;
-    const AtOrder order = at_order_of(tiles, units, DP == 256 ? 1 : 2);
+    const int units = a.seqs * a.hkv;
+    const AtOrder order = at_order_of(tiles, units, sp.splits, DP == 256 ? 1 : 2);
     constexpr int lds = AtShape<BF, DP>::LDS;
     const bool general = a.capped != 0.f || a.slopes, exact = a.d == DP;
     float* const part = (float*)ws;
@@ -513,7 +511,7 @@ hipError_t at_launch(const AttArgs& a, const AttSplit& sp, void* ws, hipStream_t
     auto go = [&](auto kernel) {
         const hipError_t e = bwla_ensure_lds((const void*)kernel, lds);
         if (e != hipSuccess) return e;
-        kernel<<<dim3((unsigned)((int64_t)tiles * units)), 64 * AT_WAVES, lds, st>>>(a, order, sp, part, stat);
+        kernel<<<dim3((unsigned)((int64_t)tiles * units * sp.splits)), 64 * AT_WAVES, lds, st>>>(a, order, sp, part, stat);
         return hipGetLastError();
     };
     if (exact) return general ? go(att_tile_kernel<BF, DP, true, true>) : go(att_tile_kernel<BF, DP, true, false>);

@@ -4,10 +4,10 @@
 
 // Whether the cached tokens are dealt out over several workgroups, whose parts are then added up, and how many go to each:
 // so many that there are workgroups for the whole GPU, where the rows alone make fewer than a third of them (128 tokens behind 8192,
-// 8 key-value heads: 230 -> 48 us; a prompt of 1024 of 16 heads 36 -> 29 us), or half of them and the cache is long (256 workgroups:
-// 67 -> 62 us of 2048 tokens, but 55 -> 63 us of 1500).  Of more workgroups the parts cost more than they bring (384: 399 -> 400 us
-// of 8192 tokens, 59 -> 72 us of 1500), but for chunks of several sequences, whose lengths differ: the longest one's would be the last
-// for long (four of 900 to 7001 tokens, 448 workgroups: 281 -> 228 us, though 370 -> 399 us if all have 8192).
+// 8 key-value heads: 229 -> 45 us; a prompt of 1024 of 16 heads 36 -> 29 us), or half of them and the cache is long (256 workgroups:
+// 67 -> 62 us of 2048 tokens, but 55 -> 56 us of 1500).  Of more workgroups the parts cost as much as they bring (384 workgroups: 401
+// against 399 us of 8192 tokens, 58 against 60 of 1500), but for chunks of several sequences, whose lengths differ: the longest one's
+// would be the last for long (four of 900 to 7001 tokens, 448 workgroups: 275 -> 235 us, though 366 -> 399 us if all have 8192).
 AttSplit bwla_att_tile_split(const AttArgs& a) {
     AttSplit s = {};
     s.rows = a.max_new * a.group;
