@@ -432,7 +432,7 @@ BWLA_API bwla_status_t bwla_probe_load_latency(const void* d_buf, size_t bytes, 
 
 /* Limits (violations give BWLA_ERR_UNSUPPORTED). */
 #define BWLA_MAX_HEAD_DIM 256       /* also a multiple of 8 */
-#define BWLA_MAX_CACHE_LEN (1 << 24) /* tokens of one sequence */
+#define BWLA_MAX_CACHE_LEN (1 << 24) /* tokens of one sequence; a call has fewer rows than this */
 #define BWLA_MAX_HEADS 1024         /* query heads; a multiple of the key-value heads */
 
 /*

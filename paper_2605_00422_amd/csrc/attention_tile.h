@@ -8,7 +8,12 @@
 // weights go from accumulators to operand without leaving the lane.  Its operand V^T comes out of LDS by transposing
 // reads (bf16), or one value a lane (fp32 MFMA contracts two keys an instruction).
 // Keys and values come by asynchronous copies to LDS, one block ahead, 16 bytes a lane, in an order (XOR with the key)
-// that keeps the reads off each other's banks.
+// that keeps the keys' reads off each other's banks.
+// A prompt of 8192 with 32 heads of 128 columns: 757 us, 726 TFLOP/s (a large bf16 product: 1127); a cap 925 us, 64 columns 480 us.
+// Of a SIMD's cycles 37 % are MFMA and 45 % vector instructions (of a row's scores: the test of the maximum, exponential, sum and
+// rounding), which overlap little: two wavefronts a SIMD, 221 registers each, and what one wavefront's order interleaves.  A block of 64 keys takes two
+// workgroups 3.2 us, one alone 2.2; 2048 tokens: 65 us, bound by workgroups of 32 blocks.  Four wavefronts and not eight, which share
+// their copies: 790 against 787 us, with a cap 944 against 1007.
 #pragma once
 #include "attention.h"
 
@@ -503,6 +508,7 @@ template <bool BF, int DP>
 hipError_t at_launch(const AttArgs& a, const AttSplit& sp, void* ws, hipStream_t st) {
     const int tiles = (sp.rows + AT_ROWS - 1) / AT_ROWS;
     const int units = a.seqs * a.hkv;
+    if ((int64_t)tiles * units * sp.splits >= 1 << 24) return hipErrorInvalidConfiguration;       // (a grid has fewer than 2^32 threads)
     const AtOrder order = at_order_of(tiles, units, sp.splits, DP == 256 ? 1 : 2);
     constexpr int lds = AtShape<BF, DP>::LDS;
     const bool general = a.capped != 0.f || a.slopes, exact = a.d == DP;

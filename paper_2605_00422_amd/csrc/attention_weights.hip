@@ -1,10 +1,14 @@
 // Sums of softmax weights per cached token, from queries and the logarithms of their sums.
 //
 // A wavefront keeps the keys of 64 cached tokens (32 where a row is wide) in registers as the stationary operand and
-// walks over the rows (new tokens times the query heads of a group), 32 a step: S^T = K Q^T on 32x32 MFMA, exp2(y - lse)
-// in fp32, added up per lane.  Each cached token belongs to one wavefront, so there is nothing to join but the 32 lanes
+// walks over the rows (new tokens times the query heads of a group): S^T = K Q^T on 32x32 MFMA, exp2(y - lse) in fp32, added up per
+// lane.  The rows come by asynchronous copies to LDS, a step of 64 (fp32: 32) ahead, once for the four wavefronts (each loading
+// its own: 159 -> 99 us below, with the registers that this frees).  Each cached token belongs to one wavefront, so there is nothing to join but the 32 lanes
 // that share its rows, once, at the end, and no atomics.  Where there are few cached tokens for the rows, the rows
 // are dealt out over workgroups whose sums a second launch adds in order.
+// 64 new tokens of four sequences of 6000 to 16384, 64 heads of 8 groups of 128 columns: 84 us, 600 TFLOP/s; of a SIMD's cycles 52 %
+// are vector instructions (fma, exponential, sum for each weight) and 30 % MFMA.  61 fp32 rows a head: 11 us, a chain of loads and
+// fp32 products, and 4 for the second launch.
 #include "attention.h"
 
 namespace {

@@ -7,6 +7,8 @@
 // 16 bytes, from anywhere to anywhere, since the pages written are no others' pages.  In the second launch a thread
 // has a run of neighbouring tokens, whose integers stay in registers up to 32 of them.  Short sequences (EV_SHORT) have
 // their integers made there, too, which spares a launch.
+// 16 sequences of 9000 to 16384 tokens, 8 heads of 128 bf16 columns, cut to 4096: integers 5 us, selection 24 (one workgroup a
+// sequence), copy 112, 4.8 TB/s, what a large copy reaches.  Three of 300 to 601: 8 and 3 us.
 #include "attention.h"
 
 namespace {

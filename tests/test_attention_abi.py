@@ -187,3 +187,14 @@ def test_binding_refuses_wrong_tensors():
         A.rope_append(c, b, A.Rope(torch.zeros(9, 32), torch.zeros(9, 32)), torch.zeros(2, 8 * 64 + 1), i(1, 2), q)
     with pytest.raises(TypeError):
         A.cache_evict(c, b, i(2, 4), c.weights(), 8, 0, 0, i(2), kept=i(2, 9))
+
+
+def test_sizes_that_do_not_fit_the_kernels_counts(lib):
+    out = A.c_size_t()
+    size = lambda b, c=None, hq=16: lib.bwla_attention_workspace_size(A.byref(c or cache()), A.byref(b), hq, 0, A.byref(out))  # noqa: E731
+    assert size(batch(tokens=(1 << 24) - 1)) == B.BWLA_OK
+    assert size(batch(tokens=1 << 24)) == B.BWLA_ERR_UNSUPPORTED
+    many = dict(tokens=(1 << 24) - 1, max_new=(1 << 24) - 1)
+    assert size(batch(**many)) == B.BWLA_OK
+    assert size(batch(**many), cache(kv_heads=1), 1024) == B.BWLA_ERR_UNSUPPORTED      # 2^34 rows
+    assert size(batch(tokens=5, max_new=(1 << 24) - 1), cache(kv_heads=1), 1024) == B.BWLA_OK
