@@ -312,6 +312,21 @@ def test_many_rows_joined(A, layout, lens, news):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,news", [([500], [500]), ([3000], [2]), ([1500], [100])])
+def test_scores_that_rise_along_the_cache(A, dtype, lens, news):
+    """Each key's product with every query is larger than the one before it by enough to move the maximum again and again."""
+    c = Case(dtype, 64, 4, 2, 16, lens, news, seed=24)
+    n = lens[0]
+    step = c.torch.linspace(0.0, 60.0, n)[:, None]
+    k, v = c.kv[0]
+    k[:, :, 0] = step.to(c.T)
+    c.q[:, :, 0] = 8.0
+    for j in range(n):
+        c.k[int(c.table_np[0, j // 16]), :, j % 16, 0] = k[j, :, 0].cuda()
+    check(c, A)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("names", [(), ("prefix",), ("window",), ("position", "window")])
 @pytest.mark.parametrize("run", [1, 5, 40, 200])
 def test_rows_of_several_documents(A, dtype, names, run):
