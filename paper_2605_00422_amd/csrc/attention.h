@@ -165,17 +165,27 @@ __device__ __forceinline__ float att_score(const AttArgs& a, float prod) {
     return a.capped != 0.f ? a.capped * att_tanh(prod * a.c2) : prod * a.c1;
 }
 
+// What the kernels of many rows make of products, an instance each: nothing but the scale, or a cap or a bias.  In bf16 the latter take
+// tanh as 1 - 2 / (1 + exp), whose error is one of the cap, 1.2e-7 of it, and not of the score: up to ATT_SHORT_CAP (128, in base 2)
+// at most 1.5e-5 of a weight, a hundredth of what rounding a weight to bf16 costs.  Above it they take att_tanh, as fp32 does always.
+enum AttForm { ATT_PLAIN, ATT_SHORT, ATT_LONG };
+constexpr float ATT_SHORT_CAP = 128.f * ATT_LOG2E;
+inline AttForm att_form(const AttArgs& a, bool bf) {
+    if (a.capped == 0.f && !a.slopes) return ATT_PLAIN;
+    return bf && a.capped <= ATT_SHORT_CAP ? ATT_SHORT : ATT_LONG;
+}
+
 // Products of 32 keys (rows of the tile) and 32 rows (lanes, in both halves alike) into scores: cap and bias.  (Without either they
 // stay products until their weights are taken.)  The tile's keys are number 32 k .. of those behind j0, of which lane i knows the
 // position of key i; mp: the row's position.
-template <bool BF>
+template <int FORM>
 __device__ __forceinline__ void att_transform(const AttArgs& a, v16f& sc, int mp, float slope, int j0, int k, int kp, bool moved) {
     const int hf = (threadIdx.x >> 5) & 1;
     if (a.capped != 0.f) {
         const float C = a.capped, c3 = a.c2 * (2.f * ATT_LOG2E);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            if constexpr (BF)                          // (an error of 1e-7 of the cap: weights are rounded to 8 bits)
+            if constexpr (FORM == ATT_SHORT)
                 sc[r] = fmaf(-2.f * C, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(sc[r] * c3)), C);
             else
                 sc[r] = C * att_tanh(sc[r] * a.c2);

@@ -66,12 +66,13 @@ struct AtShape {
     static constexpr int LDS = 4 * TILE + AT_MAP / 8 + 2 * AT_WAVES * 4 + 8 * AT_WAVES;    // two blocks of each, a map of blocks, words of the wavefronts
 };
 
-// BF: bf16 (else fp32); DP: columns, 64, 128 or 256; EXACT: d == DP; GENERAL: a cap or a bias
-template <bool BF, int DP, bool EXACT, bool GENERAL>
+// BF: bf16 (else fp32); DP: columns, 64, 128 or 256; EXACT: d == DP; FORM: AttForm, scale, cap and bias
+template <bool BF, int DP, bool EXACT, int FORM>
 __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_kernel(AttArgs a, AtOrder order, AttSplit sp, float* __restrict__ part,
                                                                                 float4* __restrict__ stat) {
     using S = AtShape<BF, DP>;
     constexpr int ES = S::ES, BK = S::BK, ROWB = S::ROWB, CH = S::CH, KT = BK / 32, DT = DP / 32, CS = CH / 2;
+    constexpr bool GENERAL = FORM != ATT_PLAIN;
     extern __shared__ __align__(16) char smem[];
     char* const ks = smem;                             // [2][BK][ROWB]
     char* const vs = smem + 2 * S::TILE;
@@ -381,7 +382,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
             const bool whole = even && att_uniform(__all(mine | blind)) && (j0 + BK - 1 <= w_first || j0 + BK <= s.prefix);
             // a tile's scores made ready: cap, bias, mask, and a maximum that will do for them
             auto ready = [&](v16f& sc, int k, auto first) {
-                if constexpr (GENERAL) att_transform<BF>(a, sc, me.p, slope, j0, k, now.p, s.pos != nullptr);
+                if constexpr (GENERAL) att_transform<FORM>(a, sc, me.p, slope, j0, k, now.p, s.pos != nullptr);
                 bool fine = false;
                 if (__builtin_expect(whole, 1)) {
                     had += 16;
@@ -511,7 +512,8 @@ hipError_t at_launch(const AttArgs& a, const AttSplit& sp, void* ws, hipStream_t
     if ((int64_t)tiles * units * sp.splits >= 1 << 24) return hipErrorInvalidConfiguration;       // (a grid has fewer than 2^32 threads)
     const AtOrder order = at_order_of(tiles, units, sp.splits, DP == 256 ? 1 : 2);
     constexpr int lds = AtShape<BF, DP>::LDS;
-    const bool general = a.capped != 0.f || a.slopes, exact = a.d == DP;
+    const int form = att_form(a, BF);
+    const bool exact = a.d == DP;
     float* const part = (float*)ws;
     float4* const stat = (float4*)((char*)ws + sp.part_bytes);
     auto go = [&](auto kernel) {
@@ -520,8 +522,10 @@ hipError_t at_launch(const AttArgs& a, const AttSplit& sp, void* ws, hipStream_t
         kernel<<<dim3((unsigned)((int64_t)tiles * units * sp.splits)), 64 * AT_WAVES, lds, st>>>(a, order, sp, part, stat);
         return hipGetLastError();
     };
-    if (exact) return general ? go(att_tile_kernel<BF, DP, true, true>) : go(att_tile_kernel<BF, DP, true, false>);
-    return general ? go(att_tile_kernel<BF, DP, false, true>) : go(att_tile_kernel<BF, DP, false, false>);
+    if (form == ATT_PLAIN) return exact ? go(att_tile_kernel<BF, DP, true, ATT_PLAIN>) : go(att_tile_kernel<BF, DP, false, ATT_PLAIN>);
+    constexpr int SHORT = BF ? ATT_SHORT : ATT_LONG;
+    if (form == SHORT) return exact ? go(att_tile_kernel<BF, DP, true, SHORT>) : go(att_tile_kernel<BF, DP, false, SHORT>);
+    return exact ? go(att_tile_kernel<BF, DP, true, ATT_LONG>) : go(att_tile_kernel<BF, DP, false, ATT_LONG>);
 }
 
 }  // namespace

@@ -28,11 +28,12 @@ struct WtShape {
     static constexpr int LDS = 2 * TILE;
 };
 
-// GENERAL: a cap or a bias
-template <bool BF, int DP, bool EXACT, bool GENERAL>
+// FORM: AttForm, scale, cap and bias
+template <bool BF, int DP, bool EXACT, int FORM>
 __global__ __launch_bounds__(64 * WT_WAVES, BF ? (DP <= 128 ? 3 : 2) : DP == 256 ? 1 : 2) void att_weights_kernel(AttArgs a, int parts, int64_t pitch, float* __restrict__ sums) {
     using S = WtShape<BF, DP>;
     constexpr int ES = S::ES, KT = S::KT, RT = S::RT, ROWS = S::ROWS, CH = S::CH, CS = CH / 2, KSW = (CH < 16 ? CH : 16) - 1;
+    constexpr bool GENERAL = FORM != ATT_PLAIN;
     extern __shared__ __align__(16) char qs[];          // [2][ROWS][ROWB], pieces of a row at piece ^ (row & KSW)
     const int lane = threadIdx.x & 63, wave = att_wave(), l32 = lane & 31, hf = lane >> 5;
     const int h = blockIdx.y, b = blockIdx.z / parts, part = blockIdx.z - b * parts;
@@ -164,7 +165,7 @@ __global__ __launch_bounds__(64 * WT_WAVES, BF ? (DP <= 128 ? 3 : 2) : DP == 256
                 if constexpr (GENERAL) {
                     const float slope = a.slopes ? a.slopes[head_of(in, tok)] * ATT_LOG2E : 0.f;
 #pragma unroll
-                    for (int k = 0; k < KT; ++k) att_transform<BF>(a, p[k], me.p, slope, j0, k, key.p, s.pos != nullptr);
+                    for (int k = 0; k < KT; ++k) att_transform<FORM>(a, p[k], me.p, slope, j0, k, key.p, s.pos != nullptr);
                 }
             }
             if (__builtin_expect(!att_uniform(whole), 0)) {
@@ -234,9 +235,12 @@ hipError_t launch(const AttArgs& a, int parts, void* ws, hipStream_t st) {
         kernel<<<grid, 64 * WT_WAVES, lds, st>>>(a, parts, pitch, (float*)ws);
         return hipGetLastError();
     };
+    constexpr int SHORT = BF ? ATT_SHORT : ATT_LONG;
+    const int form = att_form(a, BF);
     hipError_t e;
-    if (a.capped != 0.f || a.slopes) e = a.d == DP ? go(att_weights_kernel<BF, DP, true, true>) : go(att_weights_kernel<BF, DP, false, true>);
-    else e = a.d == DP ? go(att_weights_kernel<BF, DP, true, false>) : go(att_weights_kernel<BF, DP, false, false>);
+    if (form == ATT_PLAIN) e = a.d == DP ? go(att_weights_kernel<BF, DP, true, ATT_PLAIN>) : go(att_weights_kernel<BF, DP, false, ATT_PLAIN>);
+    else if (form == SHORT) e = a.d == DP ? go(att_weights_kernel<BF, DP, true, SHORT>) : go(att_weights_kernel<BF, DP, false, SHORT>);
+    else e = a.d == DP ? go(att_weights_kernel<BF, DP, true, ATT_LONG>) : go(att_weights_kernel<BF, DP, false, ATT_LONG>);
     if (e != hipSuccess) return e;
     if (parts > 1) att_weights_add_kernel<<<dim3((a.max_len + 255) / 256, a.hkv, a.seqs), 256, 0, st>>>(a, parts, pitch, (const float*)ws);
     return hipGetLastError();

@@ -1,0 +1,62 @@
+"""Values that attention calls get now and then: caps far above the scores, queries that are not numbers, calls that leave new
+tokens out.  Oracle, cases and the bounds' derivation as in test_gpu_attention.py."""
+import numpy as np
+import pytest
+
+from oracle import bwla_attention_oracle as orc
+from test_gpu_attention import U, Case
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def A():
+    pytest.importorskip("torch")                       # (in front of the library: one HIP runtime for both)
+    from paper_2605_00422_amd import attention_binding
+    attention_binding.load()
+    return attention_binding
+
+
+def run(c, A, score, batch=None):
+    """out, lse, and the sums of weights of the same call (from 0) and of a call of their own (from 2)."""
+    torch = c.torch
+    cache, batch, q = A.KVCache(c.k, c.v), batch or c.batch(A), c.q.cuda()
+    out, lse = torch.full_like(q, 9.0), torch.full((c.tokens, c.hq), 9.0, device="cuda")
+    sums, alone = cache.weights(), cache.weights() + 2.0
+    scratch = lambda n: torch.full((max(16, n),), 0xff, dtype=torch.uint8, device="cuda")  # noqa: E731
+    A.attention_forward(cache, batch, score, q, out, lse, sums, scratch(A.attention_workspace_size(cache, batch, c.hq, True)))
+    A.attention_weights(cache, batch, score, q, lse, alone, scratch(A.attention_weights_workspace_size(cache, batch, c.hq)))
+    return out.float().cpu().numpy(), lse.cpu().numpy(), sums.cpu().numpy(), alone.cpu().numpy()
+
+
+def of_tokens(c, sums, b):
+    """(cached tokens, heads) of sequence b."""
+    return np.array([sums[c.table_np[b, j // c.page], :, j % c.page] for j in range(c.lens[b])]).reshape(c.lens[b], c.hkv)
+
+
+@pytest.mark.parametrize("cap", [127.0, 129.0, 1e3, 1e5, 1e7, 1e30])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,hq,hkv,lens,news", [(64, 6, 2, [190, 260], [190, 70]), (128, 8, 8, [300], [300]), (64, 8, 2, [900], [3]),
+                                                (128, 4, 1, [1500], [40])])
+def test_caps_far_above_the_scores(A, dtype, cap, d, hq, hkv, lens, news):
+    """A cap is relative to the score: tanh(x) of a small x is x.  x = a scale / cap and C tanh(x) are six roundings, tanh itself is good to
+    six units (below 0.6 to two): 16 U of the score.  bf16 up to a cap of 128: 8 U of the cap, which is 2^-14 at most."""
+    c = Case(dtype, d, hq, hkv, 16, lens, news, seed=31)
+    c.q = (c.q.float() * 4).to(c.T)                    # scores of +-30
+    scale, bf = d ** -0.5, dtype == "bf16"
+    out, lse, sums, alone = run(c, A, A.Score(scale, cap=cap))
+    row = 0
+    for b, (n, new) in enumerate(zip(lens, news)):
+        k, v = (x.float().numpy() for x in c.kv[b])
+        rows = slice(row, row + new)
+        row += new
+        want, want_lse, want_sums, vabs, qk, top = orc.attend(c.q[rows].float().numpy(), k, v, scale, cap=cap)
+        eps = 2 * (d + 4) * U * qk + 16 * U * top + (8 * U * cap if bf and cap <= 128 else 0)
+        rel = np.expm1(2 * eps) + (2 * n + 16) * U
+        bound = vabs * (rel[..., None] + (2.0 ** -9 if bf else 0)) + np.abs(want) * (2.0 ** -8 if bf else 4 * U) + 1e-30
+        assert np.all(np.abs(out[rows] - want) <= bound), np.max(np.abs(out[rows] - want) / bound)
+        most = rel + 8 * U * (np.abs(want_lse) + 1)
+        assert np.all(np.abs(lse[rows] - want_lse) <= most), np.max(np.abs(lse[rows] - want_lse) / most)
+        most = want_sums * ((rel + 8 * U * (np.abs(want_lse) + top)).max() + (new * hq // hkv + 8) * U)
+        assert np.all(np.abs(of_tokens(c, sums, b) - want_sums) <= most + 1e-35)
+        assert np.all(np.abs(of_tokens(c, alone, b) - 2.0 - want_sums) <= most + 2 * U * (2.0 + want_sums))
