@@ -93,13 +93,15 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
     const int tok = live ? row / a.group : 0, head = h * a.group + (live ? row - tok * a.group : 0);
     const AttRow me = att_row(s, tok, live);
     const float slope = GENERAL && a.slopes ? a.slopes[head] * ATT_LOG2E : 0.f;
+    // rows that see nothing whatever the block: what they gather on the way, from queries of 0, is dropped at the end
+    const bool blind = me.doc < 0;
     v4u qf[CS];
     {
         const char* qp = a.q + (int64_t)(s.row0 + tok) * a.q_bytes + (int64_t)head * a.d * ES;
 #pragma unroll
         for (int c = 0; c < CS; ++c) {
             const int at = (2 * c + hf) * 16;
-            qf[c] = live && (EXACT || at < a.d * ES) ? *(const v4u*)(qp + at) : v4u{0, 0, 0, 0};
+            qf[c] = !blind && (EXACT || at < a.d * ES) ? *(const v4u*)(qp + at) : v4u{0, 0, 0, 0};
         }
     }
     // indexes of the first and last row of this wavefront, and of the workgroup
@@ -113,8 +115,6 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
     int lo = s.pos || a.window == INT32_MAX ? 0 : max(g_first - a.window + 1, 0) / BK;
     if (lo < pb) lo = pb;
     const int end = min(max((g_last + BK) / BK, pb), (int)(((int64_t)from + sp.chunk + BK - 1) / BK));
-    // rows that see nothing whatever the block: what they gather on the way is dropped at the end
-    const bool blind = me.doc < 0;
     // documents: the blocks that may hold keys of the rows'
     if (s.doc) {
         uint32_t* const active = (uint32_t*)(smem + 4 * S::TILE);              // a bit for each block that may matter

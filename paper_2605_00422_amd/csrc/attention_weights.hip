@@ -135,7 +135,7 @@ __global__ __launch_bounds__(64 * WT_WAVES, BF ? (DP <= 128 ? 3 : 2) : DP == 256
             lse = lse == -INFINITY ? INFINITY : lse;
             const char* src = qs + buf * S::TILE + (r * 32 + l32) * S::ROWB;
             const int first_i = old + token_of(row0);
-            const bool whole = plain & ((first_i >= j0 + 32 * KT - 1) | (j0 + 32 * KT <= s.prefix));
+            const bool whole = plain & ((first_i >= j0 + 32 * KT - 1) | ((first_i >= 0) & (j0 + 32 * KT <= s.prefix)));
             v16f p[KT];
 #pragma unroll
             for (int k = 0; k < KT; ++k)

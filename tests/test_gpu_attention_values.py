@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from oracle import bwla_attention_oracle as orc
-from test_gpu_attention import U, Case
+from test_gpu_attention import U, Case, check
 
 pytestmark = pytest.mark.gpu
 
@@ -60,3 +60,36 @@ def test_caps_far_above_the_scores(A, dtype, cap, d, hq, hkv, lens, news):
         most = want_sums * ((rel + 8 * U * (np.abs(want_lse) + top)).max() + (new * hq // hkv + 8) * U)
         assert np.all(np.abs(of_tokens(c, sums, b) - want_sums) <= most + 1e-35)
         assert np.all(np.abs(of_tokens(c, alone, b) - 2.0 - want_sums) <= most + 2 * U * (2.0 + want_sums))
+
+
+NOT_NUMBERS = [float("nan"), float("inf")]
+
+
+@pytest.mark.parametrize("value", NOT_NUMBERS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,hq,hkv,lens,news,pad", [(64, 4, 2, [200, 150], [200, 150], 10), (128, 8, 1, [300], [260], 3), (64, 8, 8, [400], [400], 70),
+                                                    (64, 4, 2, [900], [100], 10), (256, 2, 2, [700], [300], 5), (64, 4, 2, [300, 40], [9, 4], 3)])
+def test_padding_that_is_not_a_number(A, dtype, d, hq, hkv, lens, news, pad, value):
+    """The last tokens belong to no document, and neither their queries nor their keys and values are numbers: zeros and -inf come out,
+    and all other rows as if they were not there."""
+    gone = {(b, j) for b, n in enumerate(lens) for j in range(n - pad, n)}
+    c = Case(dtype, d, hq, hkv, 16, lens, news, seed=32, nan_tokens=gone)
+    doc, ends = np.zeros((len(lens), max(lens)), np.int32), np.cumsum(news)
+    for b, n in enumerate(lens):
+        doc[b, n - pad:n] = -1
+        c.q[ends[b] - pad:ends[b]] = value
+    c.options = lambda rng, names: ({"doc": c.i32(doc)}, lambda b: {"doc": doc[b]})
+    out = check(c, A)
+    for end in ends:
+        assert not out[end - pad:end].any()
+
+
+@pytest.mark.parametrize("value", NOT_NUMBERS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,new,prefix", [(70, 75, 70), (130, 140, 128), (3, 5, 2)])
+def test_rows_in_front_of_the_cache_that_are_not_numbers(A, dtype, n, new, prefix, value):
+    """More new tokens than cached ones: the first see nothing, not the prefix either."""
+    c = Case(dtype, 64, 4, 2, 16, [n], [new], seed=33)
+    c.q[:new - n] = value
+    c.options = lambda rng, names: ({"prefix": c.i32([prefix])}, lambda b: {"prefix": prefix})
+    assert not check(c, A)[:new - n].any()
