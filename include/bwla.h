@@ -514,7 +514,7 @@ BWLA_API bwla_status_t bwla_rope_append(const bwla_kv_cache_t* cache, const bwla
  * first).  d_q: tokens rows of q_heads * head_dim, q_stride elements apart; query head h reads key-value
  * head h / (q_heads / kv_heads).  d_out: tokens x q_heads x head_dim, dense; a row that sees nothing is 0.
  * d_lse (may be NULL): tokens x q_heads, the logarithm of the sum of exp(score) over what is seen, -inf
- * where that is nothing.
+ * where that is nothing.  Where a query is NaN and sees something, its row of d_out, its lse and the sums of what it sees are NaN.
  * d_weights (may be NULL; needs d_lse): pages x kv_heads x page_size floats, dense; each seen token's softmax weights,
  * summed over the sequence's new tokens and the query heads of a group, are added at its slot.  A page
  * is named by one sequence only then.

@@ -274,4 +274,19 @@ __device__ __forceinline__ float att_add_bf16(uint32_t x, float c) {
     typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf, x), __builtin_bit_cast(v2bf, 0x3f803f80u), c, false);
 }
+// A row's end.  l: the sum of its weights, 0 where it sees nothing, NaN where a score was (as its output then is: such a row is not
+// taken for one that sees nothing); lr: the sum as above; at: its place, tokens and heads counted through.
+__device__ __forceinline__ float att_over(float l, float lr) { return l == 0.f ? 0.f : 1.f / lr; }
+template <bool BF>
+__device__ __forceinline__ void att_put(const AttArgs& a, int64_t at, int c, float4 v, float over) {
+    const int64_t to = at * a.d + c;
+    if constexpr (BF) *(uint2*)(a.out + to * 2) = make_uint2(att_pack_bf16(v.x * over, v.y * over), att_pack_bf16(v.z * over, v.w * over));
+    else *(float4*)(a.out + to * 4) = make_float4(v.x * over, v.y * over, v.z * over, v.w * over);
+}
+__device__ __forceinline__ void att_put_lse(const AttArgs& a, int64_t at, float m, float l) {
+    if (a.lse) a.lse[at] = l == 0.f ? -INFINITY : (m + __log2f(l)) * ATT_LN2;
+}
+// The maximum that stands for a part whose weights add up to l when parts are joined: fmaxf drops NaN, so that a part of nothing else
+// would have -inf, as one of which nothing is seen.
+__device__ __forceinline__ float att_part_max(float m, float l) { return l != l ? l : m; }
 #endif

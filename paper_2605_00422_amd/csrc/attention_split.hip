@@ -260,6 +260,7 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
     // ---- the four wavefronts' parts, in their order
     l = xor32(xor16(l, false), false);
     lr = BF ? xor32(xor16(lr, false), false) : l;
+    m = att_part_max(m, l);
     if (g == 0) {
         s_m[wave][li] = m;
         s_l[wave][li] = l;
@@ -287,7 +288,7 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
                 *(float4*)&s_o[wave][li][u * 16 * CW + 4 * CW * g + CW * r + c] =
                     make_float4(o[u * CW + c][r] * f, o[u * CW + c + 1][r] * f, o[u * CW + c + 2][r] * f, o[u * CW + c + 3][r] * f);
     if (wave == 0 && g == 0) {
-        if (parts) stat[at_part * 16 + li] = make_float4(mm, ll, llr, 0.f);
+        if (parts) stat[at_part * 16 + li] = make_float4(att_part_max(mm, ll), ll, llr, 0.f);
         s_mm[li] = mm;
         s_ll[li] = ll;
         s_llr[li] = llr;
@@ -306,12 +307,10 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
         if (parts) {
             if (rt * 16 + r < rows) *(float4*)(part + (at_part * 16 + r) * DP + c) = v;
         } else if (rt * 16 + r < rows && c < a.d) {
-            const float total = s_ll[r], inv = total > 0.f ? 1.f / s_llr[r] : 0.f;
             const int t = (rt * 16 + r) / a.group, hd = h * a.group + rt * 16 + r - t * a.group;
-            const int64_t at = ((int64_t)(s.row0 + t) * a.hq + hd) * a.d + c;
-            if constexpr (BF) *(uint2*)(a.out + at * 2) = make_uint2(att_pack_bf16(v.x * inv, v.y * inv), att_pack_bf16(v.z * inv, v.w * inv));
-            else *(float4*)(a.out + at * 4) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-            if (c == 0 && a.lse) a.lse[(int64_t)(s.row0 + t) * a.hq + hd] = total > 0.f ? (s_mm[r] + __log2f(total)) * ATT_LN2 : -INFINITY;
+            const int64_t at = (int64_t)(s.row0 + t) * a.hq + hd;
+            att_put<BF>(a, at, c, v, att_over(s_ll[r], s_llr[r]));
+            if (c == 0) att_put_lse(a, at, s_mm[r], s_ll[r]);
         }
     }
 }
@@ -387,12 +386,10 @@ __global__ __launch_bounds__(GROUPS * DP / 4) void att_join_kernel(AttArgs a, At
         const float4 p = *(const float4*)&s_o[i][c];
         v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
     }
-    const float inv = l > 0.f ? 1.f / lr : 0.f;
     const int t = row / a.group, hd = h * a.group + row - t * a.group;
-    const int64_t at = ((int64_t)(s.row0 + t) * a.hq + hd) * a.d + c;
-    if constexpr (BF) *(uint2*)(a.out + at * 2) = make_uint2(att_pack_bf16(v.x * inv, v.y * inv), att_pack_bf16(v.z * inv, v.w * inv));
-    else *(float4*)(a.out + at * 4) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-    if (c == 0 && a.lse) a.lse[(int64_t)(s.row0 + t) * a.hq + hd] = l > 0.f ? (m + __log2f(l)) * ATT_LN2 : -INFINITY;
+    const int64_t at = (int64_t)(s.row0 + t) * a.hq + hd;
+    att_put<BF>(a, at, c, v, att_over(l, lr));
+    if (c == 0) att_put_lse(a, at, m, l);
 }
 
 // The same where rows are many and splits few: DP / 4 threads a row, which take the splits in turn.
@@ -420,12 +417,10 @@ __global__ __launch_bounds__(256) void att_join_rows_kernel(AttArgs a, AttSplit 
         lr += x.z * f;
         v.x += p.x * f; v.y += p.y * f; v.z += p.z * f; v.w += p.w * f;
     }
-    const float inv = l > 0.f ? 1.f / lr : 0.f;
     const int t = row / a.group, hd = h * a.group + row - t * a.group;
-    const int64_t to = ((int64_t)(s.row0 + t) * a.hq + hd) * a.d + c;
-    if constexpr (BF) *(uint2*)(a.out + to * 2) = make_uint2(att_pack_bf16(v.x * inv, v.y * inv), att_pack_bf16(v.z * inv, v.w * inv));
-    else *(float4*)(a.out + to * 4) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-    if (c == 0 && a.lse) a.lse[(int64_t)(s.row0 + t) * a.hq + hd] = l > 0.f ? (m + __log2f(l)) * ATT_LN2 : -INFINITY;
+    const int64_t to = (int64_t)(s.row0 + t) * a.hq + hd;
+    att_put<BF>(a, to, c, v, att_over(l, lr));
+    if (c == 0) att_put_lse(a, to, m, l);
 }
 
 // The rows' weights of each cached token, from the scores that the first launch left, added to the token's sum.  A thread

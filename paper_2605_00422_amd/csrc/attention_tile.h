@@ -478,7 +478,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
     if (!live) return;
     if (!whole_length) {                               // in tiles of 16 rows, as the join reads them
         const int64_t to = ((int64_t)(unit * sp.row_tiles + row / 16) * sp.splits + split) * 16 + row % 16;
-        if (hf == 0) stat[to] = make_float4(blind ? -INFINITY : m, l, lr, 0.f);
+        if (hf == 0) stat[to] = make_float4(blind ? -INFINITY : att_part_max(m, l), l, lr, 0.f);
         if (m != -INFINITY) {
 #pragma unroll
             for (int d = 0; d < DT; ++d)
@@ -488,21 +488,16 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
         }
         return;
     }
-    const float inv = lr > 0.f ? 1.f / lr : 0.f;
-    const int64_t at = ((int64_t)(s.row0 + tok) * a.hq + head);
-    char* const dst = a.out + at * a.d * ES;
+    const float over = att_over(l, lr);
+    const int64_t at = (int64_t)(s.row0 + tok) * a.hq + head;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
             const int c = 32 * d + 2 * r + 4 * hf;
-            if (EXACT || c < a.d) {
-                if constexpr (BF) *(uint2*)(dst + c * 2) = make_uint2(att_pack_bf16(o[d][r] * inv, o[d][r + 1] * inv),
-                                                                      att_pack_bf16(o[d][r + 2] * inv, o[d][r + 3] * inv));
-                else *(float4*)(dst + c * 4) = make_float4(o[d][r] * inv, o[d][r + 1] * inv, o[d][r + 2] * inv, o[d][r + 3] * inv);
-            }
+            if (EXACT || c < a.d) att_put<BF>(a, at, c, make_float4(o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]), over);
         }
-    if (hf == 0 && a.lse) a.lse[at] = l > 0.f ? (m + __log2f(l)) * ATT_LN2 : -INFINITY;
+    if (hf == 0) att_put_lse(a, at, m, l);
 }
 
 template <bool BF, int DP>

@@ -176,6 +176,14 @@ __global__ __launch_bounds__(64 * WT_WAVES, BF ? (DP <= 128 ? 3 : 2) : DP == 256
 #pragma unroll
                     for (int e = 0; e < 16; ++e) p[k][e] = (mine >> ((e & 3) + 8 * (e >> 2))) & 1 ? p[k][e] : -INFINITY;
                 }
+                // a row whose sum is NaN makes NaN of what it sees, and of nothing else
+                if (__builtin_expect(att_uniform(__any(lse != lse)), 0)) {
+#pragma unroll
+                    for (int k = 0; k < KT; ++k)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) p[k][e] = lse != lse && p[k][e] != -INFINITY ? lse : p[k][e];
+                    lse = lse != lse ? INFINITY : lse;
+                }
             }
             const float c1 = GENERAL ? 1.f : a.c1;
 #pragma unroll

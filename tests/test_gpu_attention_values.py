@@ -93,3 +93,39 @@ def test_rows_in_front_of_the_cache_that_are_not_numbers(A, dtype, n, new, prefi
     c.q[:new - n] = value
     c.options = lambda rng, names: ({"prefix": c.i32([prefix])}, lambda b: {"prefix": prefix})
     assert not check(c, A)[:new - n].any()
+
+
+@pytest.mark.parametrize("value", NOT_NUMBERS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kw", [{}, {"window": 40}])
+@pytest.mark.parametrize("d,hq,hkv,lens,news", [
+    (64, 6, 2, [200, 33], [1, 1]), (64, 6, 2, [200, 33], [3, 2]),              # few rows, one part of the cache each
+    (128, 8, 1, [6000], [2]), (64, 4, 4, [900, 700], [4, 3]),                  # ... and several parts
+    (64, 4, 2, [230, 100], [230, 60]), (256, 2, 1, [130], [90]),               # many rows
+    (128, 4, 1, [900, 300], [60, 40]), (64, 14, 2, [600], [600]),              # ... over parts of the cache
+])
+def test_queries_that_are_not_numbers(A, d, hq, hkv, lens, news, kw, dtype, value):
+    """NaN comes out of the rows whose queries are not numbers, and in the sums of what these rows see; nothing else changes."""
+    c = Case(dtype, d, hq, hkv, 16, lens, news, seed=34)
+    bad, bf = [(news[0] // 2, hq - 1), (sum(news) - 1, 0)], dtype == "bf16"
+    for row, head in bad:
+        c.q[row, head] = value
+    out, lse, sums, alone = run(c, A, A.Score(d ** -0.5, **kw))
+    row = 0
+    with np.errstate(invalid="ignore"):
+        for b, (n, new) in enumerate(zip(lens, news)):
+            k, v = (x.float().numpy() for x in c.kv[b])
+            rows = slice(row, row + new)
+            row += new
+            want, want_lse, want_sums, vabs, qk, top = orc.attend(c.q[rows].float().numpy(), k, v, d ** -0.5, **kw)
+            ok = ~np.isnan(want_lse)
+            eps = 2 * (d + 4) * U * qk + 8 * U * top
+            rel = np.expm1(2 * eps) + (2 * n + 16) * U
+            bound = vabs * (rel[..., None] + (2.0 ** -9 if bf else 0)) + np.abs(want) * (2.0 ** -8 if bf else 4 * U) + 1e-30
+            assert np.array_equal(np.isnan(lse[rows]), ~ok) and np.array_equal(np.isnan(out[rows]).all(-1), ~ok)
+            assert np.all((np.abs(out[rows] - want) <= bound)[ok])
+            assert np.all((np.abs(lse[rows] - want_lse) <= rel + 8 * U * (np.abs(want_lse) + 1))[ok])
+            most = want_sums * ((rel + 8 * U * (np.abs(want_lse) + top))[ok].max(initial=0) + (new * hq // hkv + 8) * U)
+            for got, extra in ((of_tokens(c, sums, b), 1e-35), (of_tokens(c, alone, b) - 2.0, 2 * U * (2.0 + want_sums))):
+                assert np.array_equal(np.isnan(got), np.isnan(want_sums))
+                assert np.all((np.abs(got - want_sums) <= most + extra)[~np.isnan(want_sums)])
