@@ -453,7 +453,9 @@ typedef struct bwla_kv_cache {
  * d_table[b * table_stride + j / page_size].  d_len[b] counts its cached tokens, the new ones included:
  * they are its last.  Its new tokens are the rows d_first[b] to d_first[b + 1] - 1 of the call's
  * queries; d_first = NULL: one each, row b.  `tokens` is the number of rows, max_new and max_len are at
- * least the most new and the most cached tokens of a sequence (what goes beyond them is left out).
+ * least the most new and the most cached tokens of a sequence.  Where a sequence has more new tokens than max_new, or than there are
+ * rows, the first ones are taken, at the places that they have among all of them; the others are left out, and nothing sees them
+ * but as part of a prefix.
  */
 typedef struct bwla_kv_batch {
     const int32_t* d_table;

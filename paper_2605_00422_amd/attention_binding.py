@@ -107,10 +107,10 @@ class KVCache:
 
 class Batch:
     """The sequences of a call.  table (sequences, pages of the longest) and length (sequences): int32.  first (sequences + 1): the
-    new tokens' rows, or None: one new token each.  tokens, max_new, max_len: rows of the call, most new and most cached
-    tokens of a sequence, known on the host (the tensors are not read here)."""
+    new tokens' rows, or None: one new token each.  tokens, max_new (both with `first`), max_len: rows of the call, most new and most
+    cached tokens of a sequence, known on the host (the tensors are not read here)."""
 
-    def __init__(self, table, length, first=None, tokens=None, max_new=1, max_len=None):
+    def __init__(self, table, length, first=None, tokens=None, max_new=None, max_len=None):
         _types()
         self.table, self.length, self.first = _ints(table, "table", 2), _ints(length, "length", 1), _ints(first, "first", 1)
         n = length.shape[0]
@@ -118,6 +118,8 @@ class Batch:
             raise ValueError("table, length and first belong to different numbers of sequences")
         if first is not None and tokens is None:
             raise ValueError("tokens: the rows of the call")
+        if first is not None and max_new is None:
+            raise ValueError("max_new: the most new tokens of a sequence")
         if max_len is None:
             raise ValueError("max_len: the most cached tokens of a sequence")
         self.sequences, self.tokens = n, int(n if tokens is None else tokens)
@@ -125,7 +127,7 @@ class Batch:
         stride = table.stride(0) if n > 1 else table.shape[1]
         if stride < table.shape[1]:
             raise TypeError("rows of the table overlap")
-        self.desc = _Batch(_p(table), _p(length), _p(first), self.tokens, n, stride, int(max_new), self.max_len)
+        self.desc = _Batch(_p(table), _p(length), _p(first), self.tokens, n, stride, 1 if max_new is None else int(max_new), self.max_len)
         self._ref = byref(self.desc)
 
 

@@ -89,9 +89,14 @@ struct EvictArgs {
 hipError_t bwla_launch_evict(const EvictArgs& a, hipStream_t st);
 
 #ifdef __HIPCC__
-// A sequence as the kernels see it: what lies outside the caller's bounds is cut off here, once
+// New tokens of a sequence, all of them, as its length is counted from them.  (A length has 2^24 at most, and so have rows: with this
+// many all rows lie in front of the cache.)
+__device__ __forceinline__ int att_counted(int64_t fresh) { return (int)min(fresh, (int64_t)1 << 25); }
+// A sequence as the kernels see it: what lies outside the caller's bounds is cut off here, once.  Of more new tokens than the call takes
+// the first remain, at their own indexes.
 struct AttSeq {
     int n, fresh, row0;      // cached tokens, new ones among them, first row of q
+    int old;                 // the first new one's index (negative: more new tokens than cached ones)
     int prefix;
     const int32_t *table, *doc, *pos;
 };
@@ -103,11 +108,13 @@ __device__ __forceinline__ AttSeq att_seq(const AttArgs& a, int b) {
         row0 = a.first[b];
         fresh = (int64_t)a.first[b + 1] - row0;
     }
-    if (row0 < 0 || row0 > a.tokens) { row0 = 0; fresh = 0; }
-    if (fresh > a.tokens - row0) fresh = a.tokens - row0;
-    s.fresh = (int)min(max(fresh, (int64_t)0), (int64_t)a.max_new);
+    if (row0 < 0 || row0 > a.tokens || fresh < 0) { row0 = 0; fresh = 0; }
+    s.old = s.n - att_counted(fresh);
+    s.fresh = (int)min(min(fresh, a.tokens - row0), (int64_t)a.max_new);
     s.row0 = (int)row0;
     s.prefix = a.prefix ? min(a.prefix[b], s.n) : 0;
+    // (nothing sees the new tokens that are left out, unless they are in the prefix)
+    if (s.fresh < fresh) s.n = max(max(s.old + s.fresh, s.prefix), 0);
     s.table = a.table + (int64_t)b * a.table_stride;
     s.doc = a.doc ? a.doc + (int64_t)b * a.index_stride : nullptr;
     s.pos = a.pos ? a.pos + (int64_t)b * a.index_stride : nullptr;
@@ -120,7 +127,7 @@ struct AttRow {
 };
 __device__ __forceinline__ AttRow att_row(const AttSeq& s, int t, bool live) {
     AttRow r;
-    r.i = live ? s.n - s.fresh + t : -1;
+    r.i = live ? s.old + t : -1;
     if (r.i < 0) { r.i = -1; r.p = 0; r.doc = -2; return r; }
     r.p = s.pos ? max(s.pos[r.i], 0) : r.i;
     r.doc = s.doc ? s.doc[r.i] : 0;

@@ -56,7 +56,7 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a, int items)
     // the row's sequence: the last one that starts at or before it
     int b = (int)row;
     int64_t r0 = row;
-    int fresh = 1;
+    int fresh = 1, counted = 1;
     if (a.first) {
         int lo = 0, up = a.seqs;                       // first[lo] <= row < first[up], if any
         while (up - lo > 1) {
@@ -69,13 +69,14 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a, int items)
         const int64_t f = (int64_t)a.first[b + 1] - r0;
         if (r0 < 0 || row < r0 || row >= r0 + f) return;                 // a row of no sequence
         fresh = (int)min(f, (int64_t)a.max_new);
+        counted = att_counted(f);
     } else if (b >= a.seqs) {
         return;
     }
     const int t = (int)(row - r0);
     if (t >= fresh) return;
     const int n = min(max(a.len[b], 0), a.max_len);
-    const int j = n - fresh + t;                       // its index in the cache
+    const int j = n - counted + t;                       // its index in the cache
     int page = -1;
     if (j >= 0) page = a.table[(int64_t)b * a.table_stride + (j >> a.page_shift)];
     const bool there = (unsigned)page < (unsigned)a.pages;

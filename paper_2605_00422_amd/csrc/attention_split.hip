@@ -64,7 +64,7 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att_split_kernel(AttArgs a, Att
     const int64_t at_part = (int64_t)unit * sp.splits + split;
     const int c0 = split * sp.chunk, c1 = min(c0 + sp.chunk, s.n);
     // where no position and no row count says otherwise, keys in front of the first row's window are not read
-    const int i_first = s.n - s.fresh + rt * 16 / a.group;
+    const int i_first = max(s.old + rt * 16 / a.group, 0);
     const int skip_to = (s.pos || a.window == INT32_MAX) ? 0 : i_first - a.window + 1;
     const bool none = c0 >= c1 || (c1 <= skip_to && c0 >= s.prefix);
     if (none && parts) {

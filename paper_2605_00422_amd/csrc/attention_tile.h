@@ -105,7 +105,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
         }
     }
     // indexes of the first and last row of this wavefront, and of the workgroup
-    const int old = s.n - s.fresh;
+    const int old = s.old;
     const int w_first = old + min(tile * AT_ROWS + wave * 32, rows - 1) / a.group;
     const int w_last = old + min(tile * AT_ROWS + wave * 32 + 31, rows - 1) / a.group;
     const int g_first = max(old + tile * AT_ROWS / a.group, 0);

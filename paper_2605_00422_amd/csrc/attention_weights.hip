@@ -40,7 +40,7 @@ __global__ __launch_bounds__(64 * WT_WAVES, BF ? (DP <= 128 ? 3 : 2) : DP == 256
     const AttSeq s = att_seq(a, b);
     const int g0 = blockIdx.x * S::KEYS, j0 = g0 + wave * 32 * KT;
     if (g0 >= s.n) return;
-    const int rows = s.fresh * a.group, old = s.n - s.fresh;
+    const int rows = s.fresh * a.group, old = s.old;
     const int slot_mask = (1 << a.page_shift) - 1;
 
     v4u kf[KT][CS];

@@ -198,3 +198,13 @@ def test_sizes_that_do_not_fit_the_kernels_counts(lib):
     assert size(batch(**many)) == B.BWLA_OK
     assert size(batch(**many), cache(kv_heads=1), 1024) == B.BWLA_ERR_UNSUPPORTED      # 2^34 rows
     assert size(batch(tokens=5, max_new=(1 << 24) - 1), cache(kv_heads=1), 1024) == B.BWLA_OK
+
+
+def test_batch_of_rows_asks_for_its_bounds():
+    """One new token each needs neither; with `first` a bound of 1 would leave out all but a sequence's first row."""
+    import torch
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    assert A.Batch(i(2, 4), i(2), max_len=9).desc.max_new == 1
+    with pytest.raises(ValueError):
+        A.Batch(i(2, 4), i(2), first=i(3), tokens=5, max_len=9)
+    assert A.Batch(i(2, 4), i(2), first=i(3), tokens=5, max_new=3, max_len=9).desc.max_new == 3

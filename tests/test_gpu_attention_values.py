@@ -129,3 +129,77 @@ def test_queries_that_are_not_numbers(A, d, hq, hkv, lens, news, kw, dtype, valu
             for got, extra in ((of_tokens(c, sums, b), 1e-35), (of_tokens(c, alone, b) - 2.0, 2 * U * (2.0 + want_sums))):
                 assert np.array_equal(np.isnan(got), np.isnan(want_sums))
                 assert np.all((np.abs(got - want_sums) <= most + extra)[~np.isnan(want_sums)])
+
+
+# ---------------------------------------------------------------- more new tokens than the call takes
+CUT = [  # (cached, new, max_new, rows of the call): sequences with more new tokens than max_new, or than there are rows
+    ([200, 90, 33], [20, 3, 1], 4, 24), ([200, 90], [90, 60], 50, 150), ([600, 500], [300, 200], 130, 500), ([120, 100], [40, 30], 40, 60),
+    ([9, 30], [20, 30], 15, 50), ([40, 40], [30, 10], 30, 30),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("prefix", [0, 150])
+@pytest.mark.parametrize("lens,news,max_new,tokens", CUT)
+def test_more_new_tokens_than_the_call_takes(A, dtype, prefix, lens, news, max_new, tokens):
+    """The first of them come out as if all had been taken; the others' rows stay, and what is stored of them may be anything
+    (in a prefix it is seen)."""
+    first = np.concatenate([[0], np.cumsum(news)])
+    taken = [max(0, min(new, max_new, tokens - int(r0))) for new, r0 in zip(news, first)]
+    left = {(b, j) for b, n in enumerate(lens) for j in range(max(n - news[b] + taken[b], 0), n)} if not prefix else set()
+    c = Case(dtype, 64, 4, 2, 16, lens, news, seed=35, nan_tokens=left)
+    q, per = c.q, [min(prefix, n) for n in lens]
+    c.q, c.tokens = q[:tokens], tokens
+    score = A.Score(0.125, prefix=c.i32(per) if prefix else None)
+    out, lse, sums, _ = run(c, A, score, c.batch(A, max_new=max_new))
+    for b, (n, new) in enumerate(zip(lens, news)):
+        rows = slice(int(first[b]), int(first[b]) + taken[b])
+        rest = slice(rows.stop, min(int(first[b + 1]), tokens))
+        assert (out[rest] == 9).all() and (lse[rest] == 9).all()
+        if not taken[b]:
+            continue
+        k, v = (x.float().numpy() for x in c.kv[b])
+        # all new rows (what the ones that are left out see does not matter), so that indexes are the sequence's
+        doc = np.zeros(n, int)
+        full = np.zeros((new, 4, 64), np.float32)
+        full[:taken[b]] = c.q[rows].float().numpy()
+        finite = lambda x: np.where(np.isfinite(x), x, 0)  # noqa: E731
+        want, want_lse, _, vabs, qk, top = (x[:taken[b]] for x in orc.attend(full, finite(k), finite(v), 0.125, prefix=per[b], doc=doc))
+        rel = np.expm1(4 * 68 * U * qk + 16 * U * top) + (2 * n + 16) * U
+        bf = dtype == "bf16"
+        bound = vabs * (rel[..., None] + (2.0 ** -9 if bf else 0)) + np.abs(want) * (2.0 ** -8 if bf else 4 * U) + 1e-30
+        assert np.all(np.abs(out[rows] - want) <= bound), b
+        some = ~np.isneginf(want_lse)
+        assert np.array_equal(np.isneginf(lse[rows]), ~some)
+        assert np.all((np.abs(lse[rows] - want_lse) <= rel + 8 * U * (np.abs(want_lse) + 1))[some])
+        # each row that sees anything gives its tokens a weight of 1 in all, and heads of a group share a sum
+        got = of_tokens(c, sums, b)
+        assert np.all(np.abs(got.sum(0) - some.sum(0).reshape(2, 2).sum(1)) <= 1e-3 * taken[b])
+        seen = max(n - new + taken[b], per[b], 0)
+        assert not got[seen:].any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rope_append_of_more_new_tokens_than_the_call_takes(A, dtype):
+    import torch
+    lens, news, max_new, tokens, hq, hkv, d, page = [40, 7, 25], [9, 1, 12], 4, 16, 4, 2, 64, 16
+    c = Case(dtype, d, hq, hkv, page, lens, news, seed=36)
+    first = np.concatenate([[0], np.cumsum(news)])
+    c.tokens = tokens
+    rope = A.Rope(torch.ones(50, 32, device="cuda"), torch.zeros(50, 32, device="cuda"))         # (turned by nothing)
+    qkv = torch.randn(tokens, (hq + 2 * hkv) * d, device="cuda").to(c.T).float()
+    pos = torch.arange(tokens, dtype=torch.int32, device="cuda")[None]
+    q, cpos = torch.full((tokens, hq, d), 9.0, dtype=c.T, device="cuda"), torch.full((3, 40), -7, dtype=torch.int32, device="cuda")
+    cache = A.KVCache(c.k, c.v)
+    k, v, w = c.k.float().cpu().numpy(), c.v.float().cpu().numpy(), cache.weights() + 1.0
+    A.rope_append(cache, c.batch(A, max_new=max_new), rope, qkv, pos, q, w, cpos)
+    h, want_w, want_pos = qkv.cpu().numpy().reshape(tokens, -1, d), np.ones(tuple(w.shape)), np.full((3, 40), -7)
+    want_q = np.full((tokens, hq, d), 9.0)
+    for b, (n, new) in enumerate(zip(lens, news)):
+        for t in range(min(new, max_new, tokens - int(first[b]))):
+            row, j = int(first[b]) + t, n - new + t
+            p, s = c.table_np[b, j // page], j % page
+            want_q[row], k[p, :, s], v[p, :, s], want_w[p, :, s], want_pos[b, j] = h[row, :hq], h[row, hq:hq + hkv], h[row, hq + hkv:], 0, row
+    assert np.array_equal(q.float().cpu().numpy(), want_q)
+    assert np.array_equal(c.k.float().cpu().numpy(), k, equal_nan=True) and np.array_equal(c.v.float().cpu().numpy(), v, equal_nan=True)
+    assert np.array_equal(w.cpu().numpy(), want_w) and np.array_equal(cpos.cpu().numpy(), want_pos)
