@@ -480,8 +480,10 @@ hipError_t launch(const AttArgs& a, const AttSplit& s, void* ws, hipStream_t st)
     const dim3 grid((unsigned)groups);
     if (a.d == DP) att_split_kernel<BF, DP, true><<<grid, 64 * SP_WAVES, 0, st>>>(a, s, part, stat, scores);
     else att_split_kernel<BF, DP, false><<<grid, 64 * SP_WAVES, 0, st>>>(a, s, part, stat, scores);
-    if (s.splits > 1) join<BF, DP>(a, s, ws, st);
-    if (scores && a.max_len > 0) att_sum_kernel<<<dim3((a.max_len + 1023) / 1024, a.hkv, a.seqs), 256, 0, st>>>(a, s, scores);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && s.splits > 1) e = join<BF, DP>(a, s, ws, st);
+    if (e != hipSuccess || !scores || a.max_len == 0) return e;            // (what is not there is not added to the sums)
+    att_sum_kernel<<<dim3((a.max_len + 1023) / 1024, a.hkv, a.seqs), 256, 0, st>>>(a, s, scores);
     return hipGetLastError();
 }
 

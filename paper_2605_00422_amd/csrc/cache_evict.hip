@@ -186,13 +186,18 @@ __global__ __launch_bounds__(256) void evict_copy_kernel(EvictArgs a, int pieces
 }  // namespace
 
 hipError_t bwla_launch_evict(const EvictArgs& a, hipStream_t st) {
-    if (a.max_len > EV_SHORT) evict_keys_kernel<<<dim3((a.max_len + 255) / 256, a.seqs), 256, 0, st>>>(a);
+    hipError_t e = hipSuccess;
+    if (a.max_len > EV_SHORT) {
+        evict_keys_kernel<<<dim3((a.max_len + 255) / 256, a.seqs), 256, 0, st>>>(a);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
     if (a.max_len <= EV_SHORT) evict_pick_kernel<2><<<a.seqs, EV_T, 0, st>>>(a);
     else if (a.max_len <= 4 * EV_T) evict_pick_kernel<4><<<a.seqs, EV_T, 0, st>>>(a);
     else if (a.max_len <= 8 * EV_T) evict_pick_kernel<8><<<a.seqs, EV_T, 0, st>>>(a);
     else if (a.max_len <= 16 * EV_T) evict_pick_kernel<16><<<a.seqs, EV_T, 0, st>>>(a);
     else if (a.max_len <= 32 * EV_T) evict_pick_kernel<32><<<a.seqs, EV_T, 0, st>>>(a);
     else evict_pick_kernel<0><<<a.seqs, EV_T, 0, st>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;                   // (a list that was not made is not followed)
     const int pieces = a.row_bytes / 16;
     const int64_t work = (int64_t)(a.keep < a.max_len ? a.keep : a.max_len) * pieces;
     if (work > 0) evict_copy_kernel<<<dim3((unsigned)((work + 255) / 256), a.hkv, a.seqs), 256, 0, st>>>(a, pieces);

@@ -208,3 +208,60 @@ def test_batch_of_rows_asks_for_its_bounds():
     with pytest.raises(ValueError):
         A.Batch(i(2, 4), i(2), first=i(3), tokens=5, max_len=9)
     assert A.Batch(i(2, 4), i(2), first=i(3), tokens=5, max_new=3, max_len=9).desc.max_new == 3
+
+
+# What the library calls of the runtime to launch, in front of the real one: launches fail on demand, and none reaches a GPU.
+FAILING_LAUNCHES = """
+static int launches, failing, last;
+void fail_at(int n) { launches = 0; failing = n; last = 0; }
+int launched(void) { return launches; }
+int __hipPushCallConfiguration(void) { return 0; }
+int __hipPopCallConfiguration(void) { return 0; }
+int hipLaunchKernel(void) { return last = ++launches == failing ? 1 : last; }
+int hipGetLastError(void) { int e = last; last = 0; return e; }
+int hipPeekAtLastError(void) { return last; }
+int hipFuncSetAttribute(void) { return 0; }
+int hipGetDevice(int *d) { return *d = 0; }
+"""
+EACH_LAUNCH = """
+import ctypes, sys
+sys.path[:0] = [{root!r}, {tests!r}]
+hip = ctypes.CDLL({stub!r}, ctypes.RTLD_GLOBAL)         # (in front of the library, which finds its functions first)
+import test_attention_abi as t
+from paper_2605_00422_amd import binding as B
+lib = t.A.load()
+hip.fail_at(0)
+assert lib.bwla_probe_empty_launch(None) == B.BWLA_OK and hip.launched() == 1, "launches go past the functions above"
+long, many = dict(c=t.cache(pages=1000), b=t.batch(table_stride=600, max_len=9000)), t.batch(tokens=90, max_new=60, table_stride=600, max_len=9000)
+calls = {{
+    "few rows": (1, lambda: t.forward(lib)), "sums": (2, lambda: t.forward(lib, weights=t.P)),
+    "parts": (2, lambda: t.forward(lib, **long)), "parts, sums": (3, lambda: t.forward(lib, **long, weights=t.P)),
+    "many rows": (1, lambda: t.forward(lib, b=t.batch(tokens=90, max_new=60))),
+    "many rows, parts, sums": (3, lambda: t.forward(lib, long["c"], many, weights=t.P)),
+    "rotation": (1, lambda: t.append(lib)), "eviction": (2, lambda: t.evict(lib)), "long eviction": (3, lambda: t.evict(lib, **long)),
+}}
+for name, (least, call) in calls.items():
+    hip.fail_at(0)
+    status, n = call(), hip.launched()
+    assert status == B.BWLA_OK and n >= least, (name, status, n)
+    for k in range(1, n + 1):
+        hip.fail_at(k)
+        status = call()
+        assert status == B.BWLA_ERR_HIP, (name, "launch", k, "of", n, "failed", status)
+        assert hip.hipGetLastError() == 0, (name, "leaves its error behind")
+        assert hip.launched() == k, (name, "goes on after launch", k)
+"""
+
+
+def test_each_launch_that_fails_is_an_error(lib, tmp_path):
+    import shutil
+    import subprocess
+    import sys
+    if not shutil.which("gcc"):
+        pytest.skip("gcc not available")
+    here, stub = os.path.dirname(os.path.abspath(__file__)), str(tmp_path / "hip_failing.so")
+    (tmp_path / "hip_failing.c").write_text(FAILING_LAUNCHES)
+    subprocess.run(["gcc", "-w", "-shared", "-fPIC", "-o", stub, str(tmp_path / "hip_failing.c")], check=True)
+    run = subprocess.run([sys.executable, "-c", EACH_LAUNCH.format(root=os.path.dirname(here), tests=here, stub=stub)], capture_output=True,
+                         text=True, timeout=100)
+    assert run.returncode == 0, run.stdout + run.stderr
