@@ -123,12 +123,17 @@ class Batch:
         if max_len is None:
             raise ValueError("max_len: the most cached tokens of a sequence")
         self.sequences, self.tokens = n, int(n if tokens is None else tokens)
-        self.max_len = int(max_len)
+        self.max_len, self.columns = int(max_len), table.shape[1]
         stride = table.stride(0) if n > 1 else table.shape[1]
         if stride < table.shape[1]:
             raise TypeError("rows of the table overlap")
         self.desc = _Batch(_p(table), _p(length), _p(first), self.tokens, n, stride, 1 if max_new is None else int(max_new), self.max_len)
         self._ref = byref(self.desc)
+
+    # (The library knows the distance of rows, not how much of it belongs to them: a view may be narrower.)
+    def _fits(self, cache):
+        if self.columns * cache.page_size < self.max_len:
+            raise ValueError("table: too few pages for max_len")
 
 
 class Score:
@@ -141,6 +146,7 @@ class Score:
         self.heads = None if slopes is None else slopes.numel()
         rows = {t.shape[0] for t in (prefix, doc, position) if t is not None}
         self.sequences = None if not rows else rows.pop() if len(rows) == 1 else -1        # (-1: they disagree)
+        self.columns = min((t.shape[1] for t in (doc, position) if t is not None), default=None)
         strides = {t.stride(0) if t.shape[0] > 1 else t.shape[1] for t in (doc, position) if t is not None}
         if len(strides) > 1:
             raise TypeError("doc and position must have rows of one length")
@@ -152,6 +158,8 @@ class Score:
             raise ValueError("slopes: one for each query head")
         if self.sequences is not None and self.sequences != batch.sequences:
             raise ValueError("prefix, doc and position: one row for each sequence")
+        if self.columns is not None and self.columns < batch.max_len:
+            raise ValueError("doc and position: an entry for each of max_len cached tokens")
 
 
 class Rope:
@@ -171,6 +179,7 @@ class Rope:
 
 def _rows(q, cache, batch, what="q"):
     """Query heads and the distance of rows of q: (tokens, q_heads, head_dim), dense but for that distance."""
+    batch._fits(cache)
     shape = q.shape
     if len(shape) != 3 or shape[0] != batch.tokens or shape[2] != cache.head_dim or q.dtype is not cache.dtype:
         raise TypeError(f"{what} must be (tokens, q_heads, head_dim) in the cache's type")
@@ -196,6 +205,8 @@ def rope_append(cache: KVCache, batch: Batch, rope: Rope, qkv, position, q, weig
         raise TypeError("position must be int32, (axes, tokens)")
     if _ints(cache_position, "cache_position", 2) is not None and cache_position.shape[0] != batch.sequences:
         raise ValueError("cache_position: one row for each sequence")
+    if cache_position is not None and cache_position.shape[1] < batch.max_len:
+        raise ValueError("cache_position: an entry for each of max_len cached tokens")
     stride = 0 if cache_position is None else cache_position.stride(0) if batch.sequences > 1 else cache_position.shape[1]
     _ck(load().bwla_rope_append(cache._ref, batch._ref, rope._ref, _p(position), _p(qkv), _b._xdtype(qkv), apart if tokens > 1 else qkv.shape[1], hq,
                                 _p(q), _p(cache._of(weights, "weights")), _p(cache_position), stride, _s()), "bwla_rope_append")
@@ -249,14 +260,19 @@ def cache_evict(cache: KVCache, batch: Batch, table_out, weights, keep: int, sin
     (sequences, pages); length_out gets their number, kept (sequences, keep) their indices, position_out (sequences, keep) their
     entries of position (sequences, at least max_len)."""
     n = batch.sequences
+    batch._fits(cache)
     _ints(table_out, "table_out", 2), _ints(length_out, "length_out", 1)
     if table_out.shape[0] != n or length_out.shape[0] != n:
         raise ValueError("table_out and length_out: one row for each sequence")
+    if table_out.shape[1] * cache.page_size < min(keep, batch.max_len):
+        raise ValueError("table_out: too few pages for keep")
     for t, what in ((kept, "kept"), (position_out, "position_out")):
         if _ints(t, what, 2) is not None and (tuple(t.shape) != (n, keep) or not t.is_contiguous()):
             raise TypeError(f"{what} must be (sequences, keep), dense")
     if _ints(position, "position", 2) is not None and position.shape[0] != n:
         raise ValueError("position: one row for each sequence")
+    if position is not None and position.shape[1] < batch.max_len:
+        raise ValueError("position: an entry for each of max_len cached tokens")
     if keep == 0:                                      # (an empty tensor has no address)
         position = position_out = None
     row = lambda t: 0 if t is None else t.stride(0) if n > 1 else t.shape[1]  # noqa: E731

@@ -265,3 +265,26 @@ def test_each_launch_that_fails_is_an_error(lib, tmp_path):
     run = subprocess.run([sys.executable, "-c", EACH_LAUNCH.format(root=os.path.dirname(here), tests=here, stub=stub)], capture_output=True,
                          text=True, timeout=100)
     assert run.returncode == 0, run.stdout + run.stderr
+
+
+def test_binding_refuses_views_that_are_too_narrow():
+    """Views of wide tensors, whose rows lie far enough apart but do not hold what max_len or keep asks for."""
+    import torch
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    c = A.KVCache(torch.zeros(4, 2, 16, 64), torch.zeros(4, 2, 16, 64))
+    good, narrow = A.Batch(i(2, 9)[:, :4], i(2), max_len=64), A.Batch(i(2, 9)[:, :3], i(2), max_len=49)
+    q, wide, short, rope = torch.zeros(2, 4, 64), i(2, 99), i(2, 99)[:, -63:], A.Rope(torch.zeros(9, 32), torch.zeros(9, 32))
+    qkv, pos, lse, w = torch.zeros(2, 8 * 64), i(1, 2), torch.zeros(2, 4), c.weights()
+    for call in (lambda: A.attention_forward(c, narrow, A.Score(0.1), q, q.clone()),
+                 lambda: A.attention_forward(c, good, A.Score(0.1, doc=short), q, q.clone()),
+                 lambda: A.attention_forward(c, good, A.Score(0.1, position=short), q, q.clone()),
+                 lambda: A.attention_forward(c, good, A.Score(0.1, position=wide, doc=i(2, 99)[:, :63]), q, q.clone()),
+                 lambda: A.attention_weights(c, narrow, A.Score(0.1), q, lse, w),
+                 lambda: A.attention_weights(c, good, A.Score(0.1, doc=short), q, lse, w),
+                 lambda: A.rope_append(c, narrow, rope, qkv, pos, q),
+                 lambda: A.rope_append(c, good, rope, qkv, pos, q, w, short),
+                 lambda: A.cache_evict(c, narrow, i(2, 4), w, 8, 0, 0, i(2)),
+                 lambda: A.cache_evict(c, good, i(2, 9)[:, :2], w, 33, 0, 0, i(2)),
+                 lambda: A.cache_evict(c, good, i(2, 4), w, 8, 0, 0, i(2), position=short, position_out=i(2, 8))):
+        with pytest.raises(ValueError):
+            call()
