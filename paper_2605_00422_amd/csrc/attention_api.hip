@@ -266,7 +266,7 @@ bwla_status_t bwla_cache_evict(const bwla_kv_cache_t* cache, const bwla_kv_batch
     if ((d_position == nullptr) != (d_position_out == nullptr)) return BWLA_ERR_NULL;
     if (d_position && position_stride < batch->max_len) return BWLA_ERR_SHAPE;
     if (batch->sequences == 0) return BWLA_OK;
-    if (!d_len_out || !d_weights || (most > 0 && (!d_table_out || !d_ws))) return BWLA_ERR_NULL;
+    if (!d_len_out || !d_weights || (most > 0 && !d_table_out) || (evict_bytes(batch) > 0 && !d_ws)) return BWLA_ERR_NULL;
     if (off16(d_weights) || off16(d_ws)) return BWLA_ERR_ALIGN;
     if (ws_bytes < evict_bytes(batch)) return BWLA_ERR_BUFSIZE;
     EvictArgs a = {};

@@ -288,3 +288,10 @@ def test_binding_refuses_views_that_are_too_narrow():
                  lambda: A.cache_evict(c, good, i(2, 4), w, 8, 0, 0, i(2), position=short, position_out=i(2, 8))):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("max_len", [60, 3000])
+@pytest.mark.parametrize("ws_bytes", [0, 1 << 40])
+def test_eviction_of_all_needs_its_scratch_as_well(lib, max_len, ws_bytes):
+    """Integers of the weights are made of long sequences whatever is kept of them."""
+    assert evict(lib, b=batch(table_stride=200, max_len=max_len), keep=0, sinks=0, recent=0, ws=None, ws_bytes=ws_bytes) == B.BWLA_ERR_NULL
