@@ -470,8 +470,9 @@ typedef struct bwla_kv_batch {
  * the key's (the index is the position where d_position is NULL):
  *   seen   = the key's page exists, doc[i] = doc[j] >= 0, and (j < prefix or j <= i and p - r < window)
  *   score  = capped(scale q.k) - slope_h |p - r|,  capped(x) = cap tanh(x / cap)
- * cap = 0: no cap; window = 0: none; any pointer may be NULL.  d_slopes has an entry for each query
- * head, d_prefix one for each sequence; d_doc and d_position are sequences x index_stride.
+ * cap = 0: no cap; window = 0: none; any pointer may be NULL.  Scale and cap times log2(e), and scale / cap, are normal fp32 numbers
+ * (else BWLA_ERR_UNSUPPORTED).  d_slopes has an entry for each query head, d_prefix one for each sequence; d_doc and d_position are
+ * sequences x index_stride.
  * Stored keys and values of tokens that a query of the call sees are finite; what lies in slots behind
  * a sequence's length, in pages that no table names, or in tokens that no query of a sequence sees may
  * be anything.

@@ -99,6 +99,8 @@ bwla_status_t attention_args(const bwla_kv_cache_t* c, const bwla_kv_batch_t* b,
     a->c1 = s->scale * ATT_LOG2E;
     a->c2 = s->cap > 0.f ? s->scale / s->cap : 0.f;
     a->capped = s->cap * ATT_LOG2E;
+    // (what the kernels compute with has to be there in fp32: infinite, or rounded to a few bits, it would make NaN or other scores)
+    if (!isnormal(a->c1) || (s->cap > 0.f && (!isnormal(a->c2) || !isnormal(a->capped)))) return BWLA_ERR_UNSUPPORTED;
     return BWLA_OK;
 }
 

@@ -295,3 +295,14 @@ def test_binding_refuses_views_that_are_too_narrow():
 def test_eviction_of_all_needs_its_scratch_as_well(lib, max_len, ws_bytes):
     """Integers of the weights are made of long sequences whatever is kept of them."""
     assert evict(lib, b=batch(table_stride=200, max_len=max_len), keep=0, sinks=0, recent=0, ws=None, ws_bytes=ws_bytes) == B.BWLA_ERR_NULL
+
+
+def test_scales_and_caps_that_fp32_does_not_hold(lib):
+    """In base 2 they, or their ratio, are infinite or have lost bits: a cap of 1e-39 makes 0 * inf of a product of 0."""
+    for kw in (dict(scale=3e38), dict(scale=1e-40), dict(scale=0.1, cap=3e38), dict(scale=0.1, cap=1e-40), dict(scale=1e4, cap=1e-37), dict(scale=1e-4, cap=1e36)):
+        s = score(**kw)
+        assert forward(lib, s=s) == B.BWLA_ERR_UNSUPPORTED, kw
+        assert lib.bwla_attention_weights(byref(cache()), byref(batch()), byref(s), P, 16 * 128, 16, P, P, P, 1 << 40, None) == B.BWLA_ERR_UNSUPPORTED
+    none = batch(sequences=0, tokens=0, d_table=None, d_len=None, d_first=None)
+    for kw in (dict(scale=0.1, cap=1e30), dict(scale=1e-6, cap=1e-6), dict(scale=1e6)):
+        assert forward(lib, b=none, s=score(**kw), q=None, out=None) == B.BWLA_OK, kw
