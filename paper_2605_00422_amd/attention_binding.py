@@ -68,7 +68,7 @@ def _bytes(t) -> int:
 
 def _ints(t, what: str, dims: int):
     """A dense int32 tensor of so many dimensions (rows may be apart), or None."""
-    if t is not None and (t.dtype is not _i32 or t.dim() != dims or (t.stride()[-1] != 1 and t.numel())):
+    if t is not None and (t.dtype is not _i32 or t.dim() != dims or (t.stride()[-1] != 1 and t.shape[-1] > 1 and t.numel())):
         raise TypeError(f"{what} must be an int32 tensor of {dims} dimensions, contiguous in the last")
     return t
 

@@ -306,3 +306,14 @@ def test_scales_and_caps_that_fp32_does_not_hold(lib):
     none = batch(sequences=0, tokens=0, d_table=None, d_len=None, d_first=None)
     for kw in (dict(scale=0.1, cap=1e30), dict(scale=1e-6, cap=1e-6), dict(scale=1e6)):
         assert forward(lib, b=none, s=score(**kw), q=None, out=None) == B.BWLA_OK, kw
+
+
+def test_a_single_element_has_no_stride():
+    """One sequence, one page: views of other tensors, whose last stride says nothing."""
+    import torch
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    b = A.Batch(i(4, 3)[::4, ::3], i(8)[::8], i(9)[::8], tokens=5, max_new=5, max_len=9)
+    assert b.desc.table_stride == 1 and b.sequences == 1
+    assert A.Score(0.1, prefix=i(7)[::7], doc=i(3, 9)[:1, ::9]).sequences == 1
+    with pytest.raises(TypeError):
+        A.Batch(i(4, 6)[:, ::3], i(4), max_len=9)
