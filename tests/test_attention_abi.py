@@ -312,7 +312,7 @@ def test_a_single_element_has_no_stride():
     """One sequence, one page: views of other tensors, whose last stride says nothing."""
     import torch
     i = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
-    b = A.Batch(i(4, 3)[::4, ::3], i(8)[::8], i(9)[::8], tokens=5, max_new=5, max_len=9)
+    b = A.Batch(i(4, 3)[::4, ::3], i(8)[::8], i(2), tokens=5, max_new=5, max_len=9)
     assert b.desc.table_stride == 1 and b.sequences == 1
     assert A.Score(0.1, prefix=i(7)[::7], doc=i(3, 9)[:1, ::9]).sequences == 1
     with pytest.raises(TypeError):
