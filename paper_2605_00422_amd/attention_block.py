@@ -13,55 +13,73 @@ from . import attention_binding as A, binding as B
 
 class AttentionBlock:
     """qkv, o: PackedLayer of the merged projection ((q_heads + 2 kv_heads) head_dim rows) and of the output.  cache: KVCache,
-    bfloat16.  Scores: scale (default head_dim^-1/2), and what else Score takes, per call."""
+    bfloat16.  Scores: scale (default head_dim^-1/2), and what else Score takes, per call.
+    rows: of a call, that room is made for at the start; a call of more makes room for twice as many as before at least, and what was
+    there stays, where captured calls find it (so that all of it is a few times the longest call's).  ws: uint8, scratch of all calls, which
+    raise BwlaError where it is too small for them (attention_binding.*_workspace_size say what they want); without it each takes its own
+    from torch's allocator, a captured call from the graph's.  A block serves one stream at a time."""
 
-    def __init__(self, qkv, o, cache: A.KVCache, rope: A.Rope, q_heads: int, scale=None):
+    def __init__(self, qkv, o, cache: A.KVCache, rope: A.Rope, q_heads: int, scale=None, rows: int = 64, ws=None):
         d = cache.head_dim
         if qkv.desc.N != (q_heads + 2 * cache.kv_heads) * d or o.desc.K != q_heads * d:
             raise ValueError("qkv must have (q_heads + 2 kv_heads) head_dim rows, o q_heads head_dim columns")
         self.qkv, self.o, self.cache, self.rope, self.q_heads = qkv, o, cache, rope, q_heads
         self.scale = d ** -0.5 if scale is None else scale
         self.sums = cache.weights()                    # of the softmax weights that each cached token got
-        self._rows, self._ws = {}, None
+        self._room, self._rows, self._last, self._ws = [], {}, None, ws
+        self._make(rows)
 
-    def _scratch(self, nbytes):
+    def _make(self, M):
         import torch
-        if self._ws is None or self._ws.numel() < nbytes:
-            self._ws = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=self.cache.k.device)
-        return self._ws
+        c = self.cache
+        new = lambda *s, t=torch.float32: torch.empty(M, *s, dtype=t, device=c.k.device)  # noqa: E731
+        self.rows = M
+        self._room.append((B.Activations(self.qkv, M), new(self.qkv.desc.N), new(self.q_heads, c.head_dim, t=c.dtype),
+                           new(self.q_heads, c.head_dim, t=c.dtype), new(self.q_heads), B.Activations(self.o, M)))
+
+    def _scratch(self, size, *args):
+        """size(*args) bytes, where the caller gave none."""
+        if self._ws is not None:
+            return self._ws
+        import torch
+        return torch.empty(max(size(*args), 16), dtype=torch.uint8, device=self.cache.k.device)
 
     def _buffers(self, M):
-        """What a call of M rows writes on the way, kept for the next of as many."""
-        import torch
+        """What a call of M rows writes on the way: the first rows of the room (kept as views until a call of another number)."""
         if M not in self._rows:
-            dev, c = self.cache.k.device, self.cache
-            new = lambda *s, t=torch.float32: torch.empty(*s, dtype=t, device=dev)  # noqa: E731
-            self._rows[M] = (B.Activations(self.qkv, M), new(M, self.qkv.desc.N), new(M, self.q_heads, c.head_dim, t=c.k.dtype),
-                             new(M, self.q_heads, c.head_dim, t=c.k.dtype), new(M, self.q_heads), B.Activations(self.o, M))
+            if M > self.rows:
+                self._make(max(M, 2 * self.rows))
+            act_in, qkv, q, out, lse, act_out = self._room[-1]
+            self._rows = {M: (act_in, qkv[:M], q[:M], out[:M], lse[:M], act_out)}
         return self._rows[M]
 
     def __call__(self, x, batch: A.Batch, position, y, watch: bool = True, **score):
         """x (tokens, columns of qkv), bfloat16 or float32 -> y (tokens, rows of o), float32.  position: int32 (axes, tokens).
         watch: whether the weights that this call's queries give count; the new tokens' sums start at zero either way."""
         act_in, qkv, q, out, lse, act_out = self._buffers(x.shape[0])
+        self._last = batch
         score = A.Score(self.scale, **score)
         B.decode_forward(self.qkv, x, act_in, qkv)
         A.rope_append(self.cache, batch, self.rope, qkv, position, q, self.sums)
-        ws = self._scratch(A.attention_workspace_size(self.cache, batch, self.q_heads, watch))
+        ws = self._scratch(A.attention_workspace_size, self.cache, batch, self.q_heads, watch)
         A.attention_forward(self.cache, batch, score, q, out, lse, self.sums if watch else None, ws)
         return B.decode_forward(self.o, out.view(x.shape[0], -1), act_out, y)
 
     def watch_last(self, batch: A.Batch, last: A.Batch, **score):
         """The sums of weights of a long prompt's last queries alone: batch was the call before, of one sequence (watch=False), whose queries
         are still there; last is the same sequence with its last tokens as the new ones."""
+        if batch is not self._last:
+            raise ValueError("batch is not that of the call before: its queries are gone")
+        if batch.sequences != 1 or last.sequences != 1 or last.tokens > batch.tokens:
+            raise ValueError("one sequence, and the last of its rows")
         _, _, q, _, lse, _ = self._rows[batch.tokens]
-        ws = self._scratch(A.attention_weights_workspace_size(self.cache, last, self.q_heads))
+        ws = self._scratch(A.attention_weights_workspace_size, self.cache, last, self.q_heads)
         A.attention_weights(self.cache, last, A.Score(self.scale, **score), q[batch.tokens - last.tokens:],
                             lse[batch.tokens - last.tokens:], self.sums, ws)
 
     def cut(self, batch: A.Batch, table_out, keep: int, sinks: int, recent: int, length_out):
         """Each sequence's `keep` tokens with the largest sums, its first and last ones among them, to the pages of table_out."""
-        ws = self._scratch(A.cache_evict_workspace_size(self.cache, batch))
+        ws = self._scratch(A.cache_evict_workspace_size, self.cache, batch)
         return A.cache_evict(self.cache, batch, table_out, self.sums, keep, sinks, recent, length_out, ws=ws)
 
 
