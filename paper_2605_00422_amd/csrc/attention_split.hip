@@ -9,7 +9,8 @@
 // gathered from rows of V by byte permutes: lane m reads columns 8m to 8m + 7 of its four keys, whole rows of
 // 256 bytes side by side, and tile c of the result holds columns 8m + c.
 // Softmax: running maximum and sum in fp32 per wavefront, joined over the four wavefronts in LDS and over the
-// splits in att_join_kernel, in a fixed order.  Weights enter the second product in the cache's type.
+// splits in att_join_kernel, in a fixed order.  Weights enter the second product in the cache's type: bf16 ones rounded (by 2^-9 of
+// each at most), as the instruction takes them, and divided by their sum as rounded, rows of few keys as well.
 // Bound by the reads of keys and values: one token behind 32768, 64 heads of 8 groups of 128 columns 25 us, 5.3 TB/s, what a large
 // read reaches, and 5 us for the join; 64 sequences of 500 to 8192 238 us, 4.8 TB/s, with the sums of weights 302 us (the
 // scores, 71 MB, are written here and read again).  Three such sequences of 37 fp32 tokens and 8 heads of 64: 6.5 us, a chain of loads.
@@ -489,6 +490,12 @@ hipError_t launch(const AttArgs& a, const AttSplit& s, void* ws, hipStream_t st)
 
 }  // namespace
 
+// Up to 64 rows of a sequence and key-value head are split over the cache's length here, more go to the tiles.  Up to 16 rows read
+// each key once.  17 to 64 rows read it for each 16, which the tiles do not, but these start later; 64 heads of 8, "/": here, tiles:
+// one sequence of 1024, 4 and 8 new tokens 12.9 / 15.5 and 13.2 / 16.3 us; behind 8192 21.5 / 17.9 and 31 / 20, behind 32768 49 / 32 and 87 /
+// 36; 16 sequences of 8192 161 / 102 and 310 / 107.  Of the tiles' time that is, over 1 to 32 sequences of 64 to 16384 tokens, 0.7 to 3.0
+// in bf16, less than 1 where few sequences have up to 1024; 0.35 to 1 in fp32, but up to 1.3 behind 4096 and more, and up to 2.8 where 32
+// sequences bring 64 rows to each of 32 heads.  (128 rows, one sequence: 14.7 / 18.4, 49 / 24 and 159 / 45 us.)
 bool bwla_att_is_split(const AttArgs& a) { return (int64_t)a.max_new * a.group <= 64; }
 
 AttSplit bwla_att_split(const AttArgs& a, bool weights) {

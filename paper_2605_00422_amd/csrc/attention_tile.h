@@ -9,9 +9,11 @@
 // reads (bf16), or one value a lane (fp32 MFMA contracts two keys an instruction).
 // Keys and values come by asynchronous copies to LDS, one block ahead, 16 bytes a lane, in an order (XOR with the key)
 // that keeps the keys' reads off each other's banks.
-// A prompt of 8192 with 32 heads of 128 columns: 757 us, 726 TFLOP/s (a large bf16 product: 1127); a cap 925 us, 64 columns 480 us.
-// Of a SIMD's cycles 37 % are MFMA and 45 % vector instructions (of a row's scores: the test of the maximum, exponential, sum and
-// rounding), which overlap little: two wavefronts a SIMD, 221 registers each, and what one wavefront's order interleaves.  A block of 64 keys takes two
+// A prompt of 8192 with 32 heads of 128 columns: 684 us, 804 TFLOP/s (a large bf16 product: 1127), in an unbroken row of calls (the first
+// ones after a pause: 745); a cap 833 us, one above 128 1049, a bias 853, 64 columns 410.
+// Of a SIMD's cycles 37 % are MFMA and 50 % vector instructions (of a row's scores: the test of the maximum, exponential, sum and
+// rounding), 11 % both at once: two wavefronts a SIMD, 219 registers each, and what one wavefront's order interleaves.  With a cap 29 %
+// and 65 %: its exponential and reciprocal take twice the cycles of other instructions.  A block of 64 keys takes two
 // workgroups 3.2 us, one alone 2.2; 2048 tokens: 65 us, bound by workgroups of 32 blocks.  Four wavefronts and not eight, which share
 // their copies: 790 against 787 us, with a cap 944 against 1007.
 #pragma once
@@ -215,8 +217,9 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
         for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
     float m = -INFINITY, l = 0.f, lr = 0.f;            // l: sum of the weights, lr: as the second product takes them
     // Weights enter the second product rounded to bf16, whose errors (2^-9 of a weight in the mean) average out over
-    // many keys.  Where a row has seen fewer than FEW (in a lane's half), what the rounding lost goes in as well: the first
-    // tokens of a prompt or a document, at no cost to the others.
+    // many keys.  In blocks that are masked for some row, where one has seen fewer than FEW (in a lane's half), what the rounding lost
+    // goes in as well: the first tokens of a prompt or a document, at no cost to the others.  (A block that all rows see brings each
+    // of them 64 keys at once.)
     constexpr int FEW = 64;
     int had = 0;
 

@@ -2,12 +2,19 @@
 #include <algorithm>
 #include "attention_tile.h"
 
-// Whether the cached tokens are dealt out over several workgroups, whose parts are then added up, and how many go to each:
-// so many that there are workgroups for the whole GPU, where the rows alone make fewer than a third of them (128 tokens behind 8192,
-// 8 key-value heads: 229 -> 45 us; a prompt of 1024 of 16 heads 36 -> 29 us), or half of them and the cache is long (256 workgroups:
-// 67 -> 62 us of 2048 tokens, but 55 -> 56 us of 1500).  Of more workgroups the parts cost as much as they bring (384 workgroups: 401
-// against 399 us of 8192 tokens, 58 against 60 of 1500), but for chunks of several sequences, whose lengths differ: the longest one's
-// would be the last for long (four of 900 to 7001 tokens, 448 workgroups: 275 -> 235 us, though 366 -> 399 us if all have 8192).
+// Whether the cached tokens are dealt out over several workgroups, whose parts are then added up, and how many go to each.  The GPU has
+// places for 512 workgroups (of up to 128 columns); "->": without parts, with them.
+// - Rows that make up to a third of these: so many parts that all places are taken.  128 tokens behind 8192, 8 key-value heads: 229 -> 45
+//   us; prompts of 768, 1024, 1536 and 2048 tokens with 8 heads 27 -> 24, 34 -> 23, 47 -> 33, 61 -> 40.  (Prompts of 512 get two
+//   parts: 20 -> 20 us with 8 and 16 heads, 20 -> 24 with 32.)
+// - Up to half, and the cache is long: 192 workgroups of 3000 tokens 88 -> 58 us, 256 of 4096 118 -> 96, 256 of 2048 62 -> 58.  Shorter
+//   ones can lose: 256 of 1024 35 -> 40, 192 of 768 27 -> 32 (though 192 of 1536 48 -> 40).
+// - More: of one prompt the parts cost as much as they bring (384 workgroups: 401 against 399 us of 8192 tokens, 58 against 60 of 1500).
+//   Chunks of several sequences may differ in length, and the longest one's workgroups would be the last for long, so caches are cut in
+//   four, in parts of 2048 at least.  2 to 8 chunks, 320 to 448 workgroups: caches of an eighth to the whole of 16384 tokens 595 -> 358 to
+//   460 us, of a half on 559 to 599 -> 453 to 518, all alike 595 to 633 -> 501 to 619; of 8192 271 to 300 -> 186 to 245, 282 to 303
+//   -> 241 to 272, 302 to 311 -> 259 to 323.  The lengths are not known here, and it does not pay for all: of 4000 alike 147 to 153 -> 149
+//   to 170, and of 512 workgroups with caches of 8192 280 -> 275 from an eighth on, but 341 -> 390 alike.
 AttSplit bwla_att_tile_split(const AttArgs& a) {
     AttSplit s = {};
     s.rows = a.max_new * a.group;

@@ -6,9 +6,9 @@
 // its own: 159 -> 99 us below, with the registers that this frees).  Each cached token belongs to one wavefront, so there is nothing to join but the 32 lanes
 // that share its rows, once, at the end, and no atomics.  Where there are few cached tokens for the rows, the rows
 // are dealt out over workgroups whose sums a second launch adds in order.
-// 64 new tokens of four sequences of 6000 to 16384, 64 heads of 8 groups of 128 columns: 84 us, 600 TFLOP/s; of a SIMD's cycles 52 %
-// are vector instructions (fma, exponential, sum for each weight) and 30 % MFMA.  61 fp32 rows a head: 11 us, a chain of loads and
-// fp32 products, and 4 for the second launch.
+// 64 new tokens of four sequences of 6000 to 16384, 64 heads of 8 groups of 128 columns: 84 us, 600 TFLOP/s; of a SIMD's cycles 60 %
+// are vector instructions (fma, exponential, sum for each weight) and 30 % MFMA, 11 % both at once.  A cap: 173 us, above 128 213 (31
+// registers more than there are).  61 fp32 rows a head: 11 us, a chain of loads and fp32 products, and 4 for the second launch.
 #include "attention.h"
 
 namespace {
