@@ -564,6 +564,116 @@ BWLA_API bwla_status_t bwla_cache_evict(const bwla_kv_cache_t* cache, const bwla
                                const int32_t* d_position, int32_t position_stride, int32_t* d_position_out, void* d_ws,
                                size_t ws_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Around the attention of a serving step: norms of queries and keys with the rotation, a cache in 8 bits, and the step's tables
+ * built on the device from its requests' lengths.  The conventions of the calls above hold.
+ * ------------------------------------------------------------------------------------------- */
+
+/*
+ * Norm of each head x of head_dim columns, in fp32:  y = (x - mu) w / sqrt(mean((x - mu)^2) + eps),  mu = mean(x) if `centered`, else 0.
+ * d_q, d_k: weights of the query and of the key heads (NULL: 1), q_stride, k_stride floats from one head's to the next's (0: the same
+ * for all; else a multiple of 4 and at least head_dim).  eps is a normal, positive fp32 number.
+ */
+typedef struct bwla_head_norm {
+    const float *d_q, *d_k;
+    int64_t q_stride, k_stride;
+    float eps;
+    int32_t centered;
+} bwla_head_norm_t;
+
+/* bwla_rope_append of normed queries and keys: each of their heads is normed, then turned.  norm = NULL: bwla_rope_append. */
+BWLA_API bwla_status_t bwla_norm_rope_append(const bwla_kv_cache_t* cache, const bwla_kv_batch_t* batch, const bwla_rope_t* rope,
+                                    const bwla_head_norm_t* norm, const int32_t* d_position, const void* d_qkv, int x_dtype,
+                                    int64_t row_stride, int32_t q_heads, void* d_q, float* d_weights, int32_t* d_cache_position,
+                                    int32_t position_stride, void* stream);
+
+typedef enum {
+    BWLA_CODE_I8 = 0,               /* integers -127 .. 127; top = 127 */
+    BWLA_CODE_E4M3 = 1              /* e4m3 numbers without infinities, up to 448; top = 448 */
+} bwla_code_t;
+
+/*
+ * Keys and values in pages, a byte each: value = code * scale, with a scale (fp32, not negative) for each page and head at d_k_scale,
+ * d_v_scale[page * scale_stride + head].  Strides of codes in bytes, multiples of 16; the other fields as in bwla_kv_cache_t, head_dim
+ * a multiple of 16 (else BWLA_ERR_UNSUPPORTED); dtype: that of queries and outputs.
+ */
+typedef struct bwla_kv_cache8 {
+    void *d_k, *d_v;
+    float *d_k_scale, *d_v_scale;
+    int64_t page_stride, head_stride, slot_stride;
+    int64_t scale_stride;
+    int64_t pages;
+    int32_t page_size, kv_heads, head_dim;
+    int32_t code;                   /* bwla_code_t */
+    int32_t dtype;                  /* bwla_xdtype_t */
+} bwla_kv_cache8_t;
+
+/*
+ * bwla_norm_rope_append into such a cache (norm may be NULL).  With A the largest magnitude among the new tokens' values of a page and
+ * head (after norm and rotation, in fp32):
+ *   where no token of the sequence lies in the page in front of the new ones, or the scale is 0:  scale = A / top, at least 2^-126
+ *   (0 where A is 0);  else the scale stays where A <= top * scale, or is doubled until that holds, and the codes c of the tokens in
+ *   front, after n doublings, become c / 2^n;  codes: value / scale.  All to the nearest code, ties to even.
+ * A value is then off by half a step of its scale at most when it is written, and by one step of the last scale whatever follows (i8;
+ * e4m3 codes halve exactly down to 2^-6).  Values that are not finite do not move a scale: infinities become the largest code, NaN 0.
+ */
+BWLA_API bwla_status_t bwla_norm_rope_append8(const bwla_kv_cache8_t* cache, const bwla_kv_batch_t* batch, const bwla_rope_t* rope,
+                                     const bwla_head_norm_t* norm, const int32_t* d_position, const void* d_qkv, int x_dtype,
+                                     int64_t row_stride, int32_t q_heads, void* d_q, int32_t* d_cache_position,
+                                     int32_t position_stride, void* stream);
+
+/*
+ * The values that each sequence's cached tokens stand for, code * scale rounded to out_dtype: d_k, d_v (either may be NULL): sequences x max_len x
+ * kv_heads x head_dim, dense; 0 behind a sequence's length and in pages that do not exist.  d_first, max_new and tokens are not used.
+ */
+BWLA_API bwla_status_t bwla_cache8_read(const bwla_kv_cache8_t* cache, const bwla_kv_batch_t* batch, void* d_k, void* d_v, int out_dtype,
+                               void* stream);
+
+/*
+ * bwla_attention_forward over such a cache: the same scores, masks, outputs and scratch rules (without the sums of weights).  Codes enter
+ * the products exactly (as fp16, on its matrix instructions), queries as fp16 terms of 11 (bf16) or 22 bits (fp32) relative to the
+ * largest of the row or of 32 rows, weights as terms of 11 or 22 bits; all sums are fp32.  Codes and scales of what is not seen may be anything.
+ */
+BWLA_API bwla_status_t bwla_attention8_workspace_size(const bwla_kv_cache8_t* cache, const bwla_kv_batch_t* batch, int32_t q_heads,
+                                             size_t* bytes);
+BWLA_API bwla_status_t bwla_attention8_forward(const bwla_kv_cache8_t* cache, const bwla_kv_batch_t* batch, const bwla_score_t* score,
+                                      const void* d_q, int64_t q_stride, int32_t q_heads, void* d_out, float* d_lse, void* d_ws,
+                                      size_t ws_bytes, void* stream);
+
+/*
+ * Free pages in a ring of `capacity` entries: those of entries (front + i) % capacity, i < count, where d_state holds front and count.
+ * `pages`: pages of the pool; table entries outside [0, pages) name none.
+ */
+typedef struct bwla_page_pool {
+    int32_t* d_ring;
+    const int32_t* d_state;
+    int32_t* d_state_out;           /* front and count behind the call; may be d_state */
+    int64_t pages;
+    int32_t capacity, page_size;
+} bwla_page_pool_t;
+
+/*
+ * Tables of a step, from the requests alone: request b has d_len[b] cached tokens in the pages of its row of d_table and gets d_new[b]
+ * more.  d_done[b] != 0 (d_done may be NULL): the request that held the row is done; the pages of its d_len[b] tokens go to the ring's end,
+ * in order, and the d_new[b] tokens are those of a new one, which starts without any.  With n = d_len[b], or 0 for those:
+ *   the pages that n + d_new[b] tokens need beyond those of n come from the ring's front, in order of requests and of their tokens,
+ *   and are entered in the row of d_table behind those of n (pages given back by this call: from the next call on);
+ *   d_len_out[b] (may be d_len) = n + d_new[b];  d_first (sequences + 1): row offsets;
+ *   for row t, new token i of request b (any of these may be NULL): d_position[t] = n + i + d_shift[b] (d_shift may be NULL: 0),
+ *   d_slot[t] = page * page_size + slot where it lies (-1 where its page does not exist), d_sequence[t] = b; -1 in rows of no request.
+ * d_status (4): pages missing, requests that would be longer than max_len, rows missing of `tokens`, new tokens of all.  Unless the first
+ * three are 0 nothing is given out: d_len_out[b] = n, d_first is 0 throughout, all rows are of no request, and the calls that follow
+ * find a batch without new tokens.  Requests that are done have given their pages back even then (they may be listed again: their
+ * length is 0 now).  Lengths and new tokens below 0 count as 0, lengths above max_len as max_len.
+ * max_len <= table_stride * page_size.  A page that two rows name would be given back twice.
+ * d_ws: scratch of bwla_batch_build_workspace_size bytes, any contents.
+ */
+BWLA_API bwla_status_t bwla_batch_build_workspace_size(int32_t sequences, int64_t tokens, size_t* bytes);
+BWLA_API bwla_status_t bwla_batch_build(const bwla_page_pool_t* pool, const int32_t* d_len, const int32_t* d_new, const int32_t* d_done,
+                               const int32_t* d_shift, int32_t* d_table, int32_t table_stride, int32_t sequences, int64_t tokens,
+                               int32_t max_len, int32_t* d_len_out, int32_t* d_first, int32_t* d_position, int64_t* d_slot,
+                               int32_t* d_sequence, int32_t* d_status, void* d_ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

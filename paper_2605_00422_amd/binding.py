@@ -26,7 +26,9 @@ EXPORTS = ["bwla_status_string", "bwla_version", "bwla_kron_factor", "bwla_packe
            "bwla_linear_forward_room", "bwla_linear_forward_swiglu_room", "bwla_linear_forward_kernel",
            # marshalled in attention_binding.py
            "bwla_rope_append", "bwla_attention_workspace_size", "bwla_attention_forward", "bwla_attention_weights_workspace_size",
-           "bwla_attention_weights", "bwla_cache_evict_workspace_size", "bwla_cache_evict"]
+           "bwla_attention_weights", "bwla_cache_evict_workspace_size", "bwla_cache_evict",
+           "bwla_norm_rope_append", "bwla_norm_rope_append8", "bwla_cache8_read", "bwla_attention8_workspace_size", "bwla_attention8_forward",
+           "bwla_batch_build_workspace_size", "bwla_batch_build"]
 
 
 class BwlaLayer(Structure):

@@ -88,6 +88,54 @@ struct EvictArgs {
 };
 hipError_t bwla_launch_evict(const EvictArgs& a, hipStream_t st);
 
+// heads normed, then turned (attention_norm.hip), into a cache as it is or into one of codes
+struct NormArgs {
+    RopeArgs r;
+    const float *wq, *wk;                                  // weights (null: 1)
+    int64_t wq_stride, wk_stride;
+    float eps;
+    int32_t centered, normed;
+    float *k_scale, *v_scale;                              // of a cache of codes, whose strides in r are bytes
+    int64_t scale_stride;
+};
+hipError_t bwla_launch_norm_rope(const NormArgs& a, int x_dtype, int dtype, hipStream_t st);
+hipError_t bwla_launch_norm_rope8(const NormArgs& a, int x_dtype, int dtype, int code, hipStream_t st);
+
+struct ReadArgs {
+    const char *k, *v;
+    const float *k_scale, *v_scale;
+    char *k_out, *v_out;
+    const int32_t *table, *len;
+    int64_t page_bytes, head_bytes, slot_bytes, scale_stride;
+    int32_t pages, page_shift, hkv, d, seqs, table_stride, max_len;
+};
+hipError_t bwla_launch_cache8_read(const ReadArgs& a, int out_dtype, int code, hipStream_t st);
+
+// attention over codes (attention8_split*.hip, attention8_tile*.hip): the rules of the other types say how a call is split
+struct Att8 {
+    const float *k_scale, *v_scale;
+    int64_t stride;
+    int32_t code;
+};
+hipError_t bwla_launch_attention8_split(const AttArgs& a, const Att8& e, const AttSplit& s, int dtype, void* ws, hipStream_t st);
+hipError_t bwla_launch_attention8_split_f32(const AttArgs& a, const Att8& e, const AttSplit& s, void* ws, hipStream_t st);
+hipError_t bwla_launch_attention8_tile(const AttArgs& a, const Att8& e, const AttSplit& s, int dtype, void* ws, hipStream_t st);
+hipError_t bwla_launch_attention8_tile_f32(const AttArgs& a, const Att8& e, const AttSplit& s, void* ws, hipStream_t st);
+
+struct BuildArgs {
+    int32_t* ring;
+    const int32_t* state;
+    int32_t* state_out;
+    const int32_t *len, *fresh, *done, *shift;
+    int32_t *table, *len_out, *first, *position;
+    int64_t* slot;
+    int32_t *sequence, *status;
+    int64_t tokens;
+    int32_t pages, capacity, page_shift, seqs, table_stride, max_len;
+};
+size_t bwla_build_bytes(int64_t seqs);
+hipError_t bwla_launch_build(const BuildArgs& a, void* ws, hipStream_t st);
+
 #ifdef __HIPCC__
 // New tokens of a sequence, all of them, as its length is counted from them.  (A length has 2^24 at most, and so have rows: with this
 // many all rows lie in front of the cache.)

@@ -1,0 +1,52 @@
+// The 8-bit codes of a cache: integers -127 .. 127, and e4m3 numbers (no infinities, 448 the largest, 0x7f and 0xff NaN).
+#pragma once
+#include "attention.h"
+
+typedef uint32_t c8_v4u __attribute__((ext_vector_type(4)));
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+
+template <bool I8>
+__device__ __forceinline__ constexpr float code_top() { return I8 ? 127.f : 448.f; }
+
+// four numbers within the codes' range to the nearest codes, ties to even
+template <bool I8>
+__device__ __forceinline__ uint32_t code_of4(float a, float b, float c, float d) {
+    if constexpr (I8) {
+        return ((uint32_t)(int)rintf(a) & 0xffu) | ((uint32_t)(int)rintf(b) & 0xffu) << 8 | ((uint32_t)(int)rintf(c) & 0xffu) << 16 |
+               (uint32_t)(int)rintf(d) << 24;
+    } else {
+        int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
+    }
+}
+// ... and one
+template <bool I8>
+__device__ __forceinline__ uint8_t code_of(float a) { return (uint8_t)code_of4<I8>(a, 0.f, 0.f, 0.f); }
+
+// code number I of a word
+template <bool I8, int I>
+__device__ __forceinline__ float code_value(uint32_t w) {
+    if constexpr (I8) return (float)(int8_t)(w >> (8 * I));
+    else return __builtin_amdgcn_cvt_f32_fp8((int)w, I);
+}
+
+// Four codes as fp16 numbers, exactly, in order.  An e4m3 number is one by the conversion; an integer c by the number of bits
+// 0x6400 + (c + 128), which is 1024 + c + 128, less 1152.
+struct Halves {
+    uint32_t lo, hi;
+};
+template <bool I8>
+__device__ __forceinline__ Halves code_halves(uint32_t w) {
+    Halves r;
+    if constexpr (I8) {
+        const uint32_t u = w ^ 0x80808080u;
+        const v2h less = {(_Float16)-1152.f, (_Float16)-1152.f};
+        r.lo = __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) + less);
+        r.hi = __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) + less);
+    } else {
+        r.lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, false));
+        r.hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, true));
+    }
+    return r;
+}
