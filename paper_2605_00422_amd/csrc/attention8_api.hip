@@ -68,8 +68,9 @@ bwla_status_t bwla_norm_rope_append8(const bwla_kv_cache8_t* cache, const bwla_k
     const bwla_kv_cache_t c = like(cache);
     NormArgs n = {};
     bool idle;
-    bwla_status_t st = rope_args(&c, batch, rope, d_position, d_qkv, x_dtype, row_stride, q_heads, d_q, nullptr, d_cache_position,
-                                 position_stride, &n.r, &idle);
+    bwla_status_t st = check_shapes(&c, batch, q_heads);
+    if (st != BWLA_OK || (st = check_codes(cache, false)) != BWLA_OK) return st;
+    st = rope_args(&c, batch, rope, d_position, d_qkv, x_dtype, row_stride, q_heads, d_q, nullptr, d_cache_position, position_stride, &n.r, &idle);
     if (st != BWLA_OK || (st = check_codes(cache, true)) != BWLA_OK || (st = norm_args(norm, cache->head_dim, &n)) != BWLA_OK || idle) return st;
     n.k_scale = cache->d_k_scale;
     n.v_scale = cache->d_v_scale;
@@ -122,7 +123,9 @@ bwla_status_t bwla_attention8_forward(const bwla_kv_cache8_t* cache, const bwla_
     if (!cache) return BWLA_ERR_NULL;
     const bwla_kv_cache_t c = like(cache);
     AttArgs a;
-    bwla_status_t st = attention_args(&c, batch, score, d_q, q_stride, q_heads, &a);
+    bwla_status_t st = check_shapes(&c, batch, q_heads);
+    if (st != BWLA_OK || (st = check_codes(cache, false)) != BWLA_OK) return st;
+    st = attention_args(&c, batch, score, d_q, q_stride, q_heads, &a);
     if (st != BWLA_OK || (st = check_codes(cache, true)) != BWLA_OK) return st;
     if (batch->tokens == 0 || batch->sequences == 0 || a.max_new == 0) return BWLA_OK;
     if (!d_out) return BWLA_ERR_NULL;

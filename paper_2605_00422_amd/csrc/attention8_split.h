@@ -34,23 +34,6 @@ __device__ __forceinline__ float xor32(float v, bool max_of) {
     return max_of ? fmaxf(a, b) : a + b;
 }
 
-// eight numbers as operands: the nearest of fp16, and (two terms) what that leaves
-template <int T>
-struct Terms {
-    v8h t[T];
-};
-template <int T>
-__device__ __forceinline__ Terms<T> terms_of(const float* x) {
-    Terms<T> r;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) r.t[0][e] = (_Float16)x[e];
-    if constexpr (T == 2) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) r.t[1][e] = (_Float16)(x[e] - (float)r.t[0][e]);
-    }
-    return r;
-}
-
 // BF: bf16 queries and outputs (else fp32); I8: integers (else e4m3); DP: columns, 64, 128 or 256; EXACT: d == DP
 template <bool BF, bool I8, int DP, bool EXACT>
 __global__ __launch_bounds__(64 * SP_WAVES) void att8_split_kernel(AttArgs a, Att8 sc, AttSplit sp, float* __restrict__ part,

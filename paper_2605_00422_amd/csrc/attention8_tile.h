@@ -6,7 +6,7 @@
 // Codes are fp16 numbers exactly: a block's are fetched to registers while the block before is in work, become fp16 there, once for the
 // workgroup, and go to LDS, from where the products on 32x32 fp16 MFMA read them as they read bf16 ones elsewhere.  The pages' scales
 // stay outside the products: eight keys side by side lie in one page, so that a block has eight scales of each kind, scalars, which
-// multiply scores (32 a lane) and weights (32).  Queries are brought to [2^14, 2^15) by one power of two for the wavefront's 32 rows, in one
+// multiply scores (as they become weights, where there is no cap or bias) and weights (32 a lane).  Queries are brought to [2^14, 2^15) by one power of two for the wavefront's 32 rows, in one
 // term for bf16 and two for fp32; what is less than 2^-39 of the largest element of these rows is lost.  The maximum m moves where it is
 // off by 2^4, so that weights times vs / S stay below 2^4 and enter the second product times 2^11, in one term of 11 bits or two.
 #pragma once
@@ -60,7 +60,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
     const float slope = GENERAL && a.slopes ? a.slopes[head] * ATT_LOG2E : 0.f;
     // rows that see nothing whatever the block: what they gather on the way, from queries of 0, is dropped at the end
     const bool blind = me.doc < 0;
-    v8h qf[CS][T];
+    Terms<T> qf[CS];
     float qc;                                          // what a product is to be multiplied by, but for the page's scale
     {
         const char* qp = a.q + (int64_t)(s.row0 + tok) * a.q_bytes + (int64_t)head * a.d * ES;
@@ -86,12 +86,12 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
         const int up = max((int)((__float_as_uint(most) >> 23) & 255) - 127, -100);
 #pragma unroll
         for (int c = 0; c < CS; ++c)
+        {
+            float v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float v = ldexpf(value(c, e), 14 - up);
-                qf[c][0][e] = (_Float16)v;
-                if constexpr (T == 2) qf[c][1][e] = (_Float16)(v - (float)qf[c][0][e]);
-            }
+            for (int e = 0; e < 8; ++e) v[e] = ldexpf(value(c, e), 14 - up);
+            qf[c] = terms_of<T>(v);
+        }
         qc = ldexpf(GENERAL ? 1.f : a.c1, up - 14);
     }
     // indexes of the first and last row of this wavefront, and of the workgroup
@@ -229,20 +229,22 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
     for (int d = 0; d < DT; ++d) vofs[d] = tk * ROWB + ((4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (tk & VSW) * 2) * 16 + (lane & 1) * 8;
 
     // ---- the steps of a tile of 32 keys
-    struct Packed { v8h w[2][T]; };                    // weights as operands: 16 keys each
+    struct Packed { Terms<T> w[2]; };                   // weights as operands: 16 keys each
     float kg[8], vg[8];                                // a block's scales, of eight keys each
     auto products = [&](const char* kb, int k, v16f& sc) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[r] = 0.f;
         const char* src = kb + (k * 32 + l32) * ROWB;
+        v16f low = sc;                                 // (second terms apart: half as many roundings of the large sum)
 #pragma unroll
         for (int c = 0; c < CS; ++c) {
             const v8h kf = *(const v8h*)(src + ((2 * c + hf) ^ (l32 & KSW)) * 16);
-#pragma unroll
-            for (int n = 0; n < T; ++n) sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[c][n], sc, 0, 0, 0);
+            sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[c].t[0], sc, 0, 0, 0);
+            if constexpr (T == 2) low = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[c].t[1], low, 0, 0, 0);
         }
+        if constexpr (T == 2) sc += low;
     };
-    // weights of a tile's scores, and their sums
+    // Weights of a tile's scores, and their sums.  (Without cap and bias scores stay products until here: y - m is rounded once.)
     auto weigh = [&](const v16f& sc, Packed& out, int k) {
         const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
@@ -250,16 +252,11 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
             float w[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                w[e] = __builtin_amdgcn_exp2f(sc[8 * u + e] - base);
+                w[e] = __builtin_amdgcn_exp2f(GENERAL ? sc[8 * u + e] - base : fmaf(sc[8 * u + e], kg[4 * k + 2 * u + e / 4], -base));
                 l += w[e];
                 w[e] *= vg[4 * k + 2 * u + e / 4];
             }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) out.w[u][0][e] = (_Float16)w[e];
-            if constexpr (T == 2) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) out.w[u][1][e] = (_Float16)(w[e] - (float)out.w[u][0][e]);
-            }
+            out.w[u] = terms_of<T>(w);
         }
     };
     // O^T += V^T P^T: operands, and their products
@@ -283,14 +280,17 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
-                for (int n = 0; n < T; ++n) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.x[u * DT + d], p.w[u][n], o[d], 0, 0, 0);
+                for (int n = 0; n < T; ++n) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.x[u * DT + d], p.w[u].t[n], o[d], 0, 0, 0);
     };
     // The maximum moves only when it is off by 2^4; what was summed with the old one follows.
     // (first: what has to be added with the old one before)
-    auto raise = [&](const v16f& sc, auto first) {
+    auto raise = [&](const v16f& sc, int k, auto first) {
         float top = -INFINITY;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, sc[r]);
+        for (int g = 0; g < 4; ++g) {
+            const float four = fmaxf(fmaxf(sc[4 * g], sc[4 * g + 1]), fmaxf(sc[4 * g + 2], sc[4 * g + 3]));
+            top = fmaxf(top, GENERAL ? four : four * kg[4 * k + g]);
+        }
         top = half_max(top);
         if (__builtin_expect(att_uniform(__any(top > m + 4.f)), 0)) {
             first();
@@ -369,7 +369,8 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
                     top_scale = up;
                     down = 1.f / up;
                 }
-                const float kq = now.kscale * qc, vq = vscale * down * 2048.f;
+                // (never 0: an unseen key's product is -inf)
+                const float kq = fmaxf(now.kscale * qc, 0x1p-126f), vq = vscale * down * 2048.f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     kg[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(kq), 8 * i));
@@ -378,9 +379,11 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
             }
             // a tile's scores made ready: scales, cap, bias, mask, and a maximum that will do for them
             auto ready = [&](v16f& sc, int k, auto first) {
+                if constexpr (GENERAL) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) sc[r] *= kg[4 * k + r / 4];
-                if constexpr (GENERAL) att_transform<FORM>(a, sc, me.p, slope, j0, k, now.p, s.pos != nullptr);
+                    for (int r = 0; r < 16; ++r) sc[r] *= kg[4 * k + r / 4];
+                    att_transform<FORM>(a, sc, me.p, slope, j0, k, now.p, s.pos != nullptr);
+                }
                 if (!__builtin_expect(whole, 1)) {
                     if (even) {
                         const int most = (mine ? max(me.i, s.prefix - 1) : -1) - j0 - k * 32 - 4 * hf;
@@ -392,7 +395,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
                         for (int r = 0; r < 16; ++r) sc[r] = (bits >> ((r & 3) + 8 * (r >> 2))) & 1 ? sc[r] : -INFINITY;
                     }
                 }
-                raise(sc, first);
+                raise(sc, k, first);
             };
             // (Order and priorities as in the kernel of the other types: the weights of one tile are taken while the other's products run.)
             v16f s0, s1;
@@ -411,7 +414,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
-                    for (int n = 0; n < T; ++n) p0.w[u][n] = zero;
+                    for (int n = 0; n < T; ++n) p0.w[u].t[n] = zero;
             });
             __builtin_amdgcn_s_setprio(1);
             const Operands f0 = fetch(vb, 0);

@@ -50,3 +50,28 @@ __device__ __forceinline__ Halves code_halves(uint32_t w) {
     }
     return r;
 }
+
+// Eight numbers as operands: the nearest of fp16, and (two terms) what that leaves.  (The number that is taken off has to be the one that is
+// kept: the compiler would make the first term of a product without rounding that to fp32 first, but the second of the rounded one,
+// and near ties the two would not belong together.  So each is held in registers before its terms are made.)
+template <int T>
+struct Terms {
+    v8h t[T];
+};
+template <int T>
+__device__ __forceinline__ Terms<T> terms_of(const float* from) {
+    Terms<T> r;
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        x[e] = from[e];
+        if constexpr (T == 2) asm("" : "+v"(x[e]));
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r.t[0][e] = (_Float16)x[e];
+    if constexpr (T == 2) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r.t[1][e] = (_Float16)(x[e] - (float)r.t[0][e]);
+    }
+    return r;
+}
