@@ -1,31 +1,36 @@
-"""The attention half of a decoder block on W1A6 layers: x -> q|k|v projection -> rotary positions into the paged cache ->
-attention -> o projection, for prompts and for decoding steps, with the cache cut to a budget by the weights that its tokens got.
+"""The attention half of a decoder block on W1A6 layers: x -> q|k|v projection -> (norms of the heads,) rotary positions into the paged
+cache -> attention -> o projection, for prompts and for decoding steps, with the cache cut to a budget by the weights that its tokens got,
+or held in 8 bits.
 
-    python -m paper_2605_00422_amd.attention_block
+    python -m paper_2605_00422_amd.attention_block [i8 | e4m3]
 
-runs a small block of random weights: two prompts, a cut of their caches, sixteen decoding steps.  Every step is a kernel of the
-library; torch holds the memory.  Tables, lengths and pages are the caller's (a serving loop's scheduler), and so is what a
-residual or a norm adds around it."""
+runs a small block of random weights: two prompts, a cut of their caches, sixteen decoding steps; or, with a cache in 8 bits and normed heads,
+a small server's steps, in which requests come, grow and go.  Every step is a kernel of the library; torch holds the memory.  Tables, lengths
+and pages are the caller's (a serving loop's scheduler, or Requests, which builds them on the GPU), and so is what a residual or a norm adds
+around it."""
 from __future__ import annotations
+
+import sys
 
 from . import attention_binding as A, binding as B
 
 
 class AttentionBlock:
     """qkv, o: PackedLayer of the merged projection ((q_heads + 2 kv_heads) head_dim rows) and of the output.  cache: KVCache,
-    bfloat16.  Scores: scale (default head_dim^-1/2), and what else Score takes, per call.
+    bfloat16, or KVCache8 (which has no sums of weights, and is not cut).  norm: HeadNorm of queries and keys, or None.  Scores: scale (default head_dim^-1/2), and what else Score takes, per call.
     rows: of a call, that room is made for at the start; a call of more makes room for twice as many as before at least, and what was
     there stays, where captured calls find it (so that all of it is a few times the longest call's).  ws: uint8, scratch of all calls, which
     raise BwlaError where it is too small for them (attention_binding.*_workspace_size say what they want); without it each takes its own
     from torch's allocator, a captured call from the graph's.  A block serves one stream at a time."""
 
-    def __init__(self, qkv, o, cache: A.KVCache, rope: A.Rope, q_heads: int, scale=None, rows: int = 64, ws=None):
+    def __init__(self, qkv, o, cache, rope: A.Rope, q_heads: int, scale=None, rows: int = 64, ws=None, norm=None):
         d = cache.head_dim
         if qkv.desc.N != (q_heads + 2 * cache.kv_heads) * d or o.desc.K != q_heads * d:
             raise ValueError("qkv must have (q_heads + 2 kv_heads) head_dim rows, o q_heads head_dim columns")
         self.qkv, self.o, self.cache, self.rope, self.q_heads = qkv, o, cache, rope, q_heads
         self.scale = d ** -0.5 if scale is None else scale
-        self.sums = cache.weights()                    # of the softmax weights that each cached token got
+        self.norm, self.eight = norm, isinstance(cache, A.KVCache8)
+        self.sums = None if self.eight else cache.weights()            # of the softmax weights that each cached token got
         self._room, self._rows, self._last, self._ws = [], {}, None, ws
         self._make(rows)
 
@@ -53,14 +58,26 @@ class AttentionBlock:
             self._rows = {M: (act_in, qkv[:M], q[:M], out[:M], lse[:M], act_out)}
         return self._rows[M]
 
-    def __call__(self, x, batch: A.Batch, position, y, watch: bool = True, **score):
+    def __call__(self, x, batch: A.Batch, position, y, watch=None, **score):
         """x (tokens, columns of qkv), bfloat16 or float32 -> y (tokens, rows of o), float32.  position: int32 (axes, tokens).
-        watch: whether the weights that this call's queries give count; the new tokens' sums start at zero either way."""
+        watch: whether the weights that this call's queries give count (None: where the cache has sums); the new tokens' sums start at zero
+        either way."""
+        watch = not self.eight if watch is None else watch
+        if watch and self.eight:
+            raise ValueError("a KVCache8 has no sums of weights")
         act_in, qkv, q, out, lse, act_out = self._buffers(x.shape[0])
         self._last = batch
         score = A.Score(self.scale, **score)
         B.decode_forward(self.qkv, x, act_in, qkv)
-        A.rope_append(self.cache, batch, self.rope, qkv, position, q, self.sums)
+        if self.eight:
+            A.norm_rope_append(self.cache, batch, self.rope, self.norm, qkv, position, q)
+            ws = self._scratch(A.attention8_workspace_size, self.cache, batch, self.q_heads)
+            A.attention8_forward(self.cache, batch, score, q, out, lse, ws)
+            return B.decode_forward(self.o, out.view(x.shape[0], -1), act_out, y)
+        if self.norm is None:
+            A.rope_append(self.cache, batch, self.rope, qkv, position, q, self.sums)
+        else:
+            A.norm_rope_append(self.cache, batch, self.rope, self.norm, qkv, position, q, self.sums)
         ws = self._scratch(A.attention_workspace_size, self.cache, batch, self.q_heads, watch)
         A.attention_forward(self.cache, batch, score, q, out, lse, self.sums if watch else None, ws)
         return B.decode_forward(self.o, out.view(x.shape[0], -1), act_out, y)
@@ -68,6 +85,8 @@ class AttentionBlock:
     def watch_last(self, batch: A.Batch, last: A.Batch, **score):
         """The sums of weights of a long prompt's last queries alone: batch was the call before, of one sequence (watch=False), whose queries
         are still there; last is the same sequence with its last tokens as the new ones."""
+        if self.eight:
+            raise ValueError("a KVCache8 has no sums of weights")
         if batch is not self._last:
             raise ValueError("batch is not that of the call before: its queries are gone")
         if batch.sequences != 1 or last.sequences != 1 or last.tokens > batch.tokens:
@@ -79,8 +98,37 @@ class AttentionBlock:
 
     def cut(self, batch: A.Batch, table_out, keep: int, sinks: int, recent: int, length_out):
         """Each sequence's `keep` tokens with the largest sums, its first and last ones among them, to the pages of table_out."""
+        if self.eight:
+            raise ValueError("a KVCache8 has no sums of weights")
         ws = self._scratch(A.cache_evict_workspace_size, self.cache, batch)
         return A.cache_evict(self.cache, batch, table_out, self.sums, keep, sinks, recent, length_out, ws=ws)
+
+
+class Requests:
+    """The tables of up to n requests of up to max_len tokens each, over a pool of pages, built on the GPU.  step(new, done) gives the batch and
+    the positions (one axis) of new[b] more tokens of each request; done[b]: of a new request, in the place of one that is done.  rows and most:
+    bounds of all new tokens and of a request's, known on the host (new and done are int32 tensors, which are not read there).  The batch of a
+    step that does not fit is empty, and status says why (attention_binding.batch_build): pages missing, requests too long, rows missing.
+    Batches of one object share their tensors: each holds until the next step."""
+
+    def __init__(self, n: int, max_len: int, pages: int, page_size: int, device="cuda"):
+        import torch
+        self.n, self.max_len, self.device = n, max_len, device
+        self.pool = A.PagePool.full(pages, page_size, device)
+        zeros = lambda *s: torch.zeros(*s, dtype=torch.int32, device=device)  # noqa: E731
+        self.table, self.length, self.first, self.status = zeros(n, -(-max_len // page_size)) - 1, zeros(n), zeros(n + 1), zeros(4)
+        self._ws = torch.empty(A.batch_build_workspace_size(n, 0), dtype=torch.uint8, device=device)
+        self._position = {}
+
+    def step(self, new, done=None, rows=None, most: int = 1):
+        rows = self.n * most if rows is None else rows
+        if rows not in self._position:                 # (kept: a captured step finds its own)
+            import torch
+            self._position[rows] = torch.zeros(1, rows, dtype=torch.int32, device=self.device)
+        position = self._position[rows]
+        A.batch_build(self.pool, self.table, self.length, new, self.length, self.first, self.status, rows, self.max_len, done,
+                      position=position[0], ws=self._ws)
+        return A.Batch(self.table, self.length, self.first, tokens=rows, max_new=most, max_len=self.max_len), position
 
 
 def random_layer(torch, gen, N, K, rank, dev):
@@ -131,7 +179,37 @@ def main(hidden=512, q_heads=8, kv_heads=2, dim=64, page=16, prompts=(300, 77), 
     return outputs, torch.stack(lengths)
 
 
+def serve(code, hidden=512, q_heads=8, kv_heads=2, dim=64, page=16, places=4, max_len=160, steps=24, dev="cuda"):
+    """A small server's steps on a block with a cache in 8 bits (code: i8 or e4m3) and normed heads: requests of random prompts and lengths in
+    `places` rows.  Returns each step's outputs and how many rows they have, and the cached lengths."""
+    import random
+    import torch
+    gen, rng = torch.Generator(device=dev).manual_seed(1), random.Random(1)
+    pages = places * -(-max_len // page)
+    cache = A.KVCache8.empty(pages, kv_heads, page, dim, torch.bfloat16, {"i8": torch.int8, "e4m3": torch.float8_e4m3fn}[code], dev)
+    weights = lambda: 1.0 + 0.1 * torch.randn(dim, generator=gen, device=dev)  # noqa: E731
+    block = AttentionBlock(random_layer(torch, gen, (q_heads + 2 * kv_heads) * dim, hidden, 8, dev), random_layer(torch, gen, hidden, q_heads * dim, 8, dev),
+                           cache, tables(torch, max_len, dim, dev), q_heads, norm=A.HeadNorm(weights(), weights()))
+    requests = Requests(places, max_len, pages, page, dev)
+    left, outputs, lengths = [0] * places, [], []      # tokens that each request has still to give
+    for _ in range(steps):
+        done = [int(n == 0) for n in left]
+        new = [rng.randrange(1, 100) if d else 1 for d in done]
+        left = [rng.randrange(3, 40) if d else n - 1 for d, n in zip(done, left)]
+        i32 = lambda v: torch.tensor(v, dtype=torch.int32, device=dev)  # noqa: E731
+        batch, position = requests.step(i32(new), i32(done), rows=sum(new), most=max(new))
+        x, y = torch.randn(sum(new), hidden, generator=gen, device=dev).bfloat16(), torch.empty(sum(new), hidden, device=dev)
+        outputs.append(block(x, batch, position, y))
+        lengths.append(requests.length.clone())
+    return outputs, torch.stack(lengths)
+
+
 if __name__ == "__main__":
-    ys, lens = main()
-    print("prompts of %d and %d tokens; %d steps; cached tokens at the end: %s" % (ys[0].shape[0], ys[1].shape[0], len(lens), lens[-1].tolist()))
-    print("root mean square of the outputs: prompt %.4f, last step %.4f" % (ys[0].pow(2).mean().sqrt(), ys[-1].pow(2).mean().sqrt()))
+    if len(sys.argv) > 1:
+        ys, lens = serve(sys.argv[1])
+        print("%d steps of %d rows; cached tokens at the end: %s" % (len(ys), sum(len(y) for y in ys), lens[-1].tolist()))
+        print("root mean square of the outputs: first step %.4f, last step %.4f" % (ys[0].pow(2).mean().sqrt(), ys[-1].pow(2).mean().sqrt()))
+    else:
+        ys, lens = main()
+        print("prompts of %d and %d tokens; %d steps; cached tokens at the end: %s" % (ys[0].shape[0], ys[1].shape[0], len(lens), lens[-1].tolist()))
+        print("root mean square of the outputs: prompt %.4f, last step %.4f" % (ys[0].pow(2).mean().sqrt(), ys[-1].pow(2).mean().sqrt()))
