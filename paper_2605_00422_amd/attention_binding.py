@@ -102,6 +102,12 @@ def _floats(t, what: str, shape=None):
     return t
 
 
+def _on(*tensors):
+    """Index of the GPU that these tensors lie on (-1: none of them on one), None without any, -2 where they lie apart."""
+    at = {t.get_device() for t in tensors if t is not None}
+    return None if not at else at.pop() if len(at) == 1 else -2
+
+
 class KVCache:
     """Keys and values in pages: two tensors (pages, kv_heads, page_size, head_dim), float32 or bfloat16, of any strides
     (the same for both) with dense columns."""
@@ -112,7 +118,7 @@ class KVCache:
         if k.stride(3) != 1 and k.shape[3] > 1:
             raise TypeError("a head's columns must be dense")
         _types()
-        self.k, self.v, self.dtype = k, v, k.dtype
+        self.k, self.v, self.dtype, self._at = k, v, k.dtype, _on(k, v)
         self.slots = k.shape[:3]
         self.pages, self.kv_heads, self.page_size, self.head_dim = k.shape
         self.desc = _Cache(_p(k), _p(v), k.stride(0), k.stride(1), k.stride(2), *k.shape[:1], k.shape[2], k.shape[1], k.shape[3],
@@ -145,6 +151,7 @@ class Batch:
             raise ValueError("max_new: the most new tokens of a sequence")
         if max_len is None:
             raise ValueError("max_len: the most cached tokens of a sequence")
+        self._at = _on(table, length, first)
         self.sequences, self.tokens = n, int(n if tokens is None else tokens)
         self.max_len, self.columns = int(max_len), table.shape[1]
         stride = table.stride(0) if n > 1 else table.shape[1]
@@ -166,7 +173,7 @@ class Score:
         _types()
         self.slopes, self.prefix = _floats(slopes, "slopes"), _ints(prefix, "prefix", 1)
         self.doc, self.position = _ints(doc, "doc", 2), _ints(position, "position", 2)
-        self.heads = None if slopes is None else slopes.numel()
+        self.heads, self._at = None if slopes is None else slopes.numel(), _on(slopes, prefix, doc, position)
         rows = {t.shape[0] for t in (prefix, doc, position) if t is not None}
         self.sequences = None if not rows else rows.pop() if len(rows) == 1 else -1        # (-1: they disagree)
         self.columns = min((t.shape[1] for t in (doc, position) if t is not None), default=None)
@@ -194,7 +201,7 @@ class Rope:
         self.sections = [cos.shape[1]] if sections is None else [int(x) for x in sections]
         if not 1 <= len(self.sections) <= 4:
             raise ValueError("one to four axes")
-        self.axes = len(self.sections)
+        self.axes, self._at = len(self.sections), _on(cos, sin)
         self.desc = _Rope(_p(cos), _p(sin), cos.shape[0], cos.shape[1], self.axes, int(interleaved),
                           (c_int32 * 4)(*self.sections))
         self._ref = byref(self.desc)
@@ -312,17 +319,19 @@ def cache_evict(cache: KVCache, batch: Batch, table_out, weights, keep: int, sin
 
 
 # ---------------------------------------------------------------- a cache in 8 bits, normed heads, a step's tables
-def _here(first, *rest):
-    """The tensors of a call lie on the current GPU.  (The library would follow whatever address it is given.)"""
-    device = first.device
-    if device.type != "cuda":
-        raise TypeError("tensors of this call must lie on a GPU")
-    stream = _s()
-    if device.index != _b._torch._C._cuda_getDevice():
-        raise ValueError("tensors of this call must lie on the current GPU")
-    for t in rest:
-        if t is not None and t.device != device:
+def _here(at, descriptors, *tensors):
+    """The current stream, if what a call is given lies on the current GPU, `at`.  (The library would follow whatever address it gets.)"""
+    if at < 0:
+        raise TypeError("tensors of this call must lie on a GPU, one for all")
+    for d in descriptors:
+        if d._at is not None and d._at != at:
             raise ValueError("tensors of this call must lie on one GPU")
+    for t in tensors:
+        if t is not None and t.get_device() != at:
+            raise ValueError("tensors of this call must lie on one GPU")
+    stream = _s()
+    if at != _b._torch._C._cuda_getDevice():
+        raise ValueError("tensors of this call must lie on the current GPU")
     return stream
 
 
@@ -345,7 +354,7 @@ class KVCache8:
         for t in (k_scale, v_scale):
             if t.dtype is not _f32 or t.shape != k.shape[:2] or t.stride() != k_scale.stride() or (t.shape[1] > 1 and t.stride(1) != 1):
                 raise TypeError("scales must be float32, (pages, kv_heads), rows dense and alike")
-        self.k, self.v, self.k_scale, self.v_scale, self.dtype = k, v, k_scale, v_scale, dtype
+        self.k, self.v, self.k_scale, self.v_scale, self.dtype, self._at = k, v, k_scale, v_scale, dtype, _on(k, v, k_scale, v_scale)
         self.pages, self.kv_heads, self.page_size, self.head_dim = k.shape
         self.code = CODE_I8 if k.dtype is torch.int8 else CODE_E4M3
         apart = k_scale.stride(0) if self.pages > 1 else self.kv_heads
@@ -369,7 +378,7 @@ class HeadNorm:
         for t in (q, k):
             if t is not None and (t.dtype is not _f32 or t.dim() not in (1, 2) or (t.stride(-1) != 1 and t.shape[-1] > 1)):
                 raise TypeError("weights must be float32, (head_dim) or (heads, head_dim), dense rows")
-        self.q, self.k = q, k
+        self.q, self.k, self._at = q, k, _on(q, k)
         apart = lambda t: 0 if t is None or t.dim() == 1 else t.stride(0) if t.shape[0] > 1 else t.shape[1]  # noqa: E731
         self.desc = _HeadNorm(_p(q), _p(k), apart(q), apart(k), eps, int(centered))
         self._ref = byref(self.desc)
@@ -388,8 +397,7 @@ def norm_rope_append(cache, batch: Batch, rope: Rope, norm, qkv, position, q, we
     eight = isinstance(cache, KVCache8)
     if eight and weights is not None:
         raise TypeError("a KVCache8 has no sums of weights")
-    stream = _here(cache.k, batch.table, batch.length, batch.first, rope.cos, rope.sin, qkv, position, q, weights, cache_position,
-                   *(() if norm is None else (norm.q, norm.k)))
+    stream = _here(cache._at, (batch, rope) if norm is None else (batch, rope, norm), qkv, position, q, weights, cache_position)
     args = (cache._ref, batch._ref, rope._ref, None if norm is None else norm._ref, _p(position), _p(qkv), x, apart, hq, _p(q))
     if eight:
         _ck(load().bwla_norm_rope_append8(*args, _p(cache_position), stride, stream), "bwla_norm_rope_append8")
@@ -409,7 +417,7 @@ def cache8_read(cache: KVCache8, batch: Batch, k=None, v=None):
             raise TypeError("k and v must be (sequences, max_len, kv_heads, head_dim), dense, of one type")
     if one is None:
         return k, v
-    stream = _here(cache.k, batch.table, batch.length, k, v)
+    stream = _here(cache._at, (batch,), k, v)
     _ck(load().bwla_cache8_read(cache._ref, batch._ref, _p(k), _p(v), _b._xdtype(one), stream), "bwla_cache8_read")
     return k, v
 
@@ -427,7 +435,7 @@ def attention8_forward(cache: KVCache8, batch: Batch, score: Score, q, out, lse=
         raise TypeError("out must be like q, and dense")
     score._check(batch, hq)
     _floats(lse, "lse", (batch.tokens, hq))
-    stream = _here(cache.k, batch.table, batch.length, batch.first, q, out, lse, ws, score.slopes, score.prefix, score.doc, score.position)
+    stream = _here(cache._at, (batch, score), q, out, lse, ws)
     _ck(load().bwla_attention8_forward(cache._ref, batch._ref, score._ref, _p(q), stride, hq, _p(out), _p(lse), _p(ws), _bytes(ws), stream),
         "bwla_attention8_forward")
     return out
@@ -445,6 +453,7 @@ class PagePool:
         if state.shape[0] != 2 or (state_out is not None and state_out.shape[0] != 2):
             raise TypeError("state and state_out must have two entries")
         self.ring, self.state, self.state_out, self.page_size = ring, state, state if state_out is None else state_out, int(page_size)
+        self._at = _on(ring, state, state_out)
         self.desc = _Pool(_p(ring), _p(state), _p(self.state_out), ring.shape[0] if pages is None else pages, ring.shape[0], self.page_size)
         self._ref = byref(self.desc)
 
@@ -461,6 +470,11 @@ def batch_build_workspace_size(sequences: int, tokens: int) -> int:
     return out.value
 
 
+def _vector(t, what, size):
+    if t is not None and (t.dtype is not _i32 or t.shape != (size,) or not t.is_contiguous()):
+        raise TypeError(f"{what} must be a dense int32 tensor of {size} entries")
+
+
 def batch_build(pool: PagePool, table, length, new, length_out, first, status, tokens, max_len, done=None, shift=None, position=None,
                 slot=None, sequence=None, ws=None):
     """A step's tables: table (sequences, pages of the longest) gets the pages of the new tokens, length_out (may be length) the lengths,
@@ -468,25 +482,22 @@ def batch_build(pool: PagePool, table, length, new, length_out, first, status, t
     of each request; done: requests whose place a new one takes; shift: position less index in the cache.  status (4): pages missing,
     requests longer than max_len, rows missing, new tokens; unless the first three are 0 the batch is empty.  All int32 but slot.
     ws: batch_build_workspace_size bytes."""
-    n = length.shape[0]
-    for t, what, size in ((length, "length", n), (new, "new", n), (done, "done", n), (shift, "shift", n), (length_out, "length_out", n),
-                          (first, "first", n + 1), (status, "status", 4), (position, "position", tokens), (sequence, "sequence", tokens)):
-        if _ints(t, what, 1) is not None and (t.shape[0] != size or not t.is_contiguous()):
-            raise ValueError(f"{what} must have {size} entries, dense")
-    if _ints(table, "table", 2).shape[0] != n:
-        raise ValueError("table: one row for each request")
+    n, columns = table.shape
+    _vector(length, "length", n), _vector(new, "new", n), _vector(done, "done", n), _vector(shift, "shift", n), _vector(length_out, "length_out", n)
+    _vector(first, "first", n + 1), _vector(status, "status", 4), _vector(position, "position", tokens), _vector(sequence, "sequence", tokens)
+    _ints(table, "table", 2)
     if slot is not None and (slot.dtype is not _i64 or slot.shape != (tokens,) or not slot.is_contiguous()):
         raise TypeError("slot must be a dense int64 tensor of an entry for each row")
-    if table.shape[1] * pool.page_size < max_len:
+    if columns * pool.page_size < max_len:
         raise ValueError("table: too few pages for max_len")
-    stride = table.stride(0) if n > 1 else table.shape[1]
-    if stride < table.shape[1]:
+    stride = table.stride()[0] if n > 1 else columns
+    if stride < columns:
         raise TypeError("rows of the table overlap")
     if n == 0:                                         # (an empty tensor has no address)
         length = new = done = shift = table = length_out = None
     if tokens == 0:
         position = slot = sequence = None
-    stream = _here(pool.ring, pool.state, pool.state_out, table, length, new, length_out, first, status, done, shift, position, slot, sequence, ws)
+    stream = _here(pool._at, (), table, length, new, length_out, first, status, done, shift, position, slot, sequence, ws)
     _ck(load().bwla_batch_build(pool._ref, _p(length), _p(new), _p(done), _p(shift), _p(table), stride, n, tokens, max_len, _p(length_out),
                                 _p(first), _p(position), _p(slot), _p(sequence), _p(status), _p(ws), _bytes(ws), stream), "bwla_batch_build")
     return first

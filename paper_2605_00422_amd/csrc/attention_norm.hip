@@ -6,8 +6,8 @@
 //
 // A head of a row belongs to a group of 4 to 64 lanes, which hold it in registers from load to store: an item is VEC pairs to turn, or
 // 2 VEC columns that stay, and the sums of a norm are exchanges between a group's lanes.  Codes: a workgroup has the new tokens
-// of a page and head, of keys or of values, all of them in registers where they are up to four for each of its groups (else they
-// are read and computed twice); the largest magnitude goes through LDS, and older codes of the page follow where its scale grew.
+// of a page and head, of keys or of values, one for each of its groups in registers (in pages of more tokens than that the others are
+// read and computed twice); the largest magnitude goes through LDS, and older codes of the page follow where its scale grew.
 #include <algorithm>
 
 #include "code8.h"
@@ -254,7 +254,7 @@ __device__ __forceinline__ float magnitude(float v) {
     const float m = fabsf(v);
     return m <= 3.402823466e38f ? m : 0.f;
 }
-// the largest over a workgroup of up to four wavefronts
+// the largest over a workgroup
 __device__ __forceinline__ float block_max(float v, float* words) {
     v = bwla_wave_max(v);
     if ((threadIdx.x & 63) == 0) words[threadIdx.x >> 6] = v;
@@ -281,22 +281,33 @@ __device__ __forceinline__ void put_codes(uint8_t* dst, const float* x, float ov
     }
 }
 
-// The first query_blocks workgroups write queries; of the others each has a page's new tokens, of one key-value head's keys or values.
+// The first query_blocks workgroups write queries, of `rows` rows each or of a part of one's heads; of the others each has a page's new
+// tokens, of one key-value head's keys or values.
 // Page number u of the call: those that sequence b touches begin at first[b] / page + 2 b, which leaves room for each one's.
 template <int VEC, bool XBF, bool BF, bool I8>
-__global__ __launch_bounds__(256) void norm_rope8_kernel(NormArgs n, Items it, int64_t query_blocks, int heads_a_block) {
-    constexpr int KEPT = VEC == 1 ? 2 : 4, IT = items_a_lane<VEC>();
-    __shared__ float words[4];
+__global__ __launch_bounds__(1024) void norm_rope8_kernel(NormArgs n, Items it, int64_t query_blocks, int rows) {
+    constexpr int IT = items_a_lane<VEC>();
+    __shared__ float words[16];
     const RopeArgs& a = n.r;
     const int groups = blockDim.x / it.lanes, group = threadIdx.x / it.lanes, lane = threadIdx.x & (it.lanes - 1);
     if (blockIdx.x < query_blocks) {
-        const int per = (a.hq + heads_a_block - 1) / heads_a_block;
-        const int64_t row = blockIdx.x / per;
-        const int head = (int)(blockIdx.x % per) * heads_a_block + group;
-        const RowOf r = row_of(a, row);
-        if (!r.live) return;
-        if (head == 0 && lane == 0 && a.cache_pos && r.j >= 0) a.cache_pos[(int64_t)r.b * a.pos_stride + r.j] = a.pos[row];
-        const bool live = head < a.hq;
+        int64_t row;
+        int head;
+        bool live;
+        if (rows > 0) {
+            const int r = group / a.hq;
+            row = blockIdx.x * (int64_t)rows + r;
+            head = group - r * a.hq;
+            live = r < rows && row < a.tokens;
+        } else {
+            const int per = (a.hq + groups - 1) / groups;
+            row = blockIdx.x / per;
+            head = (int)(blockIdx.x % per) * groups + group;
+            live = head < a.hq;
+        }
+        const RowOf r = row_of(a, live ? row : 0);
+        live = live && r.live;
+        if (live && head == 0 && lane == 0 && a.cache_pos && r.j >= 0) a.cache_pos[(int64_t)r.b * a.pos_stride + r.j] = a.pos[row];
         float x[IT][2 * VEC];
         head_values<VEC, XBF>(n, it, row, head, 0, live, lane, x);
         if (live) put_head<VEC, BF>(n, it, a.q, (row * a.hq + head) * a.d, 0, lane, x);
@@ -334,8 +345,7 @@ __global__ __launch_bounds__(256) void norm_rope8_kernel(NormArgs n, Items it, i
     float* const scale_at = (kind == 1 ? n.k_scale : n.v_scale) + page * n.scale_stride + head;
     const int64_t row_from = r0 + (from - start);
     const int count = to - from;
-    const bool kept = count <= KEPT * groups;
-    float x[KEPT][IT][2 * VEC];
+    float x[IT][2 * VEC];                              // the first token of this group
     float most = 0.f;
     auto values = [&](int t, float (&y)[IT][2 * VEC]) {
         head_values<VEC, XBF>(n, it, row_from + min(t, count - 1), head, kind, t < count, lane, y);
@@ -347,20 +357,14 @@ __global__ __launch_bounds__(256) void norm_rope8_kernel(NormArgs n, Items it, i
             for (int c = 0; c < 2 * VEC; ++c) most = fmaxf(most, magnitude(y[i][c]));
     };
     const float was = inside > 0 ? *scale_at : 0.f;
-    if (kept) {
-#pragma unroll
-        for (int k = 0; k < KEPT; ++k)
-            if (k * groups < count) {
-                values(k * groups + group, x[k]);
-                watch(x[k]);
-            }
-    } else {
-        for (int t = 0; t < count; t += groups) {
-            values(t + group, x[0]);
-            watch(x[0]);
-        }
+    values(group, x);
+    watch(x);
+    for (int t = groups; t < count; t += groups) {
+        float y[IT][2 * VEC];
+        values(t + group, y);
+        watch(y);
     }
-    most = block_max(most, words);                     // (everyone has read the scale behind it)
+    most = block_max(most, words);                     // (everyone has read the scale in front of it)
     constexpr float top = code_top<I8>();
     float scale = was;
     int doubled = 0;
@@ -402,15 +406,11 @@ __global__ __launch_bounds__(256) void norm_rope8_kernel(NormArgs n, Items it, i
             if (hi >= 0) put_codes<I8, VEC>(dst + hi, y[i] + VEC, over);
         }
     };
-    if (kept) {
-#pragma unroll
-        for (int k = 0; k < KEPT; ++k)
-            if (k * groups < count) put(k * groups + group, x[k]);
-    } else {
-        for (int t = 0; t < count; t += groups) {
-            values(t + group, x[0]);
-            put(t + group, x[0]);
-        }
+    put(group, x);
+    for (int t = groups; t < count; t += groups) {
+        float y[IT][2 * VEC];
+        values(t + group, y);
+        put(t + group, y);
     }
 }
 
@@ -492,18 +492,18 @@ hipError_t bwla_launch_norm_rope8(const NormArgs& n, int x_dtype, int dtype, int
         constexpr int V = decltype(vec)::value;
         const RopeArgs& a = n.r;
         const Items it = items_of<V>(a);
-        // as many threads as a page's new tokens have work for
+        // as many threads as a page's new tokens have work for, so that each is read once
         int threads = 64;
-        while (threads < 256 && (int64_t)threads < (int64_t)it.lanes * std::min(a.max_new, 1 << a.page_shift)) threads *= 2;
-        const int heads = threads / it.lanes;
-        const int64_t queries = a.tokens * ((a.hq + heads - 1) / heads);
+        while (threads < 1024 && (int64_t)threads < (int64_t)it.lanes * std::min(a.max_new, 1 << a.page_shift)) threads *= 2;
+        const int groups = threads / it.lanes, rows = groups / a.hq;
+        const int64_t queries = rows > 0 ? (a.tokens + rows - 1) / rows : a.tokens * ((a.hq + groups - 1) / groups);
         const int64_t units = a.first ? (a.tokens >> a.page_shift) + 2ll * a.seqs : a.seqs;
         const int64_t blocks = queries + units * 2 * a.hkv;
         if (blocks * threads >= 1ll << 32) return hipErrorInvalidConfiguration;       // (a grid has fewer than 2^32 threads)
         return by_types(x_dtype == BWLA_X_BF16, dtype == BWLA_X_BF16, [&](auto x, auto y) {
             constexpr bool X = decltype(x)::value, Y = decltype(y)::value;
-            if (code == BWLA_CODE_I8) norm_rope8_kernel<V, X, Y, true><<<(unsigned)blocks, threads, 0, st>>>(n, it, queries, heads);
-            else norm_rope8_kernel<V, X, Y, false><<<(unsigned)blocks, threads, 0, st>>>(n, it, queries, heads);
+            if (code == BWLA_CODE_I8) norm_rope8_kernel<V, X, Y, true><<<(unsigned)blocks, threads, 0, st>>>(n, it, queries, rows);
+            else norm_rope8_kernel<V, X, Y, false><<<(unsigned)blocks, threads, 0, st>>>(n, it, queries, rows);
             return hipGetLastError();
         });
     });

@@ -226,3 +226,16 @@ def test_captured_and_replayed(A):
             assert torch.equal(one[k], two[k]), k
         assert torch.equal(one["pool"].state, two["pool"].state) and torch.equal(one["pool"].ring, two["pool"].ring)
     assert one["status"][1] > 0
+
+
+@pytest.mark.parametrize("tokens", [3, 5000])
+def test_no_requests_but_rows(A, tokens):
+    s = Step([], [], tokens=tokens)
+    s.table = np.zeros((0, 1), np.int32)
+    s.check(A)
+
+
+@pytest.mark.parametrize("n", [256, 257, 320, 65535])
+def test_many_requests(A, n):
+    rng = np.random.default_rng(n)
+    Step(rng.integers(0, 40, n), rng.integers(0, 3, n), done=rng.integers(0, 9, n) == 0, seed=n).check(A)
