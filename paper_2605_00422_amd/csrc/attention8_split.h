@@ -34,9 +34,10 @@ __device__ __forceinline__ float xor32(float v, bool max_of) {
     return max_of ? fmaxf(a, b) : a + b;
 }
 
-// BF: bf16 queries and outputs (else fp32); I8: integers (else e4m3); DP: columns, 64, 128 or 256; EXACT: d == DP
-template <bool BF, bool I8, int DP, bool EXACT>
-__global__ __launch_bounds__(64 * SP_WAVES) void att8_split_kernel(AttArgs a, Att8 sc, AttSplit sp, float* __restrict__ part,
+// BF: bf16 queries and outputs (else fp32); I8: integers (else e4m3); DP: columns, 64, 128 or 256; EXACT: d == DP;
+// FORM: AttForm, scale, cap and bias
+template <bool BF, bool I8, int DP, bool EXACT, int FORM>
+__global__ __launch_bounds__(64 * SP_WAVES, (DP == 256 ? 1 : 2)) void att8_split_kernel(AttArgs a, Att8 sc, AttSplit sp, float* __restrict__ part,
                                                                   float4* __restrict__ stat) {
     constexpr int ES = BF ? 2 : 4, T = BF ? 1 : 2;
     constexpr int KS = DP / 64;                // 64-byte steps along a row of K
@@ -80,7 +81,7 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att8_split_kernel(AttArgs a, At
     // this lane's row
     const int tok = row / a.group, head = h * a.group + row - tok * a.group;
     const AttRow me = att_row(s, tok, row < rows);
-    const float slope = a.slopes && row < rows ? a.slopes[head] * ATT_LOG2E : 0.f;
+    [[maybe_unused]] const float slope = FORM != ATT_PLAIN && a.slopes && row < rows ? a.slopes[head] * ATT_LOG2E : 0.f;
     Terms<T> qf[KS][2];
     float qc;                                  // what a product is to be multiplied by, but for the page's scale
     {
@@ -118,7 +119,7 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att8_split_kernel(AttArgs a, At
             qf[u][0] = terms_of<T>(x[u]);
             qf[u][1] = terms_of<T>(x[u] + 8);
         }
-        qc = ldexpf(a.capped != 0.f ? 1.f : a.c1, up - 14);
+        qc = ldexpf(FORM != ATT_PLAIN && a.capped != 0.f ? 1.f : a.c1, up - 14);
     }
     __syncthreads();
 
@@ -176,14 +177,19 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att8_split_kernel(AttArgs a, At
         }
     };
     constexpr int STRIDE = SP_WAVES * SP_STEP;
+    [[maybe_unused]] const float c3 = a.c2 * (2.f * ATT_LOG2E);
     if (c0 + wave * SP_STEP < c1) {
         load_keys(c0 + wave * SP_STEP);
         load_values(c0 + wave * SP_STEP);
     }
+    // keys in front of this index are seen by every row, where nothing but the index counts
+    const int seen_to = s.doc || s.pos || a.window != INT32_MAX ? 0 : min(c1, max(s.old + rt * 16 / a.group, -1) + 1);
     for (int j0 = c0 + wave * SP_STEP; j0 < c1; j0 += STRIDE) {
+        // Every row sees every key of the step, as when one token follows a cache without windows and documents: nothing is tested then.  (One
+        // body for both: two of them took 189 registers instead of 128.)
+        const bool whole = j0 + SP_STEP <= seen_to && att_uniform(__all((page_v[0] >= 0) & (page_v[1] >= 0)));
         float y[2][4];
-        uint32_t used[2];                      // of a lane's four keys those that any row sees
-        float top = -INFINITY, now_s = 0.f;
+        uint32_t used[2] = {15u, 15u};         // of a lane's four keys those that any row sees
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             v4f acc{0.f, 0.f, 0.f, 0.f};
@@ -198,21 +204,47 @@ __global__ __launch_bounds__(64 * SP_WAVES) void att8_split_kernel(AttArgs a, At
                         acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, x), qf[u][i].t[n], acc, 0, 0, 0);
                 }
             const float kq = ks_v[t] * qc;
-            used[t] = 0;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int j = j0 + 16 * t + 4 * g + r;
-                const AttKey key = att_key(a, s, j, page_v[t] >= 0 && j < c1);
-                const bool seen = att_sees(me, s.prefix, a.window, j, key.p, key.doc);
-                float v = acc[r] * kq;
-                if (a.capped != 0.f) v = a.capped * att_tanh(v * a.c2);
-                if (a.slopes) v -= slope * fabsf((float)(me.p - key.p));
-                y[t][r] = seen ? v : -INFINITY;
-                used[t] |= ((__ballot(seen) >> (16 * g)) & 0xffffull) != 0 ? 1u << r : 0u;
-                top = fmaxf(top, y[t][r]);
-            }
-            now_s = fmaxf(now_s, used[t] ? vs_v[t] : 0.f);
+            for (int r = 0; r < 4; ++r) y[t][r] = acc[r] * kq;
         }
+        if constexpr (FORM != ATT_PLAIN) {
+            if (a.capped != 0.f) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    float& v = y[i / 4][i % 4];
+                    if constexpr (FORM == ATT_SHORT) v = fmaf(-2.f * a.capped, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * c3)), a.capped);
+                    else v = a.capped * att_tanh(v * a.c2);
+                }
+            }
+        }
+        if (__builtin_expect(whole, 1)) {
+            if constexpr (FORM != ATT_PLAIN) {
+                if (a.slopes) {
+                    const float away = (float)(me.p - j0 - 4 * g);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) y[i / 4][i % 4] -= slope * fabsf(away - (float)(16 * (i / 4) + i % 4));
+                }
+            }
+        } else {
+            const int last = c1 - 1;
+            used[0] = used[1] = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int j = j0 + 16 * (i / 4) + 4 * g + i % 4, in = min(j, last);
+                const int kp = s.pos ? max(s.pos[in], 0) : j;
+                const int kd = page_v[i / 4] >= 0 && j <= last ? (s.doc ? max(s.doc[in], -1) : 0) : -1;
+                const bool seen = att_sees(me, s.prefix, a.window, j, kp, kd);
+                if constexpr (FORM != ATT_PLAIN) {
+                    if (a.slopes) y[i / 4][i % 4] -= slope * fabsf((float)(me.p - kp));
+                }
+                y[i / 4][i % 4] = seen ? y[i / 4][i % 4] : -INFINITY;
+                used[i / 4] |= ((__ballot(seen) >> (16 * g)) & 0xffffull) != 0 ? 1u << (i % 4) : 0u;
+            }
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, y[i / 4][i % 4]);
+        float now_s = fmaxf(used[0] ? vs_v[0] : 0.f, used[1] ? vs_v[1] : 0.f);
         // as the values' scales stand for this step: nothing of what no row sees
         float over[2] = {used[0] ? vs_v[0] : 0.f, used[1] ? vs_v[1] : 0.f};
         if (j0 + STRIDE < c1) load_keys(j0 + STRIDE);
@@ -339,9 +371,17 @@ hipError_t launch8(const AttArgs& a, const Att8& e, const AttSplit& s, void* ws,
         kernel<<<grid, 64 * SP_WAVES, 0, st>>>(a, e, s, part, stat);
         return hipGetLastError();
     };
+    auto columns = [&](auto i8, auto form) {
+        constexpr bool I8 = decltype(i8)::value;
+        constexpr int FORM = decltype(form)::value;
+        return a.d == DP ? go(att8_split_kernel<BF, I8, DP, true, FORM>) : go(att8_split_kernel<BF, I8, DP, false, FORM>);
+    };
+    auto codes = [&](auto form) { return e.code == BWLA_CODE_I8 ? columns(std::true_type{}, form) : columns(std::false_type{}, form); };
+    const AttForm form = att_form(a, BF);
     hipError_t r;
-    if (e.code == BWLA_CODE_I8) r = a.d == DP ? go(att8_split_kernel<BF, true, DP, true>) : go(att8_split_kernel<BF, true, DP, false>);
-    else r = a.d == DP ? go(att8_split_kernel<BF, false, DP, true>) : go(att8_split_kernel<BF, false, DP, false>);
+    if (form == ATT_PLAIN) r = codes(std::integral_constant<int, ATT_PLAIN>{});
+    else if (form == ATT_LONG) r = codes(std::integral_constant<int, ATT_LONG>{});
+    else r = codes(std::integral_constant<int, BF ? ATT_SHORT : ATT_LONG>{});
     if (r != hipSuccess || s.splits == 1) return r;
     return bwla_launch_attention_join(a, s, BF ? BWLA_X_BF16 : BWLA_X_F32, ws, st);
 }
