@@ -230,7 +230,9 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
 
     // ---- the steps of a tile of 32 keys
     struct Packed { Terms<T> w[2]; };                   // weights as operands: 16 keys each
-    float kg[8], vg[8];                                // a block's scales, of eight keys each
+    // A block's scales, of eight keys each: of keys, with what else a product is multiplied by; of values, as a factor F vs / S (two terms), or
+    // that factor's logarithm and reciprocal.
+    float kg[8], vg[8], lv[8];
     auto products = [&](const char* kb, int k, v16f& sc) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[r] = 0.f;
@@ -244,17 +246,36 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
         }
         if constexpr (T == 2) sc += low;
     };
-    // Weights of a tile's scores, and their sums.  (Without cap and bias scores stay products until here: y - m is rounded once.)
+    // Behind a matrix instruction of 8 passes 12 others have to be issued before its result is read.  The compiler sees to that, but not where a
+    // branch that may be skipped lies between (it counts the longer way): weights were taken relative to a maximum of numbers that were
+    // not there yet.
+    auto arrive = [&](v16f& sc) { asm volatile("s_nop 11" : "+v"(sc)); };
+    // Weights of a tile's scores as they enter the second product, w F vs / S (F = 2^11), and the sums of w alone.  (Without cap and bias scores
+    // stay products until here: y - m is rounded once.)  One term: the factor is part of the exponent, and goes out of the sum for four keys
+    // at once, which takes an instruction less a score and costs 2^-20 of a weight.  Two terms: the weight, then the product.
     auto weigh = [&](const v16f& sc, Packed& out, int k) {
         const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             float w[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                w[e] = __builtin_amdgcn_exp2f(GENERAL ? sc[8 * u + e] - base : fmaf(sc[8 * u + e], kg[4 * k + 2 * u + e / 4], -base));
-                l += w[e];
-                w[e] *= vg[4 * k + 2 * u + e / 4];
+            for (int q = 0; q < 2; ++q) {
+                const int g = 4 * k + 2 * u + q;
+                const float less = T == 1 ? lv[g] - base : -base;
+#pragma unroll
+                for (int e = 4 * q; e < 4 * q + 4; ++e) {
+                    const float y = sc[8 * u + e];
+                    w[e] = __builtin_amdgcn_exp2f(GENERAL ? y + less : fmaf(y, kg[g], less));
+                }
+                if constexpr (T == 1) {
+                    l = fmaf((w[4 * q] + w[4 * q + 1]) + (w[4 * q + 2] + w[4 * q + 3]), vg[g], l);
+                } else {
+#pragma unroll
+                    for (int e = 4 * q; e < 4 * q + 4; ++e) {
+                        l += w[e];
+                        w[e] *= vg[g];
+                    }
+                }
             }
             out.w[u] = terms_of<T>(w);
         }
@@ -281,6 +302,10 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
             for (int d = 0; d < DT; ++d)
 #pragma unroll
                 for (int n = 0; n < T; ++n) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.x[u * DT + d], p.w[u].t[n], o[d], 0, 0, 0);
+    };
+    // the compiler is told to have these now
+    auto hold = [&](Packed& p) {
+        if constexpr (T == 1) asm volatile("" : "+v"(p.w[0].t[0]), "+v"(p.w[1].t[0]), "+v"(l));
     };
     // The maximum moves only when it is off by 2^4; what was summed with the old one follows.
     // (first: what has to be added with the old one before)
@@ -369,16 +394,21 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
                     top_scale = up;
                     down = 1.f / up;
                 }
-                // (never 0: an unseen key's product is -inf)
-                const float kq = fmaxf(now.kscale * qc, 0x1p-126f), vq = vscale * down * 2048.f;
+                // (never 0: an unseen key's product is -inf, and a page of zeros still has weights; 2^-60 is nothing beside 2^11)
+                const float kq = fmaxf(now.kscale * qc, 0x1p-126f), vq = vscale * down * 2048.f, vn = fmaxf(vq, 0x1p-60f);
+                const float logarithm = __builtin_amdgcn_logf(vn);
+                // (of the logarithm as it is, rounded: what goes out of the sum is what went in)
+                const float factor = T == 1 ? __builtin_amdgcn_exp2f(-logarithm) : vq;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     kg[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(kq), 8 * i));
-                    vg[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vq), 8 * i));
+                    vg[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(factor), 8 * i));
+                    if constexpr (T == 1) lv[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(logarithm), 8 * i));
                 }
             }
             // a tile's scores made ready: scales, cap, bias, mask, and a maximum that will do for them
             auto ready = [&](v16f& sc, int k, auto first) {
+                arrive(sc);
                 if constexpr (GENERAL) {
 #pragma unroll
                     for (int r = 0; r < 16; ++r) sc[r] *= kg[4 * k + r / 4];
@@ -398,15 +428,35 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
                 raise(sc, k, first);
             };
             // (Order and priorities as in the kernel of the other types: the weights of one tile are taken while the other's products run.)
+            constexpr int MFMAS = CS * T, VALU = 88;
             v16f s0, s1;
             Packed p0, p1;
             __builtin_amdgcn_s_setprio(1);
             products(kb, 0, s0);
+            if constexpr (T == 1) {
+                __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+                for (int i = 0; i < CS - AHEAD; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                }
+                __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+            }
             __builtin_amdgcn_s_setprio(0);
             ready(s0, 0, [] {});
             __builtin_amdgcn_s_setprio(1);
             products(kb, 1, s1);
             weigh(s0, p0, 0);
+            hold(p0);                                  // (here, and not where they are used)
+            if constexpr (T == 1) {
+                __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 1);
+#pragma unroll
+                for (int i = 0; i < MFMAS; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+                    if (i < MFMAS - AHEAD) __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+                    __builtin_amdgcn_sched_group_barrier(0x002, VALU / MFMAS, 1);
+                }
+            }
             __builtin_amdgcn_s_setprio(0);
             ready(s1, 1, [&] {
                 values(fetch(vb, 0), p0);
@@ -418,9 +468,18 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
             });
             __builtin_amdgcn_s_setprio(1);
             const Operands f0 = fetch(vb, 0);
+            __builtin_amdgcn_sched_barrier(0);
             values(f0, p0);
             weigh(s1, p1, 1);
+            if constexpr (T == 1) {
+#pragma unroll
+                for (int i = 0; i < 2 * DT; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 2);
+                    __builtin_amdgcn_sched_group_barrier(0x002, VALU / (2 * DT), 2);
+                }
+            }
             const Operands f1 = fetch(vb, 1);
+            __builtin_amdgcn_sched_barrier(0);
             values(f1, p1);
             __builtin_amdgcn_s_setprio(0);
         }
