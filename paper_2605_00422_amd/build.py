@@ -17,7 +17,7 @@ SOURCES = ["api.hip", "pack.hip", "rotate_quant.hip", "gemm_decode.hip", "gemm_d
            "attention_api.hip", "attention_rope.hip", "attention_split.hip", "attention_tile.hip", "attention_tile_f32.hip",
            "attention_weights.hip", "cache_evict.hip",
            "attention8_api.hip", "attention_norm.hip", "attention8_split.hip", "attention8_split_f32.hip", "attention8_tile.hip",
-           "attention8_tile_f32.hip", "batch_build.hip"]
+           "attention8_tile_e4m3.hip", "attention8_tile_f32.hip", "attention8_tile_f32_e4m3.hip", "batch_build.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",

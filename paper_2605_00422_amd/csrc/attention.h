@@ -120,7 +120,9 @@ struct Att8 {
 hipError_t bwla_launch_attention8_split(const AttArgs& a, const Att8& e, const AttSplit& s, int dtype, void* ws, hipStream_t st);
 hipError_t bwla_launch_attention8_split_f32(const AttArgs& a, const Att8& e, const AttSplit& s, void* ws, hipStream_t st);
 hipError_t bwla_launch_attention8_tile(const AttArgs& a, const Att8& e, const AttSplit& s, int dtype, void* ws, hipStream_t st);
+hipError_t bwla_launch_attention8_tile_e4m3(const AttArgs& a, const Att8& e, const AttSplit& s, void* ws, hipStream_t st);
 hipError_t bwla_launch_attention8_tile_f32(const AttArgs& a, const Att8& e, const AttSplit& s, void* ws, hipStream_t st);
+hipError_t bwla_launch_attention8_tile_f32_e4m3(const AttArgs& a, const Att8& e, const AttSplit& s, void* ws, hipStream_t st);
 
 struct BuildArgs {
     int32_t* ring;

@@ -30,8 +30,17 @@ struct At8Shape {
 template <int T, int DP>
 constexpr int at8_groups() { return T == 2 || DP == 256 ? 1 : 2; }     // workgroups of a compute unit
 
-// T: terms of queries and weights, 1 for bf16, 2 for fp32; DP: columns, 64, 128 or 256; EXACT: d == DP; FORM: AttForm, scale, cap and bias
-template <int T, int DP, bool EXACT, int FORM>
+// whether any lane has it: a scalar, so that what depends on it is a jump
+__device__ __forceinline__ bool some(bool x) { return __builtin_amdgcn_ballot_w64(x) != 0; }
+// (fmaxf would make each number a quiet one first)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
+// T: terms of queries and weights, 1 for bf16, 2 for fp32; I8: integers (else e4m3); DP: columns, 64, 128 or 256; EXACT: d == DP; FORM: AttForm, scale, cap and bias
+template <int T, bool I8, int DP, bool EXACT, int FORM>
 __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_tile_kernel(AttArgs a, Att8 e8, AtOrder order, AttSplit sp,
                                                                                       float* __restrict__ part, float4* __restrict__ stat) {
     using S = At8Shape<DP>;
@@ -92,7 +101,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
             for (int e = 0; e < 8; ++e) v[e] = ldexpf(value(c, e), 14 - up);
             qf[c] = terms_of<T>(v);
         }
-        qc = ldexpf(GENERAL ? 1.f : a.c1, up - 14);
+        qc = ldexpf(GENERAL && a.capped != 0.f ? 1.f : a.c1, up - 14);
     }
     // indexes of the first and last row of this wavefront, and of the workgroup
     const int old = s.old;
@@ -156,12 +165,18 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
     // from there.  Pieces lie in LDS at piece ^ (key & KSW) of a row of keys, piece ^ (key & VSW) * 2 of values.
     constexpr int KSW = (CH < 16 ? CH : 16) - 1, VSW = CH < 16 ? 3 : 7;
     struct Found { int page, pos, doc; };
+    // (without positions or documents an entry of the table is read for them and dropped: no branch lies in the way of what overlaps)
+    const int32_t* const positions = s.pos ? s.pos : s.table;
+    const int32_t* const documents = s.doc ? s.doc : s.table;
+    const int has_pos = s.pos ? -1 : 0, has_doc = s.doc ? -1 : 0;
     auto look = [&](int t) {                           // (kept as loaded: nothing here waits)
         Found f;
         const int j = t * BK + lane, in = min(j, s.n - 1);
         f.page = s.table[in >> a.page_shift];
-        f.pos = s.pos ? s.pos[in] : j;
-        f.doc = s.doc ? s.doc[in] : 0;
+        f.pos = positions[in & has_pos];
+        f.doc = documents[in & has_doc];
+        f.pos = has_pos ? f.pos : j;
+        f.doc = has_doc ? f.doc : 0;
         return f;
     };
     struct Key { int64_t at; int p, doc; float kscale, vscale; };              // doc: -1 where the key does not exist
@@ -191,8 +206,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
             got_v[i] = in ? *(const v4u*)(vh + piece * 16 + off) : v4u{0, 0, 0, 0};
         }
     };
-    auto put_codes = [&](int buf, auto i8) {
-        constexpr bool I8 = decltype(i8)::value;
+    auto put_block = [&](int buf) {
 #pragma unroll
         for (int i = 0; i < S::PIECES; ++i) {
             const int key = key0 + i * STEP;
@@ -206,11 +220,6 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
                 *(v4u*)(vr + ((2 * piece + p) ^ (key & VSW) * 2) * 16) = v4u{v0.lo, v0.hi, v1.lo, v1.hi};
             }
         }
-    };
-    const bool ints = e8.code == BWLA_CODE_I8;
-    auto put_block = [&](int buf) {
-        if (ints) put_codes(buf, std::true_type{});
-        else put_codes(buf, std::false_type{});
     };
 
     v16f o[DT];
@@ -310,14 +319,15 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
     // The maximum moves only when it is off by 2^4; what was summed with the old one follows.
     // (first: what has to be added with the old one before)
     auto raise = [&](const v16f& sc, int k, auto first) {
-        float top = -INFINITY;
+        float four[4];
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            const float four = fmaxf(fmaxf(sc[4 * g], sc[4 * g + 1]), fmaxf(sc[4 * g + 2], sc[4 * g + 3]));
-            top = fmaxf(top, GENERAL ? four : four * kg[4 * k + g]);
+            four[g] = max3(sc[4 * g], sc[4 * g + 1], max3(sc[4 * g + 2], sc[4 * g + 3], -INFINITY));
+            if constexpr (!GENERAL) four[g] *= kg[4 * k + g];
         }
+        float top = max3(four[0], four[1], max3(four[2], four[3], -INFINITY));
         top = half_max(top);
-        if (__builtin_expect(att_uniform(__any(top > m + 4.f)), 0)) {
+        if (__builtin_expect(some(top > m + 4.f), 0)) {
             first();
             const float now = fmaxf(m, top);
             const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
@@ -349,23 +359,28 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
         const char* const kb = ks + buf * S::TILE;
         const char* const vb = vs + buf * S::TILE;
         bwla_lds_barrier();                            // everyone's codes of the block are there, and the other buffer is free
-        Key after = next;
-        if (t2 < end) after = settle(far, t2);
-        if (t3 < end) far = look(t3);
-        if (t1 < end) fetch_codes(next.at);
+        // What comes next: codes of t1, addresses of t2, entries of t3 (or, at the end, of the last block once more: no branches).  Its
+        // instructions go between the first products, its conversions between the last ones.
+        Key after;
+        auto prepare = [&] {
+            fetch_codes(next.at);
+            after = settle(far, min(t2, end - 1));
+            far = look(min(t3, end - 1));
+        };
+        prepare();
         // Even: every key exists and is of one document, and in reach of the windows, so that a row of that document sees those up
         // to its index, or all of the prefix.  Else each wavefront works out what each of its rows sees (a bit for each key).  Values
         // of keys that no row of the workgroup sees may be anything: integers get a weight of 0, but e4m3 codes may be NaN and are
         // cleared.
         const int doc = __builtin_amdgcn_readfirstlane(now.doc);
-        const bool even = doc >= 0 && att_uniform(__all(now.doc == doc) &&
-                                                  (a.window == INT32_MAX || (!s.pos && j0 > g_last - a.window) || j0 + BK <= s.prefix));
+        const bool even = doc >= 0 && !some(now.doc != doc) &&
+                          (a.window == INT32_MAX || (!s.pos && j0 > g_last - a.window) || j0 + BK <= s.prefix);
         const bool mine = me.doc == doc;
         uint64_t ok = ALL, any = ALL;
         if (__builtin_expect(!even, 0)) {
             ok = att_seen(a, s, me, j0, now.p, now.doc);
             any = att_rows_or(ok);
-            if (!ints) {
+            if constexpr (!I8) {
                 uint64_t* const seen = (uint64_t*)(smem + 4 * S::TILE + AT_MAP / 8 + 2 * AT_WAVES * 4);
                 if (lane == 0) seen[wave] = any;
                 bwla_lds_barrier();
@@ -378,14 +393,14 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
                 bwla_lds_barrier();
             }
         }
-        if (att_uniform(even ? __any(mine) && (j0 <= w_last || j0 < s.prefix) : any != 0)) {
+        if (even ? some(mine) && (j0 <= w_last || j0 < s.prefix) : any != 0) {
             // every row sees every key
-            const bool whole = even && att_uniform(__all(mine | blind)) && (j0 + BK - 1 <= w_first || j0 + BK <= s.prefix);
+            const bool whole = even && !some(!(mine | blind)) && (j0 + BK - 1 <= w_first || j0 + BK <= s.prefix);
             // scales of pages of which no row sees a key may be anything, and count as 0
             {
-                const bool in_use = ((any >> (lane & 56)) & 0xff) != 0;
+                const bool in_use = even || ((any >> (lane & 56)) & 0xff) != 0;
                 const float vscale = in_use ? now.vscale : 0.f;
-                if (__builtin_expect(att_uniform(__any(vscale > top_scale)), 0)) {
+                if (__builtin_expect(some(vscale > top_scale), 0)) {
                     const float up = fmaxf(bwla_wave_max(vscale), top_scale), f = top_scale / up;
 #pragma unroll
                     for (int d = 0; d < DT; ++d)
@@ -399,11 +414,18 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
                 const float logarithm = __builtin_amdgcn_logf(vn);
                 // (of the logarithm as it is, rounded: what goes out of the sum is what went in)
                 const float factor = T == 1 ? __builtin_amdgcn_exp2f(-logarithm) : vq;
+                const auto of = [](float v, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane)); };
+                if (a.page_shift >= 6 && even) {               // one page: its scales are all of them
+                    const float k0 = of(kq, 0), v0 = of(factor, 0), l0 = of(logarithm, 0);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    kg[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(kq), 8 * i));
-                    vg[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(factor), 8 * i));
-                    if constexpr (T == 1) lv[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(logarithm), 8 * i));
+                    for (int i = 0; i < 8; ++i) { kg[i] = k0; vg[i] = v0; lv[i] = l0; }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        kg[i] = of(kq, 8 * i);
+                        vg[i] = of(factor, 8 * i);
+                        if constexpr (T == 1) lv[i] = of(logarithm, 8 * i);
+                    }
                 }
             }
             // a tile's scores made ready: scales, cap, bias, mask, and a maximum that will do for them
@@ -412,7 +434,23 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
                 if constexpr (GENERAL) {
 #pragma unroll
                     for (int r = 0; r < 16; ++r) sc[r] *= kg[4 * k + r / 4];
-                    att_transform<FORM>(a, sc, me.p, slope, j0, k, now.p, s.pos != nullptr);
+                    if (a.capped != 0.f) {
+                        const float c3 = a.c2 * (2.f * ATT_LOG2E);
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            if constexpr (FORM == ATT_SHORT) sc[r] = fmaf(-2.f * a.capped, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(sc[r] * c3)), a.capped);
+                            else sc[r] = a.capped * att_tanh(sc[r] * a.c2);
+                        }
+                    }
+                    if (a.slopes && s.pos) {
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            sc[r] = fmaf(-slope, fabsf((float)(me.p - __shfl(now.p, k * 32 + (r & 3) + 8 * (r >> 2) + 4 * hf, 64))), sc[r]);
+                    } else if (a.slopes) {
+                        const float away = (float)(me.p - j0 - k * 32 - 4 * hf);
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) sc[r] = fmaf(-slope, fabsf(away - (float)((r & 3) + 8 * (r >> 2))), sc[r]);
+                    }
                 }
                 if (!__builtin_expect(whole, 1)) {
                     if (even) {
@@ -433,15 +471,6 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
             Packed p0, p1;
             __builtin_amdgcn_s_setprio(1);
             products(kb, 0, s0);
-            if constexpr (T == 1) {
-                __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
-#pragma unroll
-                for (int i = 0; i < CS - AHEAD; ++i) {
-                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                }
-                __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
-            }
             __builtin_amdgcn_s_setprio(0);
             ready(s0, 0, [] {});
             __builtin_amdgcn_s_setprio(1);
@@ -483,7 +512,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
             values(f1, p1);
             __builtin_amdgcn_s_setprio(0);
         }
-        if (t1 < end) put_block(buf ^ 1);
+        put_block(buf ^ 1);
         now = next;
         next = after;
         t = t1;
@@ -519,7 +548,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
     if (hf == 0) att_put_lse(a, at, m, l);
 }
 
-template <int T, int DP>
+template <int T, bool I8, int DP>
 hipError_t at8_launch(const AttArgs& a, const Att8& e8, const AttSplit& sp, void* ws, hipStream_t st) {
     const int tiles = (sp.rows + AT_ROWS - 1) / AT_ROWS;
     const int units = a.seqs * a.hkv;
@@ -536,16 +565,16 @@ hipError_t at8_launch(const AttArgs& a, const Att8& e8, const AttSplit& sp, void
         kernel<<<dim3((unsigned)((int64_t)tiles * units * sp.splits)), 64 * AT_WAVES, lds, st>>>(a, e8, order, sp, part, stat);
         return hipGetLastError();
     };
-    if (form == ATT_PLAIN) return exact ? go(att8_tile_kernel<T, DP, true, ATT_PLAIN>) : go(att8_tile_kernel<T, DP, false, ATT_PLAIN>);
+    if (form == ATT_PLAIN) return exact ? go(att8_tile_kernel<T, I8, DP, true, ATT_PLAIN>) : go(att8_tile_kernel<T, I8, DP, false, ATT_PLAIN>);
     constexpr int SHORT = T == 1 ? ATT_SHORT : ATT_LONG;
-    if (form == SHORT) return exact ? go(att8_tile_kernel<T, DP, true, SHORT>) : go(att8_tile_kernel<T, DP, false, SHORT>);
-    return exact ? go(att8_tile_kernel<T, DP, true, ATT_LONG>) : go(att8_tile_kernel<T, DP, false, ATT_LONG>);
+    if (form == SHORT) return exact ? go(att8_tile_kernel<T, I8, DP, true, SHORT>) : go(att8_tile_kernel<T, I8, DP, false, SHORT>);
+    return exact ? go(att8_tile_kernel<T, I8, DP, true, ATT_LONG>) : go(att8_tile_kernel<T, I8, DP, false, ATT_LONG>);
 }
-template <int T>
+template <int T, bool I8>
 hipError_t at8_launch_columns(const AttArgs& a, const Att8& e8, const AttSplit& s, void* ws, hipStream_t st) {
-    if (a.d <= 64) return at8_launch<T, 64>(a, e8, s, ws, st);
-    if (a.d <= 128) return at8_launch<T, 128>(a, e8, s, ws, st);
-    return at8_launch<T, 256>(a, e8, s, ws, st);
+    if (a.d <= 64) return at8_launch<T, I8, 64>(a, e8, s, ws, st);
+    if (a.d <= 128) return at8_launch<T, I8, 128>(a, e8, s, ws, st);
+    return at8_launch<T, I8, 256>(a, e8, s, ws, st);
 }
 
 }  // namespace
