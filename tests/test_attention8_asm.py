@@ -6,9 +6,11 @@ import subprocess
 
 import pytest
 
+import mfma_waits
 from paper_2605_00422_amd import build
 
-FILES = ["attention8_split.hip", "attention8_split_f32.hip", "attention8_tile.hip", "attention8_tile_f32.hip"]
+FILES = ["attention8_split.hip", "attention8_split_f32.hip", "attention8_tile.hip", "attention8_tile_e4m3.hip", "attention8_tile_f32.hip",
+         "attention8_tile_f32_e4m3.hip"]
 
 
 @pytest.fixture(scope="module")
@@ -38,9 +40,31 @@ def test_no_mfma_under_a_narrowed_mask(asm, name):
 
 
 @pytest.mark.parametrize("name", FILES)
+def test_results_of_matrix_instructions_are_waited_for(asm, name):
+    found = 0
+    for kernel, body in mfma_waits.kernels(asm[name]):
+        found += 1
+        early = mfma_waits.early_reads(body)
+        assert not early, (kernel, early[:3])
+    assert found >= 12
+
+
+def test_an_early_read_is_found():
+    """The way around a branch that may be skipped counts, and so does a loop's way back."""
+    ahead = ["v_mfma_f32_32x32x16_f16 v[0:15], v[16:19], v[20:23], 0", "s_cbranch_scc0 .LBB0_2"]
+    long = [".LBB0_1:"] + ["v_add_f32_e32 v30, v31, v31"] * 20
+    assert mfma_waits.early_reads(ahead + long + [".LBB0_2:", "v_max_f32_e32 v30, v3, v3", "s_endpgm"])
+    assert not mfma_waits.early_reads(ahead + long + [".LBB0_2:", "s_nop 11", "v_max_f32_e32 v30, v3, v3", "s_endpgm"])
+    assert not mfma_waits.early_reads(ahead[:1] + long + [".LBB0_2:", "v_max_f32_e32 v30, v3, v3", "s_endpgm"])
+    loop = [".LBB0_1:", "v_add_f32_e32 v30, v4, v4", "v_mfma_f32_16x16x32_f16 v[4:7], v[16:19], v[20:23], v[4:7]", "s_cbranch_scc0 .LBB0_1", "s_endpgm"]
+    assert mfma_waits.early_reads(loop) and not mfma_waits.early_reads(loop[:3] + ["s_nop 6"] + loop[3:])
+
+
+@pytest.mark.parametrize("name", FILES)
 def test_codes_become_halves_without_a_detour(asm, name):
     """e4m3 codes by the conversion of pairs, integers by permutes and a packed addition: no conversions of single codes to fp32."""
     text = "\n".join(asm[name])
-    assert "v_cvt_scalef32_pk_f16_fp8" in text and "v_pk_add_f16" in text
+    both = "split" in name
+    assert ("v_cvt_scalef32_pk_f16_fp8" in text) == (both or "e4m3" in name) and ("v_pk_add_f16" in text) == (both or "e4m3" not in name)
     assert "v_cvt_f32_fp8" not in text
     assert "v_pk_fma_f32" not in text and "v_pk_mul_f32" not in text and "v_pk_add_f32" not in text
