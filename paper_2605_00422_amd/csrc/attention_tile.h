@@ -351,6 +351,9 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
             const bool whole = even && att_uniform(__all(mine | blind)) && (j0 + BK - 1 <= w_first || j0 + BK <= s.prefix);
             // a tile's scores made ready: cap, bias, mask, and a maximum that will do for them
             auto ready = [&](v16f& sc, int k, auto first) {
+                // (The compiler counts what has to be issued behind the last product by the way through the mask: where no mask is needed the
+                // maximum was taken of four numbers that were still to come.)
+                if constexpr (!BF) asm volatile("s_nop 15\n\ts_nop 1" : "+v"(sc));
                 if constexpr (GENERAL) att_transform<FORM>(a, sc, me.p, slope, j0, k, now.p, s.pos != nullptr);
                 bool fine = false;
                 if (__builtin_expect(whole, 1)) {
