@@ -611,8 +611,8 @@ typedef struct bwla_kv_cache8 {
 /*
  * bwla_norm_rope_append into such a cache (norm may be NULL).  With A the largest magnitude among the new tokens' values of a page and
  * head (after norm and rotation, in fp32):
- *   where no token of the sequence lies in the page in front of the new ones, or the scale is 0:  scale = A / top, at least 2^-126
- *   (0 where A is 0);  else the scale stays where A <= top * scale (a product of fp32), or is doubled until that holds, and the codes c of
+ *   where no token of the sequence lies in the page in front of the new ones, or the scale is 0 (codes in front become 0 then):
+ *   scale = A / top, at least 2^-126 (0 where A is 0);  else the scale stays where A <= top * scale (a product of fp32), or is doubled until that holds, and the codes c of
  *   the tokens in front, after n doublings, become c / 2^n;  codes: value / scale.  All to the nearest code, ties to even.
  * A value is then off by half a step of its scale at most when it is written, and by one step of the last scale whatever follows (i8;
  * e4m3 codes halve exactly down to 2^-6).  Values that are not finite do not move a scale: infinities become the largest code, NaN 0.

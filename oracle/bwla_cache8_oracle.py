@@ -37,7 +37,7 @@ def grow(code, scale, most, fresh):
     if fresh or not scale > 0:
         return (max(most / top, 2.0 ** -126) if most > 0 else 0.0), 0
     n, room = 0, float(np.float32(top) * np.float32(scale))    # (the product as fp32 has it: what once set a scale does not double it)
-    while most > room * 2.0 ** n:
+    while most > room * 2.0 ** n or (most > 0 and scale * 2.0 ** n < 2.0 ** -126):
         n += 1
     return scale * 2.0 ** n, n
 
@@ -47,7 +47,10 @@ def append(code, codes, scale, values, inside):
     returns the scale and the number of doublings."""
     values = np.asarray(values, np.float64)
     finite = np.abs(values[np.isfinite(values)])
+    was = scale
     scale, n = grow(code, scale, float(finite.max()) if finite.size else 0.0, inside == 0)
+    if not was > 0 and scale > 0:
+        codes[:inside] = 0                             # (what they stood for)
     if n:
         codes[:inside] = nearest(code, codes[:inside] / 2.0 ** n)
     with np.errstate(all="ignore"):

@@ -83,7 +83,7 @@ __global__ __launch_bounds__(64 * SP_WAVES, (DP == 256 ? 1 : 2)) void att8_split
     const AttRow me = att_row(s, tok, row < rows);
     [[maybe_unused]] const float slope = FORM != ATT_PLAIN && a.slopes && row < rows ? a.slopes[head] * ATT_LOG2E : 0.f;
     Terms<T> qf[KS][2];
-    float qc;                                  // what a product is to be multiplied by, but for the page's scale
+    int q_exponent;                            // ... of the power of two that was taken out of the row
     {
         const char* qp = a.q + (int64_t)(s.row0 + (row < rows ? tok : 0)) * a.q_bytes + (int64_t)(row < rows ? head : 0) * a.d * ES;
         float x[KS][16], most = 0.f;
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(64 * SP_WAVES, (DP == 256 ? 1 : 2)) void att8_split
             qf[u][0] = terms_of<T>(x[u]);
             qf[u][1] = terms_of<T>(x[u] + 8);
         }
-        qc = ldexpf(FORM != ATT_PLAIN && a.capped != 0.f ? 1.f : a.c1, up - 14);
+        q_exponent = up - 14;
     }
     __syncthreads();
 
@@ -203,7 +203,7 @@ __global__ __launch_bounds__(64 * SP_WAVES, (DP == 256 ? 1 : 2)) void att8_split
                     for (int n = 0; n < T; ++n)
                         acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, x), qf[u][i].t[n], acc, 0, 0, 0);
                 }
-            const float kq = ks_v[t] * qc;
+            const float kq = ldexpf(ks_v[t], q_exponent) * (FORM != ATT_PLAIN && a.capped != 0.f ? 1.f : a.c1);
 #pragma unroll
             for (int r = 0; r < 4; ++r) y[t][r] = acc[r] * kq;
         }
@@ -249,7 +249,7 @@ __global__ __launch_bounds__(64 * SP_WAVES, (DP == 256 ? 1 : 2)) void att8_split
         float over[2] = {used[0] ? vs_v[0] : 0.f, used[1] ? vs_v[1] : 0.f};
         if (j0 + STRIDE < c1) load_keys(j0 + STRIDE);
         if (att_uniform(__any(now_s > S))) {
-            now_s = fmaxf(S, xor32(xor16(now_s, true), true));
+            now_s = fmaxf(fmaxf(S, xor32(xor16(now_s, true), true)), 0x1p-126f);    // (a reciprocal has to be there)
             const float f = S / now_s;
 #pragma unroll
             for (int t = 0; t < NT; ++t) o[t] *= f;
@@ -323,7 +323,8 @@ __global__ __launch_bounds__(64 * SP_WAVES, (DP == 256 ? 1 : 2)) void att8_split
 #pragma unroll
     for (int w = 0; w < SP_WAVES; ++w)
         if (s_m[w][li] != -INFINITY) ll += s_l[w][li] * __builtin_amdgcn_exp2f(s_m[w][li] - mm);
-    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mm) * (S * 0x1p-15f);
+    // (one after the other: their product may have few bits)
+    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mm), back = S * 0x1p-15f;
     // lane (row li, g) holds columns 128 u + 4 CW g + CW r + c
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -332,7 +333,7 @@ __global__ __launch_bounds__(64 * SP_WAVES, (DP == 256 ? 1 : 2)) void att8_split
 #pragma unroll
             for (int c = 0; c < CW; c += 4)
                 *(float4*)&s_o[wave][li][u * 16 * CW + 4 * CW * g + CW * r + c] =
-                    make_float4(o[u * CW + c][r] * f, o[u * CW + c + 1][r] * f, o[u * CW + c + 2][r] * f, o[u * CW + c + 3][r] * f);
+                    make_float4(o[u * CW + c][r] * f * back, o[u * CW + c + 1][r] * f * back, o[u * CW + c + 2][r] * f * back, o[u * CW + c + 3][r] * f * back);
     if (wave == 0 && g == 0) {
         if (parts) stat[at_part * 16 + li] = make_float4(att_part_max(mm, ll), ll, ll, 0.f);
         s_mm[li] = mm;

@@ -70,7 +70,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
     // rows that see nothing whatever the block: what they gather on the way, from queries of 0, is dropped at the end
     const bool blind = me.doc < 0;
     Terms<T> qf[CS];
-    float qc;                                          // what a product is to be multiplied by, but for the page's scale
+    int q_exponent;                                    // ... of the power of two that was taken out of the rows
     {
         const char* qp = a.q + (int64_t)(s.row0 + tok) * a.q_bytes + (int64_t)head * a.d * ES;
         v4u raw[CS][ES / 2];
@@ -101,7 +101,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
             for (int e = 0; e < 8; ++e) v[e] = ldexpf(value(c, e), 14 - up);
             qf[c] = terms_of<T>(v);
         }
-        qc = ldexpf(GENERAL && a.capped != 0.f ? 1.f : a.c1, up - 14);
+        q_exponent = up - 14;
     }
     // indexes of the first and last row of this wavefront, and of the workgroup
     const int old = s.old;
@@ -401,7 +401,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
                 const bool in_use = even || ((any >> (lane & 56)) & 0xff) != 0;
                 const float vscale = in_use ? now.vscale : 0.f;
                 if (__builtin_expect(some(vscale > top_scale), 0)) {
-                    const float up = fmaxf(bwla_wave_max(vscale), top_scale), f = top_scale / up;
+                    const float up = fmaxf(fmaxf(bwla_wave_max(vscale), top_scale), 0x1p-126f), f = top_scale / up;       // (a reciprocal has to be there)
 #pragma unroll
                     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -410,7 +410,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
                     down = 1.f / up;
                 }
                 // (never 0: an unseen key's product is -inf, and a page of zeros still has weights; 2^-60 is nothing beside 2^11)
-                const float kq = fmaxf(now.kscale * qc, 0x1p-126f), vq = vscale * down * 2048.f, vn = fmaxf(vq, 0x1p-60f);
+                const float kq = fmaxf(ldexpf(now.kscale, q_exponent) * (GENERAL && a.capped != 0.f ? 1.f : a.c1), 0x1p-126f), vq = vscale * down * 2048.f, vn = fmaxf(vq, 0x1p-60f);
                 const float logarithm = __builtin_amdgcn_logf(vn);
                 // (of the logarithm as it is, rounded: what goes out of the sum is what went in)
                 const float factor = T == 1 ? __builtin_amdgcn_exp2f(-logarithm) : vq;
@@ -536,14 +536,14 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
         }
         return;
     }
-    const float over = att_over(l, l) * back;
+    const float over = att_over(l, l);                 // (apart from `back`: their product may have few bits)
     const int64_t at = (int64_t)(s.row0 + tok) * a.hq + head;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
             const int c = 32 * d + 2 * r + 4 * hf;
-            if (EXACT || c < a.d) att_put<BF>(a, at, c, make_float4(o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]), over);
+            if (EXACT || c < a.d) att_put<BF>(a, at, c, make_float4(o[d][r] * back, o[d][r + 1] * back, o[d][r + 2] * back, o[d][r + 3] * back), over);
         }
     if (hf == 0) att_put_lse(a, at, m, l);
 }

@@ -262,13 +262,16 @@ __device__ __forceinline__ float block_max(float v, float* words) {
     for (int w = 0; w < (int)blockDim.x / 64; ++w) v = fmaxf(v, words[w]);
     return v;
 }
+// x / scale, to the last bit but for a few: with the reciprocal alone quotients that lie in the middle of two codes, as those of bf16 values
+// often do, would go either way.
 template <bool I8, int VEC>
-__device__ __forceinline__ void put_codes(uint8_t* dst, const float* x, float over) {
+__device__ __forceinline__ void put_codes(uint8_t* dst, const float* x, float scale, float over) {
     constexpr float top = code_top<I8>();
     float y[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
-        const float v = fminf(fmaxf(x[e] * over, -top), top);
+        const float q = x[e] * over, better = fmaf(fmaf(-q, scale, x[e]), over, q);
+        const float v = fminf(fmaxf(fabsf(x[e]) <= 3.402823466e38f ? better : q, -top), top);
         y[e] = x[e] == x[e] ? v : 0.f;
     }
     if constexpr (VEC >= 4) {
@@ -370,17 +373,18 @@ __global__ __launch_bounds__(1024) void norm_rope8_kernel(NormArgs n, Items it, 
     int doubled = 0;
     if (!(was > 0.f)) {
         scale = most > 0.f ? fmaxf(most / top, 0x1p-126f) : 0.f;
+        doubled = inside > 0 && scale > 0.f ? 1000 : 0;                  // (older codes stood for 0)
     } else {
         // the least number of doublings with most <= (top * was) 2^n
         const float room = top * was;
         if (most > room) {
             doubled = ilogbf(most) - ilogbf(room);
             if (most > ldexpf(room, doubled)) ++doubled;
-            scale = ldexpf(was, doubled);
         }
+        if (most > 0.f && ldexpf(was, doubled) < 0x1p-126f) doubled = -126 - ilogbf(was);    // (of which there is no reciprocal)
+        scale = ldexpf(was, doubled);
     }
-    if (threadIdx.x == 0 && scale != was) *scale_at = scale;
-    if (threadIdx.x == 0 && inside == 0) *scale_at = scale;
+    if (threadIdx.x == 0) *scale_at = scale;
     if (doubled > 0) {
         const int pieces = a.d / 16;
         for (int i = threadIdx.x; i < inside * pieces; i += blockDim.x) {
@@ -393,7 +397,7 @@ __global__ __launch_bounds__(1024) void norm_rope8_kernel(NormArgs n, Items it, 
             *at = w;
         }
     }
-    const float over = scale > 0.f ? 1.f / scale : 0.f;
+    const float over = scale >= 0x1p-126f ? 1.f / scale : 0.f;
     auto put = [&](int t, const float (&y)[IT][2 * VEC]) {
         if (t >= count) return;
         uint8_t* const dst = (uint8_t*)base + (int64_t)((from + t) & (size - 1)) * a.slot_stride;
@@ -402,8 +406,8 @@ __global__ __launch_bounds__(1024) void norm_rope8_kernel(NormArgs n, Items it, 
             int lo, hi;
             item_columns(a, VEC, lane + i * it.lanes, kind != 2, lo, hi);
             if (lane + i * it.lanes >= it.items) continue;
-            if (lo >= 0) put_codes<I8, VEC>(dst + lo, y[i], over);
-            if (hi >= 0) put_codes<I8, VEC>(dst + hi, y[i] + VEC, over);
+            if (lo >= 0) put_codes<I8, VEC>(dst + lo, y[i], scale, over);
+            if (hi >= 0) put_codes<I8, VEC>(dst + hi, y[i] + VEC, scale, over);
         }
     };
     put(group, x);

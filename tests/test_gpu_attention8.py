@@ -399,3 +399,32 @@ def test_captured_and_replayed_beside_eager_calls(A, new):
         A.attention8_forward(cache, batch, score, q, eager, None, other)
         torch.cuda.synchronize()
         assert torch.equal(out, eager)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [1, 100])
+@pytest.mark.parametrize("scale", [0.0, 1e-44, 1e-39, 1e30])
+def test_scales_of_values_at_the_edges_of_fp32(A, dtype, new, scale):
+    import torch
+    c = Case("i8", dtype, 64, 4, 2, 16, [150], [new], seed=4)
+    c.vs[c.vs == c.vs] = scale
+    out, lse = call(c, A, {})
+    k = c.kv[0][0]
+    codes = torch.cat([c.v[int(p)].transpose(0, 1) for p in c.table_np[0]])[:150].double().cpu().numpy()
+    want = orc.attend(c.q.double().numpy(), k, codes * np.float64(np.float32(scale)), c.d ** -0.5)[0]
+    assert torch.isfinite(lse).all()
+    # (below 2^-126 outputs are numbers of few bits: half a unit of bf16's or fp32's smallest, and one that products lose)
+    tiny = 2.0 ** -133 * 1.01 if dtype == "bf16" else 2.0 ** -148
+    assert np.all(np.abs(out.double().cpu().numpy() - want) <= np.abs(want).max() * (2.0 ** -7 if dtype == "bf16" else 1e-5) + tiny)
+
+
+@pytest.mark.parametrize("new", [1, 100])
+def test_large_queries_small_keys_and_a_large_scale(A, new):
+    """Factors whose product in another order would leave fp32's range."""
+    c = Case("i8", "f32", 64, 4, 2, 16, [150], [new], seed=4)
+    c.q *= 1e30
+    c.ks *= 1e-36
+    c.kv[0][0] = c.kv[0][0] * 1e-36
+    out, _ = call(c, A, {}, 1e5)
+    want = orc.attend(c.q.double().numpy(), c.kv[0][0], c.kv[0][1], np.float64(np.float32(1e5)))[0]
+    assert np.all(np.abs(out.double().cpu().numpy() - want) <= 1e-4 * np.abs(want).max())

@@ -397,3 +397,14 @@ def test_one_token_at_a_time_ends_where_the_bound_says(A):
     scale = steps.k_scale[c.table.long()][0].repeat_interleave(16, 0)[:37, :, None], steps.v_scale[c.table.long()][0].repeat_interleave(16, 0)[:37, :, None]
     for a, b, s in zip(out[:2], out[2:], scale):
         assert ((a - b).abs() <= 1.51 * s).all()       # (half a step of the other's smaller scale besides)
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("old", [0.0, 1e-44, 1e-39, 2.0 ** -126])
+def test_scales_of_older_tokens_at_the_edge_of_fp32(A, code, old):
+    """A scale of 0 makes zeros of older codes; one without a reciprocal in fp32 is doubled until it has one, whatever the new values."""
+    for size in (1.0, 1e-37, 1e-41):
+        c = Call(A, norm="none", lens=(20, 33), news=(2, 1), seed=15, spread=size)
+        cache = make8(c, code)
+        cache.k_scale.fill_(old), cache.v_scale.fill_(old)
+        check8(A, c, code, cache)
