@@ -272,7 +272,7 @@ __device__ __forceinline__ void put_codes(uint8_t* dst, const float* x, float sc
     for (int e = 0; e < VEC; ++e) {
         const float q = x[e] * over, better = fmaf(fmaf(-q, scale, x[e]), over, q);
         const float v = fminf(fmaxf(fabsf(x[e]) <= 3.402823466e38f ? better : q, -top), top);
-        y[e] = x[e] == x[e] ? v : 0.f;
+        y[e] = q == q ? v : 0.f;                       // (over is 0 where the scale is: infinities become 0 there)
     }
     if constexpr (VEC >= 4) {
         Vec<uint32_t, VEC / 4> w;
@@ -397,7 +397,8 @@ __global__ __launch_bounds__(1024) void norm_rope8_kernel(NormArgs n, Items it, 
             *at = w;
         }
     }
-    const float over = scale >= 0x1p-126f ? 1.f / scale : 0.f;
+    // (a scale below 2^-126: nothing finite but zeros)
+    const float over = scale >= 0x1p-126f ? 1.f / scale : scale > 0.f ? 1.f : 0.f;
     auto put = [&](int t, const float (&y)[IT][2 * VEC]) {
         if (t >= count) return;
         uint8_t* const dst = (uint8_t*)base + (int64_t)((from + t) & (size - 1)) * a.slot_stride;

@@ -309,6 +309,28 @@ def test_zeros_scales_of_zero_and_values_that_are_not_finite(A, code):
 
 
 @pytest.mark.parametrize("code", CODES)
+def test_pages_of_zeros_and_infinities_have_codes_of_zero(A, code):
+    """Nothing finite but zeros: the scale is 0, and so is every code."""
+    c = Call(A, norm="none", lens=(20,), news=(18,), seed=10)
+    cache = make8(c, code)
+    c.qkv[:, c.hq * c.d:] = 0
+    c.qkv[3, (c.hq + c.hkv) * c.d + 7] = float("inf")
+    c.qkv[4, (c.hq + c.hkv) * c.d + 8] = -float("inf")
+    c.append(cache)
+    p, s = c.table_np[0, 5 // 16], 5 % 16              # (rows 3 and 4 are tokens 5 and 6: of a page with older tokens)
+    assert float(cache.v_scale[int(p)].min()) > 0
+    assert numbers(cache.v[int(p), 0, s])[7] == orc.TOP[code] and numbers(cache.v[int(p), 0, s + 1])[8] == -orc.TOP[code]
+    fresh = Call(A, norm="none", lens=(18,), news=(18,), seed=11)
+    cache = make8(fresh, code)
+    fresh.qkv[:, fresh.hq * fresh.d:] = 0
+    fresh.qkv[3, (fresh.hq + fresh.hkv) * fresh.d + 7] = float("inf")
+    fresh.qkv[4, (fresh.hq + fresh.hkv) * fresh.d + 8] = -float("inf")
+    fresh.append(cache)
+    p = int(fresh.table_np[0, 0])
+    assert not cache.v_scale[p].any() and not numbers(cache.v[p, :, :16]).any()
+
+
+@pytest.mark.parametrize("code", CODES)
 def test_rows_and_pages_that_are_left_out(A, code):
     """Rows of no sequence, more new tokens than max_new, new tokens in front of the cache, pages that do not exist: nothing is written."""
     import torch
