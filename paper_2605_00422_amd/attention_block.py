@@ -118,14 +118,14 @@ class Requests:
         zeros = lambda *s: torch.zeros(*s, dtype=torch.int32, device=device)  # noqa: E731
         self.table, self.length, self.first, self.status = zeros(n, -(-max_len // page_size)) - 1, zeros(n), zeros(n + 1), zeros(4)
         self._ws = torch.empty(A.batch_build_workspace_size(n, 0), dtype=torch.uint8, device=device)
-        self._position = {}
+        self._room = [zeros(n)]                        # positions; what a longer step outgrew stays, where captured ones find it
 
     def step(self, new, done=None, rows=None, most: int = 1):
         rows = self.n * most if rows is None else rows
-        if rows not in self._position:                 # (kept: a captured step finds its own)
+        if self._room[-1].shape[0] < rows:
             import torch
-            self._position[rows] = torch.zeros(1, rows, dtype=torch.int32, device=self.device)
-        position = self._position[rows]
+            self._room.append(torch.zeros(max(rows, 2 * self._room[-1].shape[0]), dtype=torch.int32, device=self.device))
+        position = self._room[-1][:rows].view(1, rows)
         A.batch_build(self.pool, self.table, self.length, new, self.length, self.first, self.status, rows, self.max_len, done,
                       position=position[0], ws=self._ws)
         return A.Batch(self.table, self.length, self.first, tokens=rows, max_new=most, max_len=self.max_len), position

@@ -106,7 +106,6 @@ def test_a_decoding_step_captured_with_its_tables(A, code):
         warm.step(qkv)
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
-    held.requests._position[places] = torch.zeros(1, places, dtype=torch.int32, device="cuda")
     with torch.cuda.graph(graph):
         held.step(qkv)
     for i in range(40):
@@ -183,3 +182,20 @@ def test_other_streams(A):
         A.attention8_forward(cache, batch, A.Score(0.1), q, out)
     side.synchronize()
     assert (out.float() - 1.0).abs().max() <= 2.0 ** -8
+
+
+def test_steps_of_many_sizes_share_one_room(A):
+    """Positions of steps of fewer rows lie where those of the longest lie; what a longer step outgrew stays as a captured one knows it."""
+    import torch
+    from paper_2605_00422_amd.attention_block import Requests
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    r, length = Requests(3, 400, 90, 16), [0, 0, 0]
+    seen = {}
+    for new in ([1, 1, 1], [2, 0, 9], [60, 1, 30], [1, 1, 1], [5, 70, 0]):
+        _, position = r.step(i32(new), rows=sum(new), most=max(new))
+        assert position.shape == (1, sum(new))
+        want = [n + i for n, m in zip(length, new) for i in range(m)]
+        assert position[0].tolist() == want
+        length = [n + m for n, m in zip(length, new)]
+        seen.setdefault(position.data_ptr(), []).append(sum(new))
+    assert list(seen.values()) == [[3], [11], [91, 3, 75]] and len(r._room) == 3
