@@ -615,7 +615,8 @@ typedef struct bwla_kv_cache8 {
  *   scale = A / top, at least 2^-126 (0 where A is 0);  else the scale stays where A <= top * scale (a product of fp32), or is doubled until that holds, and the codes c of
  *   the tokens in front, after n doublings, become c / 2^n;  codes: value / scale.  All to the nearest code, ties to even.
  * A value is then off by half a step of its scale at most when it is written, and by one step of the last scale whatever follows (i8;
- * e4m3 codes halve exactly down to 2^-6).  Values that are not finite do not move a scale: infinities become the largest code, NaN 0.
+ * e4m3 codes halve exactly down to 2^-6).  Values that are not finite do not move a scale: infinities become the largest code
+ * (0 where the scale is 0), NaN 0.
  */
 BWLA_API bwla_status_t bwla_norm_rope_append8(const bwla_kv_cache8_t* cache, const bwla_kv_batch_t* batch, const bwla_rope_t* rope,
                                      const bwla_head_norm_t* norm, const int32_t* d_position, const void* d_qkv, int x_dtype,
@@ -631,8 +632,9 @@ BWLA_API bwla_status_t bwla_cache8_read(const bwla_kv_cache8_t* cache, const bwl
 
 /*
  * bwla_attention_forward over such a cache: the same scores, masks, outputs and scratch rules (without the sums of weights).  Codes enter
- * the products exactly (as fp16, on its matrix instructions), queries as fp16 terms of 11 (bf16) or 22 bits (fp32) relative to the
- * largest of the row or of 32 rows, weights as terms of 11 or 22 bits; all sums are fp32.  Codes and scales of what is not seen may be anything.
+ * the products exactly (as fp16, on its matrix instructions), queries as fp16 terms of 11 (bf16) or 22 bits (fp32), not below 2^-29 of the
+ * largest element of their row; weights as terms of 11 or 22 bits, not below 2^-36 of a weight of 1 at the largest scale of values that the
+ * 16 or 32 rows computed together see.  All sums are fp32.  Codes and scales of what is not seen may be anything.
  */
 BWLA_API bwla_status_t bwla_attention8_workspace_size(const bwla_kv_cache8_t* cache, const bwla_kv_batch_t* batch, int32_t q_heads,
                                              size_t* bytes);

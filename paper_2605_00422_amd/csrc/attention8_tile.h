@@ -6,9 +6,18 @@
 // Codes are fp16 numbers exactly: a block's are fetched to registers while the block before is in work, become fp16 there, once for the
 // workgroup, and go to LDS, from where the products on 32x32 fp16 MFMA read them as they read bf16 ones elsewhere.  The pages' scales
 // stay outside the products: eight keys side by side lie in one page, so that a block has eight scales of each kind, scalars, which
-// multiply scores (as they become weights, where there is no cap or bias) and weights (32 a lane).  Queries are brought to [2^14, 2^15) by one power of two for the wavefront's 32 rows, in one
-// term for bf16 and two for fp32; what is less than 2^-39 of the largest element of these rows is lost.  The maximum m moves where it is
-// off by 2^4, so that weights times vs / S stay below 2^4 and enter the second product times 2^11, in one term of 11 bits or two.
+// multiply scores (as they become weights, where there is no cap or bias) and weights (32 a lane).  Queries are brought to [2^14, 2^15)
+// by one power of two for the wavefront's 32 rows, or one each where they lie apart, in one term for bf16 and two for fp32: what is less
+// than 2^-29 of a row's largest element is lost.  The maximum m moves where it is off by 2^4, so that weights times vs / S stay below
+// 2^4 and enter the second product times 2^11, in one term of 11 bits or two.
+//
+// Bound by vector instructions: a wavefront's block takes about 460 of them, 32 exponentials among them, beside 32 (128 columns) MFMA of 32
+// cycles, with two wavefronts a SIMD (an early form: MFMA 26 % of SIMD cycles, vector instructions 54 %, waits of some 4 cycles each 27 %).  A prompt
+// of 4096, 32 query heads of 128 columns, i8: 200 us, 687 TFLOP/s of the 1229 that a large fp16 product reaches; chunks of 333 behind up
+// to 7001 284 us; 1000 fp32 rows of documents 37 us, of which 17 are the start and a document's six blocks the rest.
+// Scales in the exponent and an instance for each code: 214 -> 199 us; one power of two for all rows alike, whatever their size: 198, but a row
+// beside larger ones lost its bits.  Not taken: eight wavefronts that share a block (prompt -3 %, chunks +9 %); conversions spread over the
+// products (spills: 533 us); three or four wavefronts a SIMD (spills).
 #pragma once
 #include "attention_order.h"
 #include "code8.h"
@@ -71,6 +80,8 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
     const bool blind = me.doc < 0;
     Terms<T> qf[CS];
     int q_exponent;                                    // ... of the power of two that was taken out of the rows
+    bool apart;                                        // whether rows have their own: 2^row_exponent times that
+    int row_exponent = 0;
     {
         const char* qp = a.q + (int64_t)(s.row0 + tok) * a.q_bytes + (int64_t)head * a.d * ES;
         v4u raw[CS][ES / 2];
@@ -91,17 +102,23 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
                 most = fmaxf(most, v <= 3.402823466e38f ? v : 0.f);    // (what is not finite makes its row's scores so)
             }
         }
-        most = bwla_wave_max(most);
-        const int up = max((int)((__float_as_uint(most) >> 23) & 255) - 127, -100);
+        // One power of two where the rows' largest elements lie within 2^10 of one another (or are 0): it goes into the keys' scales.  Else one a
+        // row, so that none of them loses bits to another's size; what they have beyond 2^-60 of the largest one's multiplies the products.
+        most = half_max(most);
+        const auto exponent = [](float v) { return max((int)((__float_as_uint(v) >> 23) & 255) - 127, -100); };
+        const int all = __builtin_amdgcn_readfirstlane(exponent(bwla_wave_max(most)));
+        int up = most > 0.f ? exponent(most) : all;
+        apart = some(up < all - 10);
+        if (apart) row_exponent = up - (all - 60);
+        else up = all;
 #pragma unroll
-        for (int c = 0; c < CS; ++c)
-        {
+        for (int c = 0; c < CS; ++c) {
             float v[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = ldexpf(value(c, e), 14 - up);
             qf[c] = terms_of<T>(v);
         }
-        q_exponent = up - 14;
+        q_exponent = (apart ? all - 60 : all) - 14;
     }
     // indexes of the first and last row of this wavefront, and of the workgroup
     const int old = s.old;
@@ -316,9 +333,18 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
     auto hold = [&](Packed& p) {
         if constexpr (T == 1) asm volatile("" : "+v"(p.w[0].t[0]), "+v"(p.w[1].t[0]), "+v"(l));
     };
+    // Scores of 2^20 and more, of which m, a rounded one, would be off by whole numbers: from there on products are rounded before m is
+    // taken off, so that the largest has a weight of 1 whatever its size.
+    bool huge = false;
+    auto round_now = [&](v16f& sc, int k) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[r] *= kg[4 * k + r / 4];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) kg[4 * k + g] = 1.f;
+    };
     // The maximum moves only when it is off by 2^4; what was summed with the old one follows.
     // (first: what has to be added with the old one before)
-    auto raise = [&](const v16f& sc, int k, auto first) {
+    auto raise = [&](v16f& sc, int k, auto first) {
         float four[4];
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
@@ -337,6 +363,12 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
             for (int d = 0; d < DT; ++d)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[d][r] *= f;
+            if constexpr (!GENERAL) {
+                if (__builtin_expect(!huge && some(fabsf(m) >= 0x1p20f && m > -INFINITY), 0)) {
+                    huge = true;
+                    round_now(sc, k);
+                }
+            }
         }
     };
 
@@ -396,6 +428,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
         if (even ? some(mine) && (j0 <= w_last || j0 < s.prefix) : any != 0) {
             // every row sees every key
             const bool whole = even && !some(!(mine | blind)) && (j0 + BK - 1 <= w_first || j0 + BK <= s.prefix);
+            const bool plainly = whole && (GENERAL || !apart);
             // scales of pages of which no row sees a key may be anything, and count as 0
             {
                 const bool in_use = even || ((any >> (lane & 56)) & 0xff) != 0;
@@ -431,7 +464,12 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
             // a tile's scores made ready: scales, cap, bias, mask, and a maximum that will do for them
             auto ready = [&](v16f& sc, int k, auto first) {
                 arrive(sc);
+                const auto scaled = [&] {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) sc[r] = ldexpf(sc[r], row_exponent);
+                };
                 if constexpr (GENERAL) {
+                    if (__builtin_expect(apart, 0)) scaled();
 #pragma unroll
                     for (int r = 0; r < 16; ++r) sc[r] *= kg[4 * k + r / 4];
                     if (a.capped != 0.f) {
@@ -452,7 +490,9 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
                         for (int r = 0; r < 16; ++r) sc[r] = fmaf(-slope, fabsf(away - (float)((r & 3) + 8 * (r >> 2))), sc[r]);
                     }
                 }
-                if (!__builtin_expect(whole, 1)) {
+                if (!__builtin_expect(plainly && !huge, 1)) {
+                    if (!GENERAL && apart) scaled();
+                    if (!GENERAL && huge) round_now(sc, k);
                     if (even) {
                         const int most = (mine ? max(me.i, s.prefix - 1) : -1) - j0 - k * 32 - 4 * hf;
 #pragma unroll
