@@ -5,8 +5,11 @@
 // each request's share lies, so that everything else is independent: no atomics, and the same answer for the same arguments.
 // Integer work of a few bytes an entry, bound by launches and chains of loads.  Two kernels: requests' shares, added up over groups of 64 (a
 // wavefront each, which also counts the pages that are given back); then, for each group, the sums in front of it, its entries of table
-// and ring, and its rows, dealt out over as many workgroups as there are rows for.  (One workgroup for all sums in between, and rows by
-// bisection of all offsets: 21.9 us for 4096 requests with 10^5 rows.)  Few requests and rows: all of it by one workgroup, in one launch.
+// and ring, and its rows, dealt out over as many workgroups as there are rows for: 4096 requests of a token each 7.0 us, of 24 8.0 us; a fortieth
+// of them done and prompts in their place, 2 x 10^5 rows, 13.9 us.  (One workgroup for all sums in between, and rows by
+// bisection of all offsets: 21.9 us for 4096 requests with 10^5 rows.)  Few requests and rows: all of it by one workgroup, in one launch, 3.6
+// us for 64 requests of a token each and 3.8 for 256 (two launches: 6.2 and 6.8); with 1024 rows 6.0 to 7.1 either way, with 4096 18.3
+// where two take 7.6.
 #include <algorithm>
 
 #include "attention.h"
@@ -311,9 +314,10 @@ hipError_t bwla_launch_build(const BuildArgs& a, void* ws, hipStream_t st) {
     build_sums_kernel<<<(groups + 3) / 4, 256, 0, st>>>(a, f);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    // workgroups for 512 rows each, and not more of them than a few for each compute unit
-    const int64_t rows = a.position || a.slot || a.sequence ? a.tokens / 512 / groups + 1 : 1;
-    const int parts = (int)std::min<int64_t>(rows, std::max(1, 2048 / groups));
+    // A row a thread, up to two workgroups for each compute unit.  (64 requests of 64 rows, 512 and 2048 rows a workgroup: 6.9, 7.7 and 10.1
+    // us.  One workgroup a compute unit at most, and two: 1024 of 100 rows 11.6 and 12.3, 2 x 10^5 rows of uneven requests 15.9 and 13.9.)
+    const int64_t rows = a.position || a.slot || a.sequence ? a.tokens / 256 / groups + 1 : 1;
+    const int parts = (int)std::min<int64_t>(rows, std::max(1, 512 / groups));
     build_apply_kernel<<<groups * parts, 256, 0, st>>>(a, f, groups, parts);
     return hipGetLastError();
 }
