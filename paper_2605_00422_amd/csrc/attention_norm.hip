@@ -348,7 +348,7 @@ __global__ __launch_bounds__(1024) void norm_rope8_kernel(NormArgs n, Items it, 
     if (end <= 0 || e << a.page_shift >= end) return;
     const int from = max(max(start, 0), (int)e << a.page_shift), to = (int)min((int64_t)end, (e + 1) << a.page_shift);
     const int page = a.table[(int64_t)b * a.table_stride + e];
-    if ((unsigned)page >= (unsigned)a.pages) return;
+    if (to <= from || (unsigned)page >= (unsigned)a.pages) return;
     const int inside = from & (size - 1);              // older tokens of the page
     char* const base = (kind == 1 ? a.k : a.v) + page * a.page_stride + head * a.head_stride;
     float* const scale_at = (kind == 1 ? n.k_scale : n.v_scale) + page * n.scale_stride + head;

@@ -331,6 +331,22 @@ def test_pages_of_zeros_and_infinities_have_codes_of_zero(A, code):
 
 
 @pytest.mark.parametrize("code", CODES)
+def test_sequences_without_new_tokens_stay_as_they_were(A, code):
+    import torch
+    c = Call(A, lens=(20, 37, 5), news=(2, 0, 0), seed=21)
+    cache = make8(c, code)
+    for p in c.table_np[1:].ravel():
+        cache.k_scale[int(p)] = -3.0                   # (no scale; a call that has nothing to write there leaves it)
+        cache.v_scale[int(p)] = float("nan")
+    before = [t.view(torch.uint8).clone() for t in (cache.k, cache.v)] + [cache.k_scale.view(torch.int32).clone(), cache.v_scale.view(torch.int32).clone()]
+    c.append(cache)
+    after = [t.view(torch.uint8) for t in (cache.k, cache.v)] + [cache.k_scale.view(torch.int32), cache.v_scale.view(torch.int32)]
+    for x, y in zip(before, after):
+        for p in c.table_np[1:].ravel():
+            assert torch.equal(x[int(p)], y[int(p)])
+
+
+@pytest.mark.parametrize("code", CODES)
 def test_rows_and_pages_that_are_left_out(A, code):
     """Rows of no sequence, more new tokens than max_new, new tokens in front of the cache, pages that do not exist: nothing is written."""
     import torch
