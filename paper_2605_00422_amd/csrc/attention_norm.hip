@@ -10,10 +10,9 @@
 // read and computed twice); the largest magnitude goes through LDS, and older codes of the page follow where its scale grew.
 //
 // Bound by memory, or, with few rows, by the launch and a chain of loads (row, table, angles; in 8 bits the page's scale too).  A prompt of 4096
-// rows, 32 query heads and 8 key-value heads of 128, fp32 in, bf16 queries and e4m3 codes out: 36 us, 4.0 TB/s; as it is,
-// 1001 rows in three chunks, 17.5 us; sixteen rows 4.0 us, 64 into codes 10.6 with their values read back (5).  A page's tokens by a
-// workgroup that reads them once, in up to 1024 threads, not by 256 that read most of them twice: 70.8 -> 42.8 us of that prompt with its
-// reading back, 512 threads the same, 256 44.1.
+// rows, 32 query heads and 8 key-value heads of 128, fp32 in, bf16 queries and e4m3 codes out: 32 us, 4.5 TB/s; as it is, 1001 rows in three chunks,
+// 17.5 us; sixteen rows 4.0 us, 64 into codes 10.8 with their values read back (5).  A page's tokens by a workgroup that reads them once, in up to
+// 1024 threads: with 256, which read most of them twice, that prompt with its reading back takes 51.1 us instead of 44.9 (other inputs each time).
 #include <algorithm>
 
 #include "code8.h"
@@ -293,8 +292,10 @@ __device__ __forceinline__ void put_codes(uint8_t* dst, const float* x, float sc
 // The first query_blocks workgroups write queries, of `rows` rows each or of a part of one's heads; of the others each has a page's new
 // tokens, of one key-value head's keys or values.
 // Page number u of the call: those that sequence b touches begin at first[b] / page + 2 b, which leaves room for each one's.
-template <int VEC, bool XBF, bool BF, bool I8>
-__global__ __launch_bounds__(1024) void norm_rope8_kernel(NormArgs n, Items it, int64_t query_blocks, int rows) {
+// ONCE: no page has more new tokens than a workgroup has groups.  (Without the loops over the others' tokens 61 registers
+// instead of 101, and twice the wavefronts: 49.8 -> 44.9 us of the prompt named at the top.)
+template <int VEC, bool XBF, bool BF, bool I8, bool ONCE>
+__global__ __launch_bounds__(1024, (ONCE ? 8 : 4)) void norm_rope8_kernel(NormArgs n, Items it, int64_t query_blocks, int rows) {
     constexpr int IT = items_a_lane<VEC>();
     __shared__ float words[16];
     const RopeArgs& a = n.r;
@@ -368,10 +369,12 @@ __global__ __launch_bounds__(1024) void norm_rope8_kernel(NormArgs n, Items it, 
     const float was = inside > 0 ? *scale_at : 0.f;
     values(group, x);
     watch(x);
-    for (int t = groups; t < count; t += groups) {
-        float y[IT][2 * VEC];
-        values(t + group, y);
-        watch(y);
+    if constexpr (!ONCE) {
+        for (int t = groups; t < count; t += groups) {
+            float y[IT][2 * VEC];
+            values(t + group, y);
+            watch(y);
+        }
     }
     most = block_max(most, words);                     // (everyone has read the scale in front of it)
     constexpr float top = code_top<I8>();
@@ -418,10 +421,12 @@ __global__ __launch_bounds__(1024) void norm_rope8_kernel(NormArgs n, Items it, 
         }
     };
     put(group, x);
-    for (int t = groups; t < count; t += groups) {
-        float y[IT][2 * VEC];
-        values(t + group, y);
-        put(t + group, y);
+    if constexpr (!ONCE) {
+        for (int t = groups; t < count; t += groups) {
+            float y[IT][2 * VEC];
+            values(t + group, y);
+            put(t + group, y);
+        }
     }
 }
 
@@ -469,7 +474,7 @@ Items items_of(const RopeArgs& a) {
     return it;
 }
 // Eight pairs a thread where they come in eights (heads and rows are 16-byte aligned), else four, else one.  (Four instead of eight: that prompt
-// 42.8 -> 59.4 us, the chunks 17.5 -> 18.9, 64 rows into codes 10.6 -> 10.0.)
+// 44.9 -> 55.5 us, the chunks 18.3 -> 19.6, 64 rows into codes 10.8 -> 10.6.)
 template <typename F>
 hipError_t by_pairs(const RopeArgs& a, F go) {
     if ((a.pairs & 7) == 0) return go(std::integral_constant<int, 8>{});
@@ -514,9 +519,11 @@ hipError_t bwla_launch_norm_rope8(const NormArgs& n, int x_dtype, int dtype, int
         if (blocks * threads >= 1ll << 32) return hipErrorInvalidConfiguration;       // (a grid has fewer than 2^32 threads)
         return by_types(x_dtype == BWLA_X_BF16, dtype == BWLA_X_BF16, [&](auto x, auto y) {
             constexpr bool X = decltype(x)::value, Y = decltype(y)::value;
-            if (code == BWLA_CODE_I8) norm_rope8_kernel<V, X, Y, true><<<(unsigned)blocks, threads, 0, st>>>(n, it, queries, rows);
-            else norm_rope8_kernel<V, X, Y, false><<<(unsigned)blocks, threads, 0, st>>>(n, it, queries, rows);
-            return hipGetLastError();
+            auto go = [&](auto i8, auto once) {
+                norm_rope8_kernel<V, X, Y, decltype(i8)::value, decltype(once)::value><<<(unsigned)blocks, threads, 0, st>>>(n, it, queries, rows);
+                return hipGetLastError();
+            };
+            return by_types(code == BWLA_CODE_I8, std::min(a.max_new, 1 << a.page_shift) <= groups, go);
         });
     });
 }
