@@ -14,7 +14,7 @@
 // Bound by vector instructions: a wavefront's block takes about 460 of them, 32 exponentials among them, beside 32 (128 columns) MFMA of 32
 // cycles, with two wavefronts a SIMD (an early form: MFMA 26 % of SIMD cycles, vector instructions 54 %, waits of some 4 cycles each 27 %).  A prompt
 // of 4096, 32 query heads of 128 columns, i8: 200 us, 687 TFLOP/s of the 1229 that a large fp16 product reaches; chunks of 333 behind up
-// to 7001 284 us; 1000 fp32 rows of documents 37 us, of which 17 are the start and a document's six blocks the rest.
+// to 7001, with a bias, 273 us; 1000 fp32 rows of documents 37 us, of which 17 are the start and a document's six blocks the rest.
 // Scales in the exponent and an instance for each code: 214 -> 199 us; one power of two for all rows alike, whatever their size: 198, but a row
 // beside larger ones lost its bits.  Not taken: eight wavefronts that share a block (prompt -3 %, chunks +9 %); conversions spread over the
 // products (spills: 533 us); three or four wavefronts a SIMD (spills).
@@ -428,6 +428,8 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
         if (even ? some(mine) && (j0 <= w_last || j0 < s.prefix) : any != 0) {
             // every row sees every key
             const bool whole = even && !some(!(mine | blind)) && (j0 + BK - 1 <= w_first || j0 + BK <= s.prefix);
+            // a bias alone, and keys no later than rows: no cap, no distance either way
+            [[maybe_unused]] const bool linear = GENERAL && a.capped == 0.f && a.slopes && !s.pos && (j0 >= s.prefix || j0 + BK - 1 <= w_first);
             const bool plainly = whole && (GENERAL || !apart);
             // scales of pages of which no row sees a key may be anything, and count as 0
             {
@@ -470,24 +472,37 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
                 };
                 if constexpr (GENERAL) {
                     if (__builtin_expect(apart, 0)) scaled();
+                    if (linear) {
+                        // A slope times the row's distance to the first of four keys, and 0 to 3 slopes back: an instruction a score less
+                        // than scale, distance and bias one after the other (chunks 284 -> 273 us, that prompt with a bias 269 -> 247).
+                        const float to = -slope * (float)(me.p - j0 - k * 32 - 4 * hf), three = 3.f * slope;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) sc[r] *= kg[4 * k + r / 4];
-                    if (a.capped != 0.f) {
-                        const float c3 = a.c2 * (2.f * ATT_LOG2E);
+                        for (int g = 0; g < 4; ++g) {
+                            const float b = g ? fmaf(8.f * g, slope, to) : to;
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            if constexpr (FORM == ATT_SHORT) sc[r] = fmaf(-2.f * a.capped, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(sc[r] * c3)), a.capped);
-                            else sc[r] = a.capped * att_tanh(sc[r] * a.c2);
+                            for (int e = 0; e < 4; ++e)
+                                sc[4 * g + e] = fmaf(sc[4 * g + e], kg[4 * k + g], e == 0 ? b : e == 1 ? b + slope : e == 2 ? fmaf(2.f, slope, b) : b + three);
                         }
-                    }
-                    if (a.slopes && s.pos) {
+                    } else {
 #pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            sc[r] = fmaf(-slope, fabsf((float)(me.p - __shfl(now.p, k * 32 + (r & 3) + 8 * (r >> 2) + 4 * hf, 64))), sc[r]);
-                    } else if (a.slopes) {
-                        const float away = (float)(me.p - j0 - k * 32 - 4 * hf);
+                        for (int r = 0; r < 16; ++r) sc[r] *= kg[4 * k + r / 4];
+                        if (a.capped != 0.f) {
+                            const float c3 = a.c2 * (2.f * ATT_LOG2E);
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) sc[r] = fmaf(-slope, fabsf(away - (float)((r & 3) + 8 * (r >> 2))), sc[r]);
+                            for (int r = 0; r < 16; ++r) {
+                                if constexpr (FORM == ATT_SHORT) sc[r] = fmaf(-2.f * a.capped, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(sc[r] * c3)), a.capped);
+                                else sc[r] = a.capped * att_tanh(sc[r] * a.c2);
+                            }
+                        }
+                        if (a.slopes && s.pos) {
+#pragma unroll
+                            for (int r = 0; r < 16; ++r)
+                                sc[r] = fmaf(-slope, fabsf((float)(me.p - __shfl(now.p, k * 32 + (r & 3) + 8 * (r >> 2) + 4 * hf, 64))), sc[r]);
+                        } else if (a.slopes) {
+                            const float away = (float)(me.p - j0 - k * 32 - 4 * hf);
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) sc[r] = fmaf(-slope, fabsf(away - (float)((r & 3) + 8 * (r >> 2))), sc[r]);
+                        }
                     }
                 }
                 if (!__builtin_expect(plainly && !huge, 1)) {
