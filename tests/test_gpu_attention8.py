@@ -196,6 +196,14 @@ def test_masks_caps_and_biases(A, code, dtype, lens, news, names):
     check(Case(code, dtype, 64, 6, 2, 16, lens, news, seed=9), A, names)
 
 
+@pytest.mark.parametrize("names", [("slopes",), ("slopes", "prefix"), ("slopes", "window", "runs"), ("slopes", "prefix", "doc"), ("slopes", "position")])
+@pytest.mark.parametrize("code,dtype,page", [("i8", "bf16", 64), ("e4m3", "f32", 16)])
+@pytest.mark.parametrize("lens,news", [([700, 333], [650, 90]), ([500, 64], [2, 1])])
+def test_a_bias_without_a_cap(A, code, dtype, page, lens, news, names):
+    """Keys in front of every row, among the rows and, in prefixes, behind them."""
+    check(Case(code, dtype, 128, 6, 2, page, lens, news, seed=17), A, names)
+
+
 @pytest.mark.parametrize("new", [1, 9, 60])
 @pytest.mark.parametrize("code,dtype", [("i8", "bf16"), ("e4m3", "f32")])
 def test_pages_that_do_not_exist(A, code, dtype, new):
