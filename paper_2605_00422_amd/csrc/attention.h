@@ -206,17 +206,21 @@ __device__ __forceinline__ int att_wave() { return __builtin_amdgcn_readfirstlan
 
 // tanh to one or two units of the last place: below 0.6 an odd polynomial (degree 11, fitted to tanh(x) / x in
 // x^2, relative error 2.5e-9 before rounding), above by the exponential
-__device__ __forceinline__ float att_tanh(float x) {
+constexpr float ATT_NEAR = 0.6f;           // ... up to which the polynomial holds
+__device__ __forceinline__ float att_tanh_near(float x) {
     const float u = x * x;
     float p = -0.00585642786f;
     p = fmaf(p, u, 0.0207574754f);
     p = fmaf(p, u, -0.0537699218f);
     p = fmaf(p, u, 0.133317047f);
     p = fmaf(p, u, -0.33333284f);
-    p = fmaf(p * u, x, x);
+    return fmaf(p * u, x, x);
+}
+__device__ __forceinline__ float att_tanh(float x) {
+    const float p = att_tanh_near(x);
     const float e = __builtin_amdgcn_exp2f(fabsf(x) * (2.f * ATT_LOG2E));
     const float big = copysignf(1.f - 2.f * __builtin_amdgcn_rcpf(1.f + e), x);
-    return fabsf(x) < 0.6f ? p : big;
+    return fabsf(x) < ATT_NEAR ? p : big;
 }
 __device__ __forceinline__ float att_score(const AttArgs& a, float prod) {
     return a.capped != 0.f ? a.capped * att_tanh(prod * a.c2) : prod * a.c1;

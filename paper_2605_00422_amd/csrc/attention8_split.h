@@ -183,7 +183,6 @@ __global__ __launch_bounds__(64 * SP_WAVES, (DP == 256 ? 1 : 2)) void att8_split
         }
     };
     constexpr int STRIDE = SP_WAVES * SP_STEP;
-    [[maybe_unused]] const float c3 = a.c2 * (2.f * ATT_LOG2E);
     if (c0 + wave * SP_STEP < c1) {
         load_keys(c0 + wave * SP_STEP);
         load_values(c0 + wave * SP_STEP);
@@ -194,7 +193,7 @@ __global__ __launch_bounds__(64 * SP_WAVES, (DP == 256 ? 1 : 2)) void att8_split
         // Every row sees every key of the step, as when one token follows a cache without windows and documents: nothing is tested then.  (One
         // body for both: two of them took 189 registers instead of 128.)
         const bool whole = j0 + SP_STEP <= seen_to && att_uniform(__all((page_v[0] >= 0) & (page_v[1] >= 0)));
-        float y[2][4];
+        float y[8];
         uint32_t used[2] = {15u, 15u};         // of a lane's four keys those that any row sees
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -211,24 +210,17 @@ __global__ __launch_bounds__(64 * SP_WAVES, (DP == 256 ? 1 : 2)) void att8_split
                 }
             const float kq = ldexpf(ks_v[t], q_exponent) * (FORM != ATT_PLAIN && a.capped != 0.f ? 1.f : a.c1);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) y[t][r] = acc[r] * kq;
+            for (int r = 0; r < 4; ++r) y[4 * t + r] = acc[r] * kq;
         }
         if constexpr (FORM != ATT_PLAIN) {
-            if (a.capped != 0.f) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    float& v = y[i / 4][i % 4];
-                    if constexpr (FORM == ATT_SHORT) v = fmaf(-2.f * a.capped, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * c3)), a.capped);
-                    else v = a.capped * att_tanh(v * a.c2);
-                }
-            }
+            if (a.capped != 0.f) capped_scores<8>(a, y);
         }
         if (__builtin_expect(whole, 1)) {
             if constexpr (FORM != ATT_PLAIN) {
                 if (a.slopes) {
                     const float away = (float)(me.p - j0 - 4 * g);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) y[i / 4][i % 4] -= slope * fabsf(away - (float)(16 * (i / 4) + i % 4));
+                    for (int i = 0; i < 8; ++i) y[i] -= slope * fabsf(away - (float)(16 * (i / 4) + i % 4));
                 }
             }
         } else {
@@ -241,15 +233,15 @@ __global__ __launch_bounds__(64 * SP_WAVES, (DP == 256 ? 1 : 2)) void att8_split
                 const int kd = page_v[i / 4] >= 0 && j <= last ? (s.doc ? max(s.doc[in], -1) : 0) : -1;
                 const bool seen = att_sees(me, s.prefix, a.window, j, kp, kd);
                 if constexpr (FORM != ATT_PLAIN) {
-                    if (a.slopes) y[i / 4][i % 4] -= slope * fabsf((float)(me.p - kp));
+                    if (a.slopes) y[i] -= slope * fabsf((float)(me.p - kp));
                 }
-                y[i / 4][i % 4] = seen ? y[i / 4][i % 4] : -INFINITY;
+                y[i] = seen ? y[i] : -INFINITY;
                 used[i / 4] |= ((__ballot(seen) >> (16 * g)) & 0xffffull) != 0 ? 1u << (i % 4) : 0u;
             }
         }
         float top = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = fmaxf(top, y[i / 4][i % 4]);
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, y[i]);
         float now_s = fmaxf(used[0] ? vs_v[0] : 0.f, used[1] ? vs_v[1] : 0.f);
         // as the values' scales stand for this step: nothing of what no row sees
         float over[2] = {used[0] ? vs_v[0] : 0.f, used[1] ? vs_v[1] : 0.f};
@@ -278,7 +270,7 @@ __global__ __launch_bounds__(64 * SP_WAVES, (DP == 256 ? 1 : 2)) void att8_split
             over[t] = over[t] * down * 32768.f;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const float e = __builtin_amdgcn_exp2f(y[t][r] - base);
+                const float e = __builtin_amdgcn_exp2f(y[4 * t + r] - base);
                 l += e;
                 w[4 * t + r] = e * over[t];
             }

@@ -39,8 +39,6 @@ struct At8Shape {
 template <int T, int DP>
 constexpr int at8_groups() { return T == 2 || DP == 256 ? 1 : 2; }     // workgroups of a compute unit
 
-// whether any lane has it: a scalar, so that what depends on it is a jump
-__device__ __forceinline__ bool some(bool x) { return __builtin_amdgcn_ballot_w64(x) != 0; }
 // (fmaxf would make each number a quiet one first)
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
@@ -487,11 +485,19 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
 #pragma unroll
                         for (int r = 0; r < 16; ++r) sc[r] *= kg[4 * k + r / 4];
                         if (a.capped != 0.f) {
-                            const float c3 = a.c2 * (2.f * ATT_LOG2E);
+                            // The short form, off by 1.2e-7 of the cap, where every row sees every key, so that little of it is left in their
+                            // sum (a row of two keys has an lse of 2, of which that is 1e-6); a prompt of 4096 with it there and nowhere: 269 and 284 us.
+                            // (256 columns: everywhere, as another body spills: 2048 rows with a bias 200 -> 239 us.)
+                            if constexpr (FORM == ATT_LONG && DP < 256) {
+                                capped_scores<16>(a, sc);
+                            } else if (FORM == ATT_SHORT && (DP == 256 || whole)) {
+                                const float c3 = a.c2 * (2.f * ATT_LOG2E);
 #pragma unroll
-                            for (int r = 0; r < 16; ++r) {
-                                if constexpr (FORM == ATT_SHORT) sc[r] = fmaf(-2.f * a.capped, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(sc[r] * c3)), a.capped);
-                                else sc[r] = a.capped * att_tanh(sc[r] * a.c2);
+                                for (int r = 0; r < 16; ++r)
+                                    sc[r] = fmaf(-2.f * a.capped, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(sc[r] * c3)), a.capped);
+                            } else {
+#pragma unroll
+                                for (int r = 0; r < 16; ++r) sc[r] = a.capped * att_tanh(sc[r] * a.c2);
                             }
                         }
                         if (a.slopes && s.pos) {

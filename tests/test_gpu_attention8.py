@@ -102,6 +102,10 @@ class Case:
         kw, per = {}, {}
         if "cap" in names:
             kw["cap"] = 5.0
+        if "cap of 50" in names:
+            kw["cap"] = 50.0
+        if "window of 2" in names:
+            kw["window"] = 2
         if "high cap" in names:
             kw["cap"] = 200.0
         if "slopes" in names:
@@ -137,8 +141,9 @@ def call(c, A, kw, scale=None, q=None, batch=None):
     return out, lse
 
 
-def check(c, A, names=(), seed=1, own=False):
-    """own: what is lost is relative to each row's own largest element, not to all rows'."""
+def check(c, A, names=(), seed=1, own=False, few=False):
+    """own: what is lost is relative to each row's own largest element, not to all rows'.  few: rows see few keys, of scores below 0.6 of
+    the cap: then tanh is off by 4 u of itself, as scales and products are, and nothing by units of the cap."""
     torch = c.torch
     kw, per = c.options(np.random.default_rng(seed), names)
     scale = c.d ** -0.5
@@ -153,6 +158,9 @@ def check(c, A, names=(), seed=1, own=False):
         out_b, lse_b, _, vabs, qk, top = orc.attend(q, k, v, scale, exists=c.exists[b], **o)
         row += new
         cap = o.get("cap", 0.0)
+        if few:
+            assert cap and np.max(np.where(np.isfinite(top), top, 0)) < 0.5 * cap
+            cap = 0.0
         lost = 2.0 ** -38 * c.d * (np.abs(c.q.double().numpy()).max() if new else 0) * (np.abs(k).max() if n else 0) * scale
         if own:
             lost = 2.0 ** -28 * c.d * np.abs(q).max(-1) * np.abs(k).max() * scale
@@ -202,6 +210,15 @@ def test_masks_caps_and_biases(A, code, dtype, lens, news, names):
 def test_a_bias_without_a_cap(A, code, dtype, page, lens, news, names):
     """Keys in front of every row, among the rows and, in prefixes, behind them."""
     check(Case(code, dtype, 128, 6, 2, page, lens, news, seed=17), A, names)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("lens,news,names", [([5, 2, 1], [1, 1, 1], ("cap of 50",)), ([400, 37], [1, 1], ("cap of 50", "window of 2")),
+                                             ([300, 90], [300, 70], ("cap of 50", "window of 2"))])
+def test_caps_of_rows_that_see_few_keys(A, code, dtype, lens, news, names):
+    """Their scores and lse keep their bits: a cap far above them costs none."""
+    check(Case(code, dtype, 64, 6, 2, 16, lens, news, seed=19, spread=0.2), A, names, few=True)
 
 
 @pytest.mark.parametrize("new", [1, 9, 60])
