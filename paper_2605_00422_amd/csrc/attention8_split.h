@@ -41,7 +41,7 @@ __device__ __forceinline__ float xor32(float v, bool max_of) {
 }
 
 // BF: bf16 queries and outputs (else fp32); I8: integers (else e4m3); DP: columns, 64, 128 or 256; EXACT: d == DP;
-// FORM: AttForm, scale, cap and bias
+// FORM: ATT_PLAIN, nothing but the scale, or ATT_LONG, a cap or a bias
 template <bool BF, bool I8, int DP, bool EXACT, int FORM>
 __global__ __launch_bounds__(64 * SP_WAVES, (DP == 256 ? 1 : 2)) void att8_split_kernel(AttArgs a, Att8 sc, AttSplit sp, float* __restrict__ part,
                                                                   float4* __restrict__ stat) {
@@ -376,11 +376,7 @@ hipError_t launch8(const AttArgs& a, const Att8& e, const AttSplit& s, void* ws,
         return a.d == DP ? go(att8_split_kernel<BF, I8, DP, true, FORM>) : go(att8_split_kernel<BF, I8, DP, false, FORM>);
     };
     auto codes = [&](auto form) { return e.code == BWLA_CODE_I8 ? columns(std::true_type{}, form) : columns(std::false_type{}, form); };
-    const AttForm form = att_form(a, BF);
-    hipError_t r;
-    if (form == ATT_PLAIN) r = codes(std::integral_constant<int, ATT_PLAIN>{});
-    else if (form == ATT_LONG) r = codes(std::integral_constant<int, ATT_LONG>{});
-    else r = codes(std::integral_constant<int, BF ? ATT_SHORT : ATT_LONG>{});
+    const hipError_t r = att_form(a, BF) == ATT_PLAIN ? codes(std::integral_constant<int, ATT_PLAIN>{}) : codes(std::integral_constant<int, ATT_LONG>{});
     if (r != hipSuccess || s.splits == 1) return r;
     return bwla_launch_attention_join(a, s, BF ? BWLA_X_BF16 : BWLA_X_F32, ws, st);
 }
