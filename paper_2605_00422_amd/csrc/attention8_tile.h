@@ -274,6 +274,12 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
     // branch that may be skipped lies between (it counts the longer way): weights were taken relative to a maximum of numbers that were
     // not there yet.
     auto arrive = [&](v16f& sc) { asm volatile("s_nop 11" : "+v"(sc)); };
+    // ... and the same of the sums, where they are scaled right behind a product: what decided how long that was is a branch as well.
+    auto arrived = [&] {
+        if constexpr (DT == 2) asm volatile("s_nop 11" : "+v"(o[0]), "+v"(o[1]));
+        else if constexpr (DT == 4) asm volatile("s_nop 11" : "+v"(o[0]), "+v"(o[1]), "+v"(o[2]), "+v"(o[3]));
+        else asm volatile("s_nop 11" : "+v"(o[0]), "+v"(o[1]), "+v"(o[2]), "+v"(o[3]), "+v"(o[4]), "+v"(o[5]), "+v"(o[6]), "+v"(o[7]));
+    };
     // Weights of a tile's scores as they enter the second product, w F vs / S (F = 2^11), and the sums of w alone.  (Without cap and bias scores
     // stay products until here: y - m is rounded once.)  One term: the factor is part of the exponent, and goes out of the sum for four keys
     // at once, which takes an instruction less a score and costs 2^-20 of a weight.  Two terms: the weight, then the product.
@@ -550,6 +556,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
             __builtin_amdgcn_s_setprio(0);
             ready(s1, 1, [&] {
                 values(fetch(vb, 0), p0);
+                arrived();
                 const v8h zero = {};
 #pragma unroll
                 for (int u = 0; u < 2; ++u)

@@ -55,6 +55,29 @@ def blocks_of(body):
     return blocks, follow
 
 
+def blocks_at_branches(body):
+    """The same with blocks that end at branches, too: what follows a branch that may be skipped has no label of its own."""
+    blocks, at = {"": []}, ""
+    for l in body:
+        m = re.match(r"^(\.LBB\S+):", l)
+        s = "" if m else l.split(";")[0].strip()
+        if m:
+            at = m.group(1)
+            blocks[at] = []
+        elif s and not s.startswith("."):
+            blocks[at].append(s)
+            if s.startswith(("s_cbranch", "s_branch", "s_endpgm")):
+                at = f"behind {len(blocks)}"
+                blocks[at] = []
+    names, follow = list(blocks), {}
+    for i, b in enumerate(names):
+        last = blocks[b][-1] if blocks[b] else ""
+        follow[b] = [last.split()[-1]] if last.startswith(("s_cbranch", "s_branch")) else []
+        if not last.startswith(("s_branch", "s_endpgm")) and i + 1 < len(names):
+            follow[b].append(names[i + 1])
+    return blocks, follow
+
+
 NO_RESULT = ("ds_write", "global_store", "scratch_store", "buffer_store", "v_cmp", "v_readlane", "v_readfirstlane")
 READ_TOO = ("v_fmac", "v_permlane", "v_mac", "v_dot", "v_writelane")               # ... what they write
 
@@ -76,8 +99,8 @@ def walk(instructions, missing, early=None):
     return missing
 
 
-def early_reads(body):
-    blocks, follow = blocks_of(body)
+def early_reads(body, split=blocks_of):
+    blocks, follow = split(body)
     state, todo, reached = {b: {} for b in blocks}, [""], {""}
     while todo:
         b = todo.pop()

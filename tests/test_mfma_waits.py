@@ -1,0 +1,34 @@
+"""Results of matrix instructions are waited for on every way through the kernels, with ways told apart at each branch (no GPU needed)."""
+import os
+import subprocess
+
+import pytest
+
+import mfma_waits
+from paper_2605_00422_amd import build
+
+FILES = ["attention8_tile.hip", "attention8_tile_e4m3.hip", "attention8_tile_f32.hip", "attention8_tile_f32_e4m3.hip"]
+
+
+def test_what_a_branch_skips_does_not_count_as_waiting():
+    """With a label in front of it or without: a block that is entered from above alone has none."""
+    ahead = ["v_mfma_f32_32x32x16_f16 v[0:15], v[16:19], v[20:23], 0", "s_cbranch_scc0 .LBB0_2"]
+    long, read = ["v_add_f32_e32 v30, v31, v31"] * 20, [".LBB0_2:", "v_max_f32_e32 v30, v3, v3", "s_endpgm"]
+    for label in (".LBB0_1:", "; %bb.1:"):
+        assert mfma_waits.early_reads(ahead + [label] + long + read, mfma_waits.blocks_at_branches)
+        assert not mfma_waits.early_reads(ahead[:1] + ["s_nop 11"] + ahead[1:] + [label] + long + read, mfma_waits.blocks_at_branches)
+
+
+@pytest.mark.parametrize("name", FILES)
+def test_results_of_matrix_instructions_are_waited_for(tmp_path, name):
+    if not os.path.exists(build.HIPCC):
+        pytest.skip("hipcc not available")
+    out = str(tmp_path / "kernels.s")
+    subprocess.run([build.HIPCC, *build.FLAGS, *build.FILE_FLAGS.get(name, []), "-w", "-S", "--cuda-device-only", "-o", out,
+                    os.path.join(build.CSRC, name)], check=True, stderr=subprocess.DEVNULL)
+    found = 0
+    for kernel, body in mfma_waits.kernels(open(out).read().split("\n")):
+        found += 1
+        early = mfma_waits.early_reads(body, mfma_waits.blocks_at_branches)
+        assert not early, (kernel, early[:3])
+    assert found
