@@ -354,6 +354,8 @@ __global__ __launch_bounds__(64 * AT_WAVES, DP == 256 ? 1 : 2) void att_tile_ker
                 // (The compiler counts what has to be issued behind the last product by the way through the mask: where no mask is needed the
                 // maximum was taken of four numbers that were still to come.)
                 if constexpr (!BF) asm volatile("s_nop 15\n\ts_nop 1" : "+v"(sc));
+                // (bf16 with a cap or a bias: a register of the result was written to one state before the result was in it.)
+                else if constexpr (GENERAL) asm volatile("s_nop 11" : "+v"(sc));
                 if constexpr (GENERAL) att_transform<FORM>(a, sc, me.p, slope, j0, k, now.p, s.pos != nullptr);
                 bool fine = false;
                 if (__builtin_expect(whole, 1)) {

@@ -7,7 +7,8 @@ import pytest
 import mfma_waits
 from paper_2605_00422_amd import build
 
-FILES = ["attention8_tile.hip", "attention8_tile_e4m3.hip", "attention8_tile_f32.hip", "attention8_tile_f32_e4m3.hip"]
+FILES = ["attention8_tile.hip", "attention8_tile_e4m3.hip", "attention8_tile_f32.hip", "attention8_tile_f32_e4m3.hip",
+         "attention_tile.hip"]
 
 
 def test_what_a_branch_skips_does_not_count_as_waiting():
