@@ -393,6 +393,9 @@ __device__ __forceinline__ void rotate3_token(char* lds, const uint16_t* __restr
                 }
             }
             if (!sh.resident) __syncthreads();                         // chunk ch + 1 is published, chunk ch is free
+            // (Eight others have to be issued behind a product before its sum is read.  The compiler counts them by the way through the
+            // barrier alone: a token's second and later steps moved sums that had two states to go.)
+            else if constexpr (LOOP) asm volatile("s_nop 7");
         }
     }
 

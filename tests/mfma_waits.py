@@ -82,29 +82,33 @@ NO_RESULT = ("ds_write", "global_store", "scratch_store", "buffer_store", "v_cmp
 READ_TOO = ("v_fmac", "v_permlane", "v_mac", "v_dot", "v_writelane")               # ... what they write
 
 
-def walk(instructions, missing, early=None):
-    """What is missing behind these instructions; early: gets those that read or overwrite a result too soon."""
-    missing = dict(missing)
+def walk(instructions, missing, early=None, busy=False):
+    """What is missing behind these instructions; early: gets those that read or overwrite a result too soon.  busy: a matrix instruction
+    keeps its unit for its passes, so that the next one issues as many states later (the compiler counts one)."""
+    missing, free = dict(missing), 0
     for s in instructions:
         op, rest = s.split()[0], s[len(s.split()[0]):]
         matrix = op.startswith(("v_mfma", "v_smfmac"))
+        if matrix and busy:
+            missing, free = {r: k - free for r, k in missing.items() if k > free}, 0
         if early is not None and not matrix and op.startswith(("v_", "ds_", "global_", "buffer_", "scratch_", "flat_")):
             early += [(s, r, missing[r]) for r in set(registers(rest)) if missing.get(r, 0) > 0]
         step = int(rest.strip(), 0) + 1 if op == "s_nop" else 1
-        missing = {r: k - step for r, k in missing.items() if k > step}
+        missing, free = {r: k - step for r, k in missing.items() if k > step}, max(free - step, 0)
         if matrix:
             need = [n for shape, n in NEED if shape in op]
             assert need, f"unknown shape: {op}"
             missing.update((r, need[0]) for r in registers(rest.split(",")[0]))
+            free = need[0] - (2 if op.endswith("_f32") else 4) - 1
     return missing
 
 
-def early_reads(body, split=blocks_of):
+def early_reads(body, split=blocks_of, busy=False):
     blocks, follow = split(body)
     state, todo, reached = {b: {} for b in blocks}, [""], {""}
     while todo:
         b = todo.pop()
-        out = walk(blocks[b], state[b])
+        out = walk(blocks[b], state[b], busy=busy)
         for to in follow[b]:
             worse = {r: k for r, k in out.items() if state[to].get(r, 0) < k}
             if worse or to not in reached:
@@ -113,5 +117,5 @@ def early_reads(body, split=blocks_of):
                 todo.append(to)
     early = []
     for b in blocks:
-        walk(blocks[b], state[b], early)
+        walk(blocks[b], state[b], early, busy)
     return early

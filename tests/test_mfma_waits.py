@@ -9,6 +9,8 @@ from paper_2605_00422_amd import build
 
 FILES = ["attention8_tile.hip", "attention8_tile_e4m3.hip", "attention8_tile_f32.hip", "attention8_tile_f32_e4m3.hip",
          "attention_tile.hip"]
+# ... where what lies between product and reading may be another product, which waits for the unit
+BUSY = ["rotate_quant.hip"]
 
 
 def test_what_a_branch_skips_does_not_count_as_waiting():
@@ -20,7 +22,15 @@ def test_what_a_branch_skips_does_not_count_as_waiting():
         assert not mfma_waits.early_reads(ahead[:1] + ["s_nop 11"] + ahead[1:] + [label] + long + read, mfma_waits.blocks_at_branches)
 
 
-@pytest.mark.parametrize("name", FILES)
+def test_a_product_in_between_waits_for_the_unit():
+    two = ["v_mfma_f32_16x16x32_f16 v[0:3], v[16:19], v[20:23], 0", "v_mfma_f32_16x16x32_f16 v[4:7], v[16:19], v[20:23], 0"]
+    read = ["v_max_f32_e32 v30, v3, v3", "s_endpgm"]
+    for n, early in ((3, False), (2, True)):           # 8 states: 4 passes, n + 1 others
+        assert bool(mfma_waits.early_reads(two + [f"s_nop {n}"] + read, busy=True)) == early
+    assert mfma_waits.early_reads(two + ["s_nop 3"] + read) and not mfma_waits.early_reads(two + ["s_nop 6"] + read)
+
+
+@pytest.mark.parametrize("name", FILES + BUSY)
 def test_results_of_matrix_instructions_are_waited_for(tmp_path, name):
     if not os.path.exists(build.HIPCC):
         pytest.skip("hipcc not available")
@@ -30,6 +40,6 @@ def test_results_of_matrix_instructions_are_waited_for(tmp_path, name):
     found = 0
     for kernel, body in mfma_waits.kernels(open(out).read().split("\n")):
         found += 1
-        early = mfma_waits.early_reads(body, mfma_waits.blocks_at_branches)
+        early = mfma_waits.early_reads(body, mfma_waits.blocks_at_branches, name in BUSY)
         assert not early, (kernel, early[:3])
     assert found
