@@ -342,6 +342,8 @@ __global__ __launch_bounds__(THREADS) void rotate_terms_kernel(RtArgs b) {
                 rb = r1 + (g & 1) * chunk_bytes + lane * 16;
             } else {
                 if (j == 0 && ch == 0) bwla_lds_barrier();                       // the R1 terms are there
+                // (Eight others have to be issued behind a product before its result is read; the compiler counts the barrier's, too.)
+                else asm volatile("s_nop 7");
                 rb = r1 + ch * chunk_bytes + lane * 16;
             }
             auto ld_b = [&](int tc) {

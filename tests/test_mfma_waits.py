@@ -10,7 +10,7 @@ from paper_2605_00422_amd import build
 FILES = ["attention8_tile.hip", "attention8_tile_e4m3.hip", "attention8_tile_f32.hip", "attention8_tile_f32_e4m3.hip",
          "attention_tile.hip"]
 # ... where what lies between product and reading may be another product, which waits for the unit
-BUSY = ["rotate_quant.hip"]
+BUSY = ["rotate_quant.hip", "rotate_terms.hip", "rotate_terms_many.hip", "rotate_terms_f32.hip"]
 
 
 def test_what_a_branch_skips_does_not_count_as_waiting():
