@@ -36,27 +36,8 @@ def kernels(lines):
 
 
 def blocks_of(body):
-    """Blocks of instructions by label, and the labels that follow each."""
-    blocks, at = {"": []}, ""
-    for l in body:
-        m = re.match(r"^(\.LBB\S+):", l)
-        if m:
-            at = m.group(1)
-            blocks[at] = []
-            continue
-        s = l.split(";")[0].strip()
-        if s and not s.startswith("."):
-            blocks[at].append(s)
-    names, follow = list(blocks), {}
-    for i, b in enumerate(names):
-        to = [s.split()[-1] for s in blocks[b] if s.startswith(("s_cbranch", "s_branch"))]
-        ends = any(s.startswith(("s_branch", "s_endpgm")) for s in blocks[b])
-        follow[b] = to + ([] if ends or i + 1 == len(names) else [names[i + 1]])
-    return blocks, follow
-
-
-def blocks_at_branches(body):
-    """The same with blocks that end at branches, too: what follows a branch that may be skipped has no label of its own."""
+    """Blocks of instructions, which end at labels and at branches (what follows a branch that may be skipped has no label of its own),
+    and the names of those that follow each."""
     blocks, at = {"": []}, ""
     for l in body:
         m = re.match(r"^(\.LBB\S+):", l)
@@ -78,10 +59,6 @@ def blocks_at_branches(body):
     return blocks, follow
 
 
-NO_RESULT = ("ds_write", "global_store", "scratch_store", "buffer_store", "v_cmp", "v_readlane", "v_readfirstlane")
-READ_TOO = ("v_fmac", "v_permlane", "v_mac", "v_dot", "v_writelane")               # ... what they write
-
-
 def walk(instructions, missing, early=None, busy=False):
     """What is missing behind these instructions; early: gets those that read or overwrite a result too soon.  busy: a matrix instruction
     keeps its unit for its passes, so that the next one issues as many states later (the compiler counts one)."""
@@ -91,8 +68,10 @@ def walk(instructions, missing, early=None, busy=False):
         matrix = op.startswith(("v_mfma", "v_smfmac"))
         if matrix and busy:
             missing, free = {r: k - free for r, k in missing.items() if k > free}, 0
-        if early is not None and not matrix and op.startswith(("v_", "ds_", "global_", "buffer_", "scratch_", "flat_")):
-            early += [(s, r, missing[r]) for r in set(registers(rest)) if missing.get(r, 0) > 0]
+        if early is not None and op.startswith(("v_", "ds_", "global_", "buffer_", "scratch_", "flat_")):
+            # (a sum that goes on in the next product is the hardware's to order)
+            text = ",".join(rest.split(",")[1:3]) if matrix else rest
+            early += [(s, r, missing[r]) for r in set(registers(text)) if missing.get(r, 0) > 0]
         step = int(rest.strip(), 0) + 1 if op == "s_nop" else 1
         missing, free = {r: k - step for r, k in missing.items() if k > step}, max(free - step, 0)
         if matrix:
@@ -103,8 +82,8 @@ def walk(instructions, missing, early=None, busy=False):
     return missing
 
 
-def early_reads(body, split=blocks_of, busy=False):
-    blocks, follow = split(body)
+def early_reads(body, busy=False):
+    blocks, follow = blocks_of(body)
     state, todo, reached = {b: {} for b in blocks}, [""], {""}
     while todo:
         b = todo.pop()

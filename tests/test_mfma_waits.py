@@ -1,4 +1,5 @@
-"""Results of matrix instructions are waited for on every way through the kernels, with ways told apart at each branch (no GPU needed)."""
+"""Results of matrix instructions are waited for on every way through the kernels, with ways told apart at each branch (no GPU needed): the
+follower itself, and the rotations' kernels."""
 import os
 import subprocess
 
@@ -7,10 +8,9 @@ import pytest
 import mfma_waits
 from paper_2605_00422_amd import build
 
-FILES = ["attention8_tile.hip", "attention8_tile_e4m3.hip", "attention8_tile_f32.hip", "attention8_tile_f32_e4m3.hip",
-         "attention_tile.hip"]
-# ... where what lies between product and reading may be another product, which waits for the unit
-BUSY = ["rotate_quant.hip", "rotate_terms.hip", "rotate_terms_many.hip", "rotate_terms_f32.hip"]
+# What lies between a product and the reading of its result may be another product here, which waits for the unit.  (The attention's kernels are
+# followed in test_attention_waits.py and test_attention8_asm.py, by the compiler's rule.)
+FILES = ["rotate_quant.hip", "rotate_terms.hip", "rotate_terms_many.hip", "rotate_terms_f32.hip"]
 
 
 def test_what_a_branch_skips_does_not_count_as_waiting():
@@ -18,8 +18,15 @@ def test_what_a_branch_skips_does_not_count_as_waiting():
     ahead = ["v_mfma_f32_32x32x16_f16 v[0:15], v[16:19], v[20:23], 0", "s_cbranch_scc0 .LBB0_2"]
     long, read = ["v_add_f32_e32 v30, v31, v31"] * 20, [".LBB0_2:", "v_max_f32_e32 v30, v3, v3", "s_endpgm"]
     for label in (".LBB0_1:", "; %bb.1:"):
-        assert mfma_waits.early_reads(ahead + [label] + long + read, mfma_waits.blocks_at_branches)
-        assert not mfma_waits.early_reads(ahead[:1] + ["s_nop 11"] + ahead[1:] + [label] + long + read, mfma_waits.blocks_at_branches)
+        assert mfma_waits.early_reads(ahead + [label] + long + read)
+        assert not mfma_waits.early_reads(ahead[:1] + ["s_nop 11"] + ahead[1:] + [label] + long + read)
+
+
+def test_a_product_that_reads_another_ones_result_as_an_operand():
+    ahead, nops = ["v_mfma_f32_16x16x32_f16 v[0:3], v[16:19], v[20:23], 0"], ["s_nop 7"]
+    for operands, early in (("v[0:3], v[20:23], v[4:7]", True), ("v[20:23], v[0:3], v[4:7]", True), ("v[16:19], v[20:23], v[0:3]", False)):
+        last = [f"v_mfma_f32_16x16x32_f16 v[0:3], {operands}", "s_endpgm"]
+        assert bool(mfma_waits.early_reads(ahead + last)) == early and not mfma_waits.early_reads(ahead + nops + last)
 
 
 def test_a_product_in_between_waits_for_the_unit():
@@ -30,7 +37,7 @@ def test_a_product_in_between_waits_for_the_unit():
     assert mfma_waits.early_reads(two + ["s_nop 3"] + read) and not mfma_waits.early_reads(two + ["s_nop 6"] + read)
 
 
-@pytest.mark.parametrize("name", FILES + BUSY)
+@pytest.mark.parametrize("name", FILES)
 def test_results_of_matrix_instructions_are_waited_for(tmp_path, name):
     if not os.path.exists(build.HIPCC):
         pytest.skip("hipcc not available")
@@ -40,6 +47,6 @@ def test_results_of_matrix_instructions_are_waited_for(tmp_path, name):
     found = 0
     for kernel, body in mfma_waits.kernels(open(out).read().split("\n")):
         found += 1
-        early = mfma_waits.early_reads(body, mfma_waits.blocks_at_branches, name in BUSY)
+        early = mfma_waits.early_reads(body, busy=True)
         assert not early, (kernel, early[:3])
     assert found
