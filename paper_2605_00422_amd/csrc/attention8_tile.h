@@ -437,7 +437,9 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
             const bool plainly = whole && (GENERAL || !apart);
             // scales of pages of which no row sees a key may be anything, and count as 0
             {
-                const bool in_use = even || ((any >> (lane & 56)) & 0xff) != 0;
+                // (an even block's keys up to the last row's are seen, and those of the prefix; what lies behind costs these rows no bits)
+                const int group = j0 + (lane & 56);
+                const bool in_use = even ? group <= w_last || group < s.prefix : ((any >> (lane & 56)) & 0xff) != 0;
                 const float vscale = in_use ? now.vscale : 0.f;
                 if (__builtin_expect(some(vscale > top_scale), 0)) {
                     const float up = fmaxf(fmaxf(bwla_wave_max(vscale), top_scale), 0x1p-126f), f = top_scale / up;       // (a reciprocal has to be there)
