@@ -282,9 +282,11 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
     };
     // Weights of a tile's scores as they enter the second product, w F vs / S (F = 2^11), and the sums of w alone.  (Without cap and bias scores
     // stay products until here: y - m is rounded once.)  One term: the factor is part of the exponent, and goes out of the sum for four keys
-    // at once, which takes an instruction less a score and costs 2^-20 of a weight.  Two terms: the weight, then the product.
+    // at once, which takes an instruction less a score and costs a weight 2^-15 at most: the logarithm is rounded where m is taken off it.  Two
+    // terms: the weight, then the product.
+    bool huge = false;                                 // scores of HUGE and more, from which m is taken off before
     auto weigh = [&](const v16f& sc, Packed& out, int k) {
-        const float base = m == -INFINITY ? 0.f : m;
+        const float base = huge || m == -INFINITY ? 0.f : m;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             float w[8];
@@ -337,9 +339,10 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
     auto hold = [&](Packed& p) {
         if constexpr (T == 1) asm volatile("" : "+v"(p.w[0].t[0]), "+v"(p.w[1].t[0]), "+v"(l));
     };
-    // Scores of 2^20 and more, of which m, a rounded one, would be off by whole numbers: from there on products are rounded before m is
-    // taken off, so that the largest has a weight of 1 whatever its size.
-    bool huge = false;
+    // Large scores.  From 2^20 on m, a rounded one, would be off by whole numbers of products that are not, and with one term the
+    // logarithm of the values' factor loses bits to m much sooner.  There products are rounded, and m is taken off them before anything
+    // else is added, so that the largest has a weight of 1 whatever its size, and keys weigh as their values' scales say.
+    constexpr float HUGE_SCORE = T == 1 ? 0x1p10f : 0x1p20f;
     auto round_now = [&](v16f& sc, int k) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[r] *= kg[4 * k + r / 4];
@@ -367,11 +370,10 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
             for (int d = 0; d < DT; ++d)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[d][r] *= f;
-            if constexpr (!GENERAL) {
-                if (__builtin_expect(!huge && some(fabsf(m) >= 0x1p20f && m > -INFINITY), 0)) {
-                    huge = true;
-                    round_now(sc, k);
-                }
+            if constexpr (!GENERAL || T == 1) {        // (two terms and a cap or a bias: scores are rounded as it is)
+                const bool was = huge;
+                huge = some(fabsf(m) >= HUGE_SCORE && m > -INFINITY);
+                if (!GENERAL && __builtin_expect(huge && !was, 0)) round_now(sc, k);
             }
         }
     };
@@ -522,7 +524,8 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
                 if (!__builtin_expect(plainly && !huge, 1)) {
                     if (!GENERAL && apart) scaled();
                     if (!GENERAL && huge) round_now(sc, k);
-                    if (even) {
+                    if (plainly) {                     // (here for the rounding alone)
+                    } else if (even) {
                         const int most = (mine ? max(me.i, s.prefix - 1) : -1) - j0 - k * 32 - 4 * hf;
 #pragma unroll
                         for (int r = 0; r < 16; ++r) sc[r] = (r & 3) + 8 * (r >> 2) <= most ? sc[r] : -INFINITY;
@@ -533,6 +536,11 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
                     }
                 }
                 raise(sc, k, first);
+                if (__builtin_expect(huge, 0)) {
+                    const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) sc[r] -= base;
+                }
             };
             // (Order and priorities as in the kernel of the other types: the weights of one tile are taken while the other's products run.)
             constexpr int MFMAS = CS * T, VALU = 88;

@@ -2,6 +2,7 @@
 import numpy as np
 import pytest
 
+from oracle import bwla_attention_oracle as orc
 from test_gpu_attention8 import A, CODES, Case, call  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -26,3 +27,34 @@ def test_a_page_of_large_scales_costs_earlier_rows_nothing(A, code, dtype, page,
     assert rows > 0
     assert torch.equal(out[:rows], want[:rows]) and torch.equal(lse[:rows], lse0[:rows])
     assert not torch.equal(out[rows:], want[rows:]) and torch.isfinite(out.float()).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("n,new", [(96, 96), (400, 60), (300, 3)])
+@pytest.mark.parametrize("size", [2.0 ** 3, 2.0 ** 9, 2.0 ** 12, -2.0 ** 14, 2.0 ** 17, -2.0 ** 19, 2.0 ** 19, 2.0 ** 21])
+@pytest.mark.parametrize("form", ["plain", "cap", "bias"])
+def test_equal_scores_weigh_as_their_values_scales_say(A, code, dtype, n, new, size, form):  # noqa: F811
+    """Every key has the same score, of any size, in pages of different scales of values: outputs are means of the values.  A weight is off by the
+    rounding of its term and, in bf16, by 2^-15 (bounds: test_gpu_attention8.py; the scores' own errors are the same for all keys), lse by
+    roundings of the score."""
+    import torch
+    u = 2.0 ** -24
+    c = Case(code, dtype, 64, 4, 2, 16, [n], [new], seed=51)
+    one = torch.tensor([1.0]).to(torch.float8_e4m3fn).view(torch.uint8).item() if code == "e4m3" else 1
+    k = c.k.view(torch.uint8)
+    k.zero_()
+    k[..., 0] = one
+    c.ks.fill_(1.0)
+    c.kv[0][0][:] = 0
+    c.kv[0][0][..., 0] = 1.0
+    c.q.zero_()
+    c.q[..., 0] = 8.0 * size
+    kw = {"plain": {}, "cap": {"cap": 2.0 ** 23}, "bias": {"slopes": torch.zeros(4, device="cuda")}}[form]
+    out, lse = call(c, A, kw)
+    want, lse_want, _, vabs, _, _ = orc.attend(c.q.double().numpy(), *c.kv[0], c.d ** -0.5, **({"cap": 2.0 ** 23} if form == "cap" else {}))
+    bf = dtype == "bf16"
+    weight = 2.0 ** -11 + 2.0 ** -15 if bf else 2.0 ** -22
+    bound = vabs * (weight + (2 * n + 24) * u) + np.abs(want) * (2.0 ** -8 if bf else 4 * u) + n * 2.0 ** -35 * np.abs(c.kv[0][1]).max()
+    assert np.all(np.abs(out.double().cpu().numpy() - want) <= bound), np.max(np.abs(out.double().cpu().numpy() - want) / bound)
+    assert np.all(np.abs(lse.double().cpu().numpy() - lse_want) <= 16 * u * (np.abs(lse_want) + 1) + (2 * n + 24) * u + (2.0 ** -17 if bf else 0))
