@@ -53,7 +53,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
     using S = At8Shape<DP>;
     constexpr bool BF = T == 1;
     constexpr int ES = BF ? 2 : 4, BK = S::BK, ROWB = S::ROWB, CH = S::CH, DT = DP / 32, CS = CH / 2;
-    constexpr bool GENERAL = FORM != ATT_PLAIN;
+    constexpr bool GENERAL = FORM != ATT_PLAIN, CAPS = FORM == ATT_LONG || (FORM == ATT_SHORT && DP < 256);
     extern __shared__ __align__(16) char smem[];
     char* const ks = smem;                             // [2][BK][ROWB]
     char* const vs = smem + 2 * S::TILE;
@@ -435,7 +435,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
             // every row sees every key
             const bool whole = even && !some(!(mine | blind)) && (j0 + BK - 1 <= w_first || j0 + BK <= s.prefix);
             // a bias alone, and keys no later than rows: no cap, no distance either way
-            [[maybe_unused]] const bool linear = GENERAL && a.capped == 0.f && a.slopes && !s.pos && (j0 >= s.prefix || j0 + BK - 1 <= w_first);
+            [[maybe_unused]] const bool linear = GENERAL && (!CAPS || a.capped == 0.f) && a.slopes && !s.pos && (j0 >= s.prefix || j0 + BK - 1 <= w_first);
             const bool plainly = whole && (GENERAL || !apart);
             // scales of pages of which no row sees a key may be anything, and count as 0
             {
@@ -453,7 +453,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
                     down = 1.f / up;
                 }
                 // (never 0: an unseen key's product is -inf, and a page of zeros still has weights; 2^-60 is nothing beside 2^11)
-                const float kq = fmaxf(ldexpf(now.kscale, q_exponent) * (GENERAL && a.capped != 0.f ? 1.f : a.c1), 0x1p-126f), vq = vscale * down * 2048.f, vn = fmaxf(vq, 0x1p-60f);
+                const float kq = fmaxf(ldexpf(now.kscale, q_exponent) * (CAPS && a.capped != 0.f ? 1.f : a.c1), 0x1p-126f), vq = vscale * down * 2048.f, vn = fmaxf(vq, 0x1p-60f);
                 const float logarithm = __builtin_amdgcn_logf(vn);
                 // (of the logarithm as it is, rounded: what goes out of the sum is what went in)
                 const float factor = T == 1 ? __builtin_amdgcn_exp2f(-logarithm) : vq;
@@ -494,13 +494,14 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
                     } else {
 #pragma unroll
                         for (int r = 0; r < 16; ++r) sc[r] *= kg[4 * k + r / 4];
-                        if (a.capped != 0.f) {
+                        if (CAPS && a.capped != 0.f) {
                             // The short form, off by 1.2e-7 of the cap, where every row sees every key, so that little of it is left in their
                             // sum (a row of two keys has an lse of 2, of which that is 1e-6); a prompt of 4096 with it there and nowhere: 269 and 284 us.
-                            // (256 columns: everywhere, as another body spills: 2048 rows with a bias 200 -> 239 us.)
+                            // (256 columns: nowhere, and caps in an instance of their own, as another body spills: 2048 rows with a bias 195 -> 239 us, with
+                            // a cap 181, where the short form for all of them takes 160.)
                             if constexpr (FORM == ATT_LONG && DP < 256) {
                                 capped_scores<16>(a, sc);
-                            } else if (FORM == ATT_SHORT && (DP == 256 || whole)) {
+                            } else if (FORM == ATT_SHORT && whole) {
                                 const float c3 = a.c2 * (2.f * ATT_LOG2E);
 #pragma unroll
                                 for (int r = 0; r < 16; ++r)
@@ -633,7 +634,7 @@ hipError_t at8_launch(const AttArgs& a, const Att8& e8, const AttSplit& sp, void
     if ((int64_t)tiles * units * sp.splits >= 1 << 24) return hipErrorInvalidConfiguration;       // (a grid has fewer than 2^32 threads)
     const AtOrder order = at_order_of(tiles, units, sp.splits, at8_groups<T, DP>());
     constexpr int lds = At8Shape<DP>::LDS;
-    const int form = att_form(a, T == 1);
+    const int form = DP == 256 && a.capped != 0.f ? ATT_LONG : att_form(a, T == 1);
     const bool exact = a.d == DP;
     float* const part = (float*)ws;
     float4* const stat = (float4*)((char*)ws + sp.part_bytes);

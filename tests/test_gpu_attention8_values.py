@@ -58,3 +58,30 @@ def test_equal_scores_weigh_as_their_values_scales_say(A, code, dtype, n, new, s
     bound = vabs * (weight + (2 * n + 24) * u) + np.abs(want) * (2.0 ** -8 if bf else 4 * u) + n * 2.0 ** -35 * np.abs(c.kv[0][1]).max()
     assert np.all(np.abs(out.double().cpu().numpy() - want) <= bound), np.max(np.abs(out.double().cpu().numpy() - want) / bound)
     assert np.all(np.abs(lse.double().cpu().numpy() - lse_want) <= 16 * u * (np.abs(lse_want) + 1) + (2 * n + 24) * u + (2.0 ** -17 if bf else 0))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("d", [64, 128, 144, 256])
+@pytest.mark.parametrize("new", [1, 90])
+@pytest.mark.parametrize("cap", [50.0, 127.0, 300.0])
+def test_caps_of_rows_that_see_one_key(A, code, dtype, d, new, cap):  # noqa: F811
+    """Products of one column, without roundings of sums: lse is the capped score, off by a few units of itself, for heads of every width."""
+    import torch
+    u = 2.0 ** -24
+    c = Case(code, dtype, d, 4, 2, 16, [100], [new], seed=52)
+    one = torch.tensor([1.0]).to(torch.float8_e4m3fn).view(torch.uint8).item() if code == "e4m3" else 1
+    c.k.view(torch.uint8).zero_()
+    c.k.view(torch.uint8)[..., 0] = one
+    c.ks.fill_(1.0)
+    c.kv[0][0][:] = 0
+    c.kv[0][0][..., 0] = 1.0
+    first = c.q[..., 0].clone()
+    c.q.zero_()
+    c.q[..., 0] = 8 * first
+    _, lse = call(c, A, {"cap": cap, "window": 1})
+    _, want, _, _, _, _ = orc.attend(c.q.double().numpy(), *c.kv[0], np.float64(np.float32(d ** -0.5)), cap=cap, window=1)
+    assert np.abs(want).max() > 0.3 and np.abs(want).max() < 0.25 * cap
+    # scale, cap, change of base there and back, tanh (4 u), the logarithm of 1: below 12 u of the score; bf16 many rows: the factor of the values, 2^-20
+    bound = 12 * u * np.abs(want) + 4 * u + (2.0 ** -20 if dtype == "bf16" else 0)
+    assert np.all(np.abs(lse.double().cpu().numpy() - want) <= bound), np.max(np.abs(lse.double().cpu().numpy() - want) / bound)
