@@ -644,7 +644,9 @@ BWLA_API bwla_status_t bwla_attention8_forward(const bwla_kv_cache8_t* cache, co
 
 /*
  * Free pages in a ring of `capacity` entries: those of entries (front + i) % capacity, i < count, where d_state holds front and count.
- * `pages`: pages of the pool; table entries outside [0, pages) name none.
+ * `pages`: pages of the pool; table entries outside [0, pages) name none.  A capacity of `pages` or more has room for every page; of pages
+ * that a call gives back the ring keeps as many as it has room for, in order, and the others are in no ring and no table then, without
+ * a sign in d_status.
  */
 typedef struct bwla_page_pool {
     int32_t* d_ring;

@@ -443,7 +443,8 @@ def attention8_forward(cache: KVCache8, batch: Batch, score: Score, q, out, lse=
 
 class PagePool:
     """Free pages.  ring (capacity): int32; state (2): int32, the ring's front and how many pages lie there; state_out: where a call
-    leaves both (None: in state).  pages: of the pool (default: capacity)."""
+    leaves both (None: in state).  pages: of the pool (default: capacity; where there are more, pages given back that the ring has no room for
+    are lost)."""
 
     def __init__(self, ring, state, page_size, state_out=None, pages=None):
         _types()
