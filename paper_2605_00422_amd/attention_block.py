@@ -59,7 +59,9 @@ class AttentionBlock:
         return self._rows[M]
 
     def __call__(self, x, batch: A.Batch, position, y, watch=None, **score):
-        """x (tokens, columns of qkv), bfloat16 or float32 -> y (tokens, rows of o), float32.  position: int32 (axes, tokens).
+        """x (tokens, columns of qkv), bfloat16 or float32 -> y (tokens, rows of o), float32.  position: int32 (axes, tokens).  Rows of no
+        sequence (padding, all rows of a batch that is empty) get no attention: both layers run on them, the second one on whatever an earlier call
+        left there, and what y has in them is to be dropped.
         watch: whether the weights that this call's queries give count (None: where the cache has sums); the new tokens' sums start at zero
         either way."""
         watch = not self.eight if watch is None else watch
@@ -108,7 +110,8 @@ class Requests:
     """The tables of up to n requests of up to max_len tokens each, over a pool of pages, built on the GPU.  step(new, done) gives the batch and
     the positions (one axis) of new[b] more tokens of each request; done[b]: of a new request, in the place of one that is done.  rows and most:
     bounds of all new tokens and of a request's, known on the host (new and done are int32 tensors, which are not read there).  The batch of a
-    step that does not fit is empty, and status says why (attention_binding.batch_build): pages missing, requests too long, rows missing.
+    step that does not fit is empty, and status says why (attention_binding.batch_build): pages missing, requests too long, rows missing.  (A block that
+    is called with it writes nothing to the cache, and its outputs mean nothing.)
     Batches of one object share their tensors: each holds until the next step."""
 
     def __init__(self, n: int, max_len: int, pages: int, page_size: int, device="cuda"):
