@@ -242,7 +242,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
-    float m = -INFINITY, l = 0.f;
+    float m = -INFINITY, l = 0.f, base = 0.f;          // base: what weights take off their scores, m where there is one and it is not taken off before
     float top_scale = 0.f, down = 0.f;                 // S, and 2^11 / S
 
     // where lane (i = lane & 15 of each 16) of a transposing read takes its 8 bytes: key 4 hf + (i >> 2), columns
@@ -282,11 +282,10 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
     };
     // Weights of a tile's scores as they enter the second product, w F vs / S (F = 2^11), and the sums of w alone.  (Without cap and bias scores
     // stay products until here: y - m is rounded once.)  One term: the factor is part of the exponent, and goes out of the sum for four keys
-    // at once, which takes an instruction less a score and costs a weight 2^-15 at most: the logarithm is rounded where m is taken off it.  Two
+    // at once, which takes an instruction less a score and costs a weight 2^-13 at most: the logarithm is rounded where m is taken off it.  Two
     // terms: the weight, then the product.
-    bool huge = false;                                 // scores of HUGE and more, from which m is taken off before
+    bool huge = false;                                 // scores of HUGE_SCORE and more, from which m is taken off before
     auto weigh = [&](const v16f& sc, Packed& out, int k) {
-        const float base = huge || m == -INFINITY ? 0.f : m;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             float w[8];
@@ -342,7 +341,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
     // Large scores.  From 2^20 on m, a rounded one, would be off by whole numbers of products that are not, and with one term the
     // logarithm of the values' factor loses bits to m much sooner.  There products are rounded, and m is taken off them before anything
     // else is added, so that the largest has a weight of 1 whatever its size, and keys weigh as their values' scales say.
-    constexpr float HUGE_SCORE = T == 1 ? 0x1p10f : 0x1p20f;
+    constexpr float HUGE_SCORE = T == 1 ? 0x1p12f : 0x1p20f;
     auto round_now = [&](v16f& sc, int k) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[r] *= kg[4 * k + r / 4];
@@ -370,9 +369,11 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
             for (int d = 0; d < DT; ++d)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[d][r] *= f;
+            base = m == -INFINITY ? 0.f : m;
             if constexpr (!GENERAL || T == 1) {        // (two terms and a cap or a bias: scores are rounded as it is)
                 const bool was = huge;
                 huge = some(fabsf(m) >= HUGE_SCORE && m > -INFINITY);
+                base = huge || m == -INFINITY ? 0.f : m;
                 if (!GENERAL && __builtin_expect(huge && !was, 0)) round_now(sc, k);
             }
         }
@@ -440,8 +441,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
             // scales of pages of which no row sees a key may be anything, and count as 0
             {
                 // (an even block's keys up to the last row's are seen, and those of the prefix; what lies behind costs these rows no bits)
-                const int group = j0 + (lane & 56);
-                const bool in_use = even ? group <= w_last || group < s.prefix : ((any >> (lane & 56)) & 0xff) != 0;
+                const bool in_use = even ? j0 + (lane & 56) <= max(w_last, s.prefix - 1) : ((any >> (lane & 56)) & 0xff) != 0;
                 const float vscale = in_use ? now.vscale : 0.f;
                 if (__builtin_expect(some(vscale > top_scale), 0)) {
                     const float up = fmaxf(fmaxf(bwla_wave_max(vscale), top_scale), 0x1p-126f), f = top_scale / up;       // (a reciprocal has to be there)
@@ -497,8 +497,8 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
                         if (CAPS && a.capped != 0.f) {
                             // The short form, off by 1.2e-7 of the cap, where every row sees every key, so that little of it is left in their
                             // sum (a row of two keys has an lse of 2, of which that is 1e-6); a prompt of 4096 with it there and nowhere: 269 and 284 us.
-                            // (256 columns: nowhere, and caps in an instance of their own, as another body spills: 2048 rows with a bias 195 -> 239 us, with
-                            // a cap 181, where the short form for all of them takes 160.)
+                            // (256 columns: nowhere, and caps in an instance of their own, as another body spills: 2048 rows with a bias 197 -> 239 us, with
+                            // a cap 186, where the short form for all of them takes 160.)
                             if constexpr (FORM == ATT_LONG && DP < 256) {
                                 capped_scores<16>(a, sc);
                             } else if (FORM == ATT_SHORT && whole) {
@@ -538,9 +538,9 @@ __global__ __launch_bounds__(64 * AT_WAVES, (at8_groups<T, DP>())) void att8_til
                 }
                 raise(sc, k, first);
                 if (__builtin_expect(huge, 0)) {
-                    const float base = m == -INFINITY ? 0.f : m;
+                    const float all = m == -INFINITY ? 0.f : m;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) sc[r] -= base;
+                    for (int r = 0; r < 16; ++r) sc[r] -= all;
                 }
             };
             // (Order and priorities as in the kernel of the other types: the weights of one tile are taken while the other's products run.)
