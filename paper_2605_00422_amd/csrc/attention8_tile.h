@@ -11,10 +11,11 @@
 // than 2^-29 of a row's largest element is lost.  The maximum m moves where it is off by 2^4, so that weights times vs / S stay below
 // 2^4 and enter the second product times 2^11, in one term of 11 bits or two.
 //
-// Bound by vector instructions: a wavefront's block takes about 460 of them, 32 exponentials among them, beside 32 (128 columns) MFMA of 32
-// cycles, with two wavefronts a SIMD (an early form: MFMA 26 % of SIMD cycles, vector instructions 54 %, waits of some 4 cycles each 27 %).  A prompt
-// of 4096, 32 query heads of 128 columns, i8: 200 us, 687 TFLOP/s of the 1229 that a large fp16 product reaches; chunks of 333 behind up
-// to 7001, with a bias, 273 us; 1000 fp32 rows of documents 37 us, of which 17 are the start and a document's six blocks the rest.
+// Bound by vector instructions: a wavefront's block takes about 440 of them, 32 exponentials among them, beside 32 (128 columns) MFMA of 32
+// cycles, with two wavefronts a SIMD (a prompt: MFMA 30 % of SIMD cycles, vector instructions 57 %, a quarter of a wavefront's time spent waiting to
+// issue; chunks with a bias 26 and 56 %).  A prompt of 4096, 32 query heads of 128 columns, i8: 206 us, 667 TFLOP/s of the 1229 that a large fp16
+// product reaches; chunks of 333 behind up to 7001, with a bias, 283 us; 1000 fp32 rows of documents 37 us, of which 17 are the start and a
+// document's six blocks the rest.
 // Scales in the exponent and an instance for each code: 214 -> 199 us; one power of two for all rows alike, whatever their size: 198, but a row
 // beside larger ones lost its bits.  Not taken: eight wavefronts that share a block (prompt -3 %, chunks +9 %); conversions spread over the
 // products (spills: 533 us); three or four wavefronts a SIMD (spills).
@@ -634,6 +635,7 @@ hipError_t at8_launch(const AttArgs& a, const Att8& e8, const AttSplit& sp, void
     if ((int64_t)tiles * units * sp.splits >= 1 << 24) return hipErrorInvalidConfiguration;       // (a grid has fewer than 2^32 threads)
     const AtOrder order = at_order_of(tiles, units, sp.splits, at8_groups<T, DP>());
     constexpr int lds = At8Shape<DP>::LDS;
+    // (256 columns: caps have the instance that is exact to units of the score)
     const int form = DP == 256 && a.capped != 0.f ? ATT_LONG : att_form(a, T == 1);
     const bool exact = a.d == DP;
     float* const part = (float*)ws;
